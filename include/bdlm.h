@@ -433,6 +433,120 @@ int bdlm_gated_rmsnorm(int64_t batch, int64_t len, int64_t nheads, int64_t ngrou
                        void *stream);
 
 /*
+ * Dense operators around the scan: the projections of a Mamba-H layer (the mixer's input and
+ * output projections, the MLP's products), and the language-model head, whose logits never exist
+ * in memory: the most probable token of every position of a denoising step, and the masked
+ * training loss of the block objective (Eq. bdlm-masked-objective) with its gradient.
+ *
+ * Shape and layout of a call.  x is [rows][in_features], w is [out_features][in_features], both of
+ * in_dtype with unit innermost stride and row strides x_stride, w_stride in elements (rows of x and
+ * w may repeat or overlap; outputs' rows may not).  A row is a token: batch and block
+ * dimensions are one axis.  bdlm_dense_desc_init fills contiguous strides.
+ *   sizes      rows 0 .. 2^22, features 1 .. 2^22, any stride up to 2^40.
+ *   alignment  x, w, residual, pre, dy and the matrices written: base pointers 16-byte
+ *              aligned (strides are free, and bf16 matrices whose strides and in_features are
+ *              multiples of 8 are read as they lie; others are laid out anew in the
+ *              workspace).
+ *   workspace  device memory, 256-byte aligned, of at least the size the query returns for
+ *              the same descriptor; its contents are scratch.  Calls that share one must
+ *              not run concurrently (captured graphs that share one neither).
+ *   overlap    no output or workspace overlaps another argument (BDLM_E_SHAPE, BDLM_E_WORKSPACE),
+ *              except that a projection's out may be its residual.
+ * Products accumulate in fp32; fp32 operands are multiplied as three bf16 terms each
+ * (24 bits), so an infinity in one of them may come out as NaN.  Results do not depend on
+ * timing: sums are taken in a fixed order.
+ */
+typedef struct bdlm_dense_desc {
+    int64_t rows;
+    int64_t in_features;
+    int64_t out_features;   /* a head: the vocabulary */
+    int64_t x_stride;
+    int64_t w_stride;
+    int32_t in_dtype;       /* enum bdlm_dtype */
+    int32_t reserved;       /* must be 0 */
+} bdlm_dense_desc_t;
+
+/* GELU is z * Phi(z) with the normal distribution's Phi (no tanh). */
+enum bdlm_act { BDLM_ACT_NONE = 0, BDLM_ACT_SILU = 1, BDLM_ACT_GELU = 2 };
+
+int bdlm_dense_desc_init(bdlm_dense_desc_t *desc, int64_t rows, int64_t in_features,
+                         int64_t out_features, int32_t in_dtype);
+
+/*
+ * Projection: pre = x w^T + bias, out = act(pre) + residual.
+ * bias         device fp32 [out_features] or NULL.
+ * residual     device [rows][out_features], out_dtype, or NULL; may be out (same stride).
+ * out          device [rows][out_features], out_dtype (BDLM_DTYPE_F32 or BDLM_DTYPE_BF16).
+ * pre          device [rows][out_features], in_dtype, or NULL: kept for the gradient.
+ * Up to 64 rows need no workspace.
+ * Errors: BDLM_E_NULL, BDLM_E_SHAPE (also an unknown act), BDLM_E_DTYPE, BDLM_E_ALIGN,
+ * BDLM_E_WORKSPACE, BDLM_E_LAUNCH.  rows == 0 enqueues nothing.
+ */
+int bdlm_projection_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_projection(const bdlm_dense_desc_t *desc, int32_t act, int32_t out_dtype, const void *x,
+                    const void *w, const float *bias, const void *residual,
+                    int64_t residual_stride, void *out, int64_t out_stride, void *pre,
+                    int64_t pre_stride, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of a projection: dz = dy * act'(pre); dx = dz w, dw = dz^T x, db = sum of dz over
+ * the rows (the residual's gradient is dy itself).
+ * dy           device [rows][out_features], dy_dtype.
+ * pre          as kept by bdlm_projection; read only if act is not BDLM_ACT_NONE.
+ * dx, dw       device, in_dtype, shaped as x and w, or NULL (not wanted: w is read for dx
+ *              alone, x for dw alone).  db fp32 [out_features] or NULL.  rows == 0 zeroes
+ *              dw and db.
+ * With bf16 inputs dz is rounded to bf16 for the products (db sums it unrounded).
+ * Errors: as bdlm_projection.
+ */
+int bdlm_projection_backward_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t dy_dtype,
+                             const void *dy, int64_t dy_stride, const void *x, const void *w,
+                             const void *pre, int64_t pre_stride, void *dx, int64_t dx_stride,
+                             void *dw, int64_t dw_stride, float *db, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+
+/*
+ * Masked loss of a head: per row, with logits l = x w^T over the vocabulary,
+ *     lse = log sum exp l,   loss = lse - l[label].
+ * exclude      a token the softmax does not range over (the mask token, whose probability
+ *              a masked diffusion model sets to zero); negative or past the vocabulary: none.
+ * labels       device int64 [rows].  A row whose label is not a token that the softmax
+ *              ranges over (negative, past the vocabulary, or exclude) is left out: its loss,
+ *              lse and gradients are 0, and its logits are not computed.
+ * loss, lse    device fp32 [rows].
+ * The backward takes dloss, the gradient of the result by each row's loss (the block
+ * objective's weights), and the forward call's loss and lse:
+ *     dx = P w,  dw = P^T x,  P = dloss * (softmax - onehot(label)),
+ * forming the logits again in pieces of the vocabulary.  With bf16 inputs P is rounded to
+ * bf16.  dx, dw in_dtype, shaped as x and w, or NULL (not wanted).  rows == 0 zeroes dw.
+ * Errors: as bdlm_projection; BDLM_E_SHAPE where exclude is the vocabulary's only token.
+ */
+int bdlm_head_loss_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_head_loss(const bdlm_dense_desc_t *desc, const int64_t *labels, int64_t exclude,
+                   const void *x, const void *w, float *loss, float *lse, void *workspace,
+                   int64_t workspace_bytes, void *stream);
+int bdlm_head_loss_backward_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_head_loss_backward(const bdlm_dense_desc_t *desc, const int64_t *labels, int64_t exclude,
+                            const void *x, const void *w, const float *loss, const float *lse,
+                            const float *dloss, void *dx, int64_t dx_stride, void *dw,
+                            int64_t dw_stride, void *workspace, int64_t workspace_bytes,
+                            void *stream);
+
+/*
+ * Head of a denoising step: per row the most probable token (the lowest of equals) and the log
+ * of its probability, which says how sure the model is of it.
+ * token        device int64 [rows]; logprob device fp32 [rows].  NaN logits are passed over
+ *              for the token and make the logprob NaN; a row of nothing but NaN gives the
+ *              lowest token.
+ * exclude, errors  as bdlm_head_loss.  rows == 0 enqueues nothing.
+ */
+int bdlm_head_select_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_head_select(const bdlm_dense_desc_t *desc, int64_t exclude, const void *x, const void *w,
+                     int64_t *token, float *logprob, void *workspace, int64_t workspace_bytes,
+                     void *stream);
+
+/*
  * Host-only argument checks used by the entry points above, exported so they
  * can be exercised without a GPU.  Same arguments (the stream is not needed),
  * same return codes; nothing is enqueued and nothing is modified.
@@ -491,6 +605,29 @@ int bdlm_check_prefill(const bdlm_desc_t *desc, const void *x, const void *dt, c
                        const int64_t *n_blocks, int64_t expected_block_index,
                        int64_t blocks_in_prefix, const float *y_fwd, const void *workspace,
                        int64_t workspace_bytes);
+int bdlm_check_projection(const bdlm_dense_desc_t *desc, int32_t act, int32_t out_dtype,
+                          const void *x, const void *w, const float *bias, const void *residual,
+                          int64_t residual_stride, const void *out, int64_t out_stride,
+                          const void *pre, int64_t pre_stride, const void *workspace,
+                          int64_t workspace_bytes);
+int bdlm_check_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t dy_dtype,
+                                   const void *dy, int64_t dy_stride, const void *x,
+                                   const void *w, const void *pre, int64_t pre_stride,
+                                   const void *dx, int64_t dx_stride, const void *dw,
+                                   int64_t dw_stride, const float *db, const void *workspace,
+                                   int64_t workspace_bytes);
+int bdlm_check_head_loss(const bdlm_dense_desc_t *desc, const int64_t *labels, int64_t exclude,
+                         const void *x, const void *w, const float *loss, const float *lse,
+                         const void *workspace, int64_t workspace_bytes);
+int bdlm_check_head_loss_backward(const bdlm_dense_desc_t *desc, const int64_t *labels,
+                                  int64_t exclude, const void *x, const void *w,
+                                  const float *loss, const float *lse, const float *dloss,
+                                  const void *dx, int64_t dx_stride, const void *dw,
+                                  int64_t dw_stride, const void *workspace,
+                                  int64_t workspace_bytes);
+int bdlm_check_head_select(const bdlm_dense_desc_t *desc, int64_t exclude, const void *x,
+                           const void *w, const int64_t *token, const float *logprob,
+                           const void *workspace, int64_t workspace_bytes);
 
 #ifdef __cplusplus
 }

@@ -16,6 +16,11 @@ Entry points (same names as the C ABI):
   (the DiffuMamba-style contrast).
 * :func:`prefill` -- summarise a long clean prefix into the cached states in one call.
 * :func:`cache_reset` -- empty the given cache slots.
+* :func:`projection`, :func:`projection_backward` -- the layer's dense products with bias,
+  activation and residual, and their gradients.
+* :func:`head_select`, :func:`head_loss`, :func:`head_loss_backward` -- the language-model head
+  without its logits: the most probable tokens of a denoising step, and the masked training
+  loss with its gradient.
 
 :class:`Cache` bundles a state pool with its host-side bookkeeping.
 """
@@ -63,6 +68,19 @@ class Desc(ctypes.Structure):
         ("x_stride", ctypes.c_int64 * 3),
         ("dt_stride", ctypes.c_int64 * 2),
         ("bc_stride", ctypes.c_int64 * 3),
+    ]
+
+
+class DenseDesc(ctypes.Structure):
+    """Mirror of ``bdlm_dense_desc_t``."""
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("in_features", ctypes.c_int64),
+        ("out_features", ctypes.c_int64),
+        ("x_stride", ctypes.c_int64),
+        ("w_stride", ctypes.c_int64),
+        ("in_dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
     ]
 
 
@@ -131,6 +149,22 @@ def lib() -> ctypes.CDLL:
                                                i64, fp, f32, fp]
         L.bdlm_gated_rmsnorm.argtypes = [i64, i64, i64, i64, ctypes.c_int32, fp, vp, i64, i64, fp,
                                          f32, fp, vp]
+        ddp, i32 = ctypes.POINTER(DenseDesc), ctypes.c_int32
+        L.bdlm_dense_desc_init.argtypes = [ddp, i64, i64, i64, i32]
+        proj = [ddp, i32, i32, vp, vp, fp, vp, i64, vp, i64, vp, i64, vp, i64]
+        back = [ddp, i32, i32, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, fp, vp, i64]
+        loss = [ddp, vp, i64, vp, vp, fp, fp, vp, i64]
+        grad = [ddp, vp, i64, vp, vp, fp, fp, fp, vp, i64, vp, i64, vp, i64]
+        pick = [ddp, i64, vp, vp, vp, fp, vp, i64]
+        dense = ["bdlm_dense_desc_init"]
+        for name, args in (("projection", proj), ("projection_backward", back), ("head_loss", loss),
+                           ("head_loss_backward", grad), ("head_select", pick)):
+            getattr(L, "bdlm_" + name).argtypes = args + [vp]
+            getattr(L, "bdlm_check_" + name).argtypes = args
+            getattr(L, f"bdlm_{name}_workspace").argtypes = [ddp, i64p]
+            dense += ["bdlm_" + name, "bdlm_check_" + name, f"bdlm_{name}_workspace"]
+        for name in dense:
+            getattr(L, name).restype = ctypes.c_int
         for name in ("bdlm_desc_init", "bdlm_check_block_step", "bdlm_check_commit",
                      "bdlm_check_gated_rmsnorm", "bdlm_gated_rmsnorm",
                      "bdlm_scan_block_step", "bdlm_commit_boundary", "bdlm_cache_reset",
@@ -753,6 +787,244 @@ def gated_rmsnorm(y, z, norm_w, eps=1e-5, ngroups=1, out=None, stream=None):
     if rc != OK:
         raise BdlmError(rc, "bdlm_gated_rmsnorm")
     return out
+
+
+ACTS = {None: 0, "none": 0, "silu": 1, "gelu": 2}
+
+
+def _dtype_code(t, what: str) -> int:
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    raise ValueError(f"{what} must be bfloat16 or float32, got {t.dtype}")
+
+
+def _act_code(act) -> int:
+    if act not in ACTS:
+        raise ValueError(f"act must be None, 'none', 'silu' or 'gelu', got {act!r}")
+    return ACTS[act]
+
+
+def _rows2d(t, cols: int, what: str, lead=None):
+    """A [..., cols] tensor as its rows: (rows, row stride in elements).  The leading dimensions
+    have to lie at one stride; ``lead``: the leading shape asked for."""
+    if t.dim() < 1 or t.shape[-1] != cols or (lead is not None and tuple(t.shape[:-1]) != tuple(lead)):
+        want = "[..., %d]" % cols if lead is None else str((*lead, cols))
+        raise ValueError(f"{what} must have shape {want}, got {tuple(t.shape)}")
+    rows = 1
+    for n in t.shape[:-1]:
+        rows *= n
+    if rows == 0:
+        return 0, cols
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {what} must be unit stride")
+    stride, span = None, 1
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if stride is None:
+            stride, span = s, n
+        elif s != stride * span:
+            raise ValueError(f"the rows of {what} must lie at one stride")
+        else:
+            span *= n
+    return rows, cols if stride is None else stride
+
+
+def _dense(x, w):
+    """(descriptor, leading shape of x) of a call on x [..., in] and w [out, in]."""
+    torch = _torch()
+    if w.dim() != 2 or x.dim() < 1:
+        raise ValueError("x [..., in_features] and w [out_features, in_features] expected")
+    if x.dtype != w.dtype:
+        raise ValueError("x and w must share one dtype")
+    if x.device != w.device:
+        raise ValueError("x and w must be on one device")
+    d = DenseDesc()
+    d.in_dtype, d.reserved = _dtype_code(x, "x"), 0
+    n, k = w.shape
+    d.rows, d.x_stride = _rows2d(x, k, "x")
+    d.in_features, d.out_features = k, n
+    _, d.w_stride = _rows2d(w, k, "w")
+    return d, tuple(x.shape[:-1])
+
+
+def _place(t, shape, dtype, device, what: str):
+    """An output of ``shape``: new if ``t`` is None or True, else checked."""
+    torch = _torch()
+    if t is None or t is True:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not torch.is_tensor(t) or t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device:
+        got = (tuple(t.shape), t.dtype, t.device) if torch.is_tensor(t) else type(t)
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)} on {device}, got {got}")
+    return t
+
+
+def _vector(t, shape, dtype, device, what: str):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+                         f"got {tuple(t.shape)} {t.dtype} {t.device}")
+    return t
+
+
+def _dense_call(name: str, d, device, workspace, stream, args):
+    """One call of a dense operator on ``device``: its workspace and stream, then the C call."""
+    torch = _torch()
+    if device.type != "cuda":
+        raise ValueError("x must be a GPU tensor (no CPU path exists)")
+    fn = getattr(lib(), "bdlm_" + name)
+    need = _workspace_bytes(getattr(lib(), f"bdlm_{name}_workspace"), d)
+    with torch.cuda.device(device):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        elif workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {device}")
+        size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        s = torch.cuda.current_stream(device) if stream is None else stream
+        if s.device != device:
+            raise ValueError(f"stream must be one of {device}")
+        if stream is not None and workspace is not None:
+            workspace.record_stream(s)
+        rc = fn(ctypes.byref(d), *args, workspace.data_ptr() if size else None, size, s.cuda_stream)
+    if rc != OK:
+        raise BdlmError(rc, "bdlm_" + name)
+
+
+def _p(t):
+    return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
+def projection(x, w, bias=None, act=None, residual=None, out=None, pre=None, stream=None,
+               workspace=None):
+    """``act(x w^T + bias) + residual`` for x [..., in_features] and w [out_features, in_features]
+    (bfloat16 or float32, one stride between rows); ``act`` None, "silu" or "gelu".
+
+    ``bias`` float32 [out_features].  ``out`` (x's dtype if None; a given tensor may be
+    bfloat16 or float32) and ``residual`` (out's dtype; may be ``out`` itself) are
+    [..., out_features].  ``pre`` keeps x w^T + bias in x's dtype for the gradient: None (no),
+    True (allocate) or a tensor.  Returns out, or (out, pre) if ``pre`` was asked for.
+    """
+    torch = _torch()
+    code = _act_code(act)
+    d, lead = _dense(x, w)
+    shape = (*lead, d.out_features)
+    if out is None:
+        out = torch.empty(shape, dtype=x.dtype if residual is None else residual.dtype, device=x.device)
+    out = _place(out, shape, out.dtype, x.device, "out")
+    odt = _dtype_code(out, "out")
+    _, ldo = _rows2d(out, d.out_features, "out", lead)
+    if bias is not None:
+        _vector(bias, (d.out_features,), torch.float32, x.device, "bias")
+    ldr = 0
+    if residual is not None:
+        if residual.dtype != out.dtype or residual.device != x.device:
+            raise ValueError("residual must have out's dtype and device")
+        _, ldr = _rows2d(residual, d.out_features, "residual", lead)
+    ldp = 0
+    if pre is not None:
+        pre = _place(pre, shape, x.dtype, x.device, "pre")
+        _, ldp = _rows2d(pre, d.out_features, "pre", lead)
+    _dense_call("projection", d, x.device, workspace, stream,
+                (code, odt, _p(x), _p(w), _p(bias), _p(residual), ldr, _p(out), ldo, _p(pre), ldp))
+    return out if pre is None else (out, pre)
+
+
+def projection_backward(dy, x, w, pre=None, act=None, dx=True, dw=True, db=None, stream=None,
+                        workspace=None):
+    """Gradients of :func:`projection` by x, w and bias: (dx, dw, db), each None if not wanted.
+
+    ``dy`` [..., out_features] (bfloat16 or float32) is the gradient of the output, ``pre`` what
+    the forward call kept (needed with an activation).  ``dx``, ``dw``, ``db``: True
+    (allocate), None (not wanted) or a tensor; dx and dw have x's dtype, db is float32.
+    The residual's gradient is dy.
+    """
+    torch = _torch()
+    code = _act_code(act)
+    d, lead = _dense(x, w)
+    if dy.device != x.device:
+        raise ValueError("dy must be on x's device")
+    ydt = _dtype_code(dy, "dy")
+    _, ldy = _rows2d(dy, d.out_features, "dy", lead)
+    ldp = 0
+    if code != 0:
+        if pre is None:
+            raise ValueError("pre is needed for the gradient of an activation")
+        if pre.dtype != x.dtype or pre.device != x.device:
+            raise ValueError("pre must have x's dtype and device")
+        _, ldp = _rows2d(pre, d.out_features, "pre", lead)
+    else:
+        pre = None
+    ldx = ldw = 0
+    if dx is not None:
+        dx = _place(dx, x.shape, x.dtype, x.device, "dx")
+        _, ldx = _rows2d(dx, d.in_features, "dx", lead)
+    if dw is not None:
+        dw = _place(dw, w.shape, w.dtype, x.device, "dw")
+        _, ldw = _rows2d(dw, d.in_features, "dw")
+    if db is not None:
+        db = _vector(_place(db, (d.out_features,), torch.float32, x.device, "db"), (d.out_features,),
+                     torch.float32, x.device, "db")
+    _dense_call("projection_backward", d, x.device, workspace, stream,
+                (code, ydt, _p(dy), ldy, _p(x), _p(w), _p(pre), ldp, _p(dx), ldx, _p(dw), ldw, _p(db)))
+    return dx, dw, db
+
+
+def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, workspace=None):
+    """Masked loss of the head: (loss, lse), float32 of ``labels``' shape, for hidden states x
+    [..., in_features] and the vocabulary's weights w [tokens, in_features]:
+    ``lse = logsumexp(x w^T)`` over the tokens but ``exclude``, ``loss = lse - logit of the label``.
+
+    ``labels`` int64.  A row whose label is not a token that the softmax ranges over (negative, past
+    the vocabulary, or ``exclude``) is left out: its loss and lse are 0.  The logits are never
+    in memory."""
+    torch = _torch()
+    d, lead = _dense(x, w)
+    _vector(labels, lead, torch.int64, x.device, "labels")
+    loss = _vector(_place(loss, lead, torch.float32, x.device, "loss"), lead, torch.float32, x.device, "loss")
+    lse = _vector(_place(lse, lead, torch.float32, x.device, "lse"), lead, torch.float32, x.device, "lse")
+    _dense_call("head_loss", d, x.device, workspace, stream,
+                (_p(labels), int(exclude), _p(x), _p(w), _p(loss), _p(lse)))
+    return loss, lse
+
+
+def head_loss_backward(dloss, x, w, labels, loss, lse, exclude=-1, dx=True, dw=True, stream=None,
+                       workspace=None):
+    """Gradients of :func:`head_loss` by x and w: (dx, dw), each None if not wanted.
+
+    ``dloss`` float32 is the gradient of the result by each row's loss (the weights of the block
+    objective); ``loss`` and ``lse`` are what :func:`head_loss` returned for the same x, w,
+    labels and exclude.  ``dx``, ``dw``: True (allocate), None (not wanted) or a tensor."""
+    torch = _torch()
+    d, lead = _dense(x, w)
+    _vector(labels, lead, torch.int64, x.device, "labels")
+    for t, what in ((dloss, "dloss"), (loss, "loss"), (lse, "lse")):
+        _vector(t, lead, torch.float32, x.device, what)
+    ldx = ldw = 0
+    if dx is not None:
+        dx = _place(dx, x.shape, x.dtype, x.device, "dx")
+        _, ldx = _rows2d(dx, d.in_features, "dx", lead)
+    if dw is not None:
+        dw = _place(dw, w.shape, w.dtype, x.device, "dw")
+        _, ldw = _rows2d(dw, d.in_features, "dw")
+    _dense_call("head_loss_backward", d, x.device, workspace, stream,
+                (_p(labels), int(exclude), _p(x), _p(w), _p(loss), _p(lse), _p(dloss), _p(dx), ldx, _p(dw), ldw))
+    return dx, dw
+
+
+def head_select(x, w, exclude=-1, token=None, logprob=None, stream=None, workspace=None):
+    """The head of a denoising step: (token, logprob) for hidden states x [..., in_features] and the
+    vocabulary's weights w [tokens, in_features]: the most probable token (int64; the lowest of
+    equals) but ``exclude``, and the log of its probability (float32)."""
+    torch = _torch()
+    d, lead = _dense(x, w)
+    token = _vector(_place(token, lead, torch.int64, x.device, "token"), lead, torch.int64, x.device, "token")
+    logprob = _vector(_place(logprob, lead, torch.float32, x.device, "logprob"), lead, torch.float32, x.device,
+                      "logprob")
+    _dense_call("head_select", d, x.device, workspace, stream,
+                (int(exclude), _p(x), _p(w), _p(token), _p(logprob)))
+    return token, logprob
 
 
 def cache_reset(h_pool, slots=None, n_committed=None, n_blocks=None, stream=None):

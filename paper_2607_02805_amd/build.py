@@ -43,7 +43,9 @@ def _run(cmd: list[str]) -> None:
 
 HIP_SRCS = ("bdlm_scan.hip", "bdlm_seq.hip", "bdlm_seq16.hip", "bdlm_mask.hip", "bdlm_maskw.hip",
             "bdlm_conv.hip",
-            "bdlm_mix.hip", "bdlm_norm.hip", "bdlm_scratch.hip")
+            "bdlm_mix.hip", "bdlm_norm.hip", "bdlm_scratch.hip", "bdlm_tile.hip", "bdlm_skinny.hip",
+            "bdlm_dense.hip")
+CPP_SRCS = ("bdlm_api.cpp", "bdlm_dense_api.cpp")
 
 
 def _bind_cmd(out: str) -> list[str]:
@@ -68,15 +70,17 @@ def build(verbose: bool = False) -> str:
         cmds.append([HIPCC, *HIP_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c",
                      os.path.join(CSRC, src), "-o", obj])
         objs.append(obj)
-    a_obj = os.path.join(BUILD, "bdlm_api.o")
-    cmds.append(["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", f"-I{INCLUDE}",
-                 f"-I{CSRC}", "-c", os.path.join(CSRC, "bdlm_api.cpp"), "-o", a_obj])
+    for src in CPP_SRCS:
+        obj = os.path.join(BUILD, src.replace(".cpp", ".o"))
+        cmds.append(["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-Wextra", f"-I{INCLUDE}",
+                     f"-I{CSRC}", "-c", os.path.join(CSRC, src), "-o", obj])
+        objs.append(obj)
     # the translation units are independent: compile them side by side
     with ThreadPoolExecutor(max_workers=min(len(cmds), os.cpu_count() or 1)) as ex:
         for f in [ex.submit(_run, c) for c in cmds]:
             f.result()
     tmp = LIB + ".tmp"
-    _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs, a_obj])
+    _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs])
     os.replace(tmp, LIB)
     btmp = BIND + ".tmp"
     _run(_bind_cmd(btmp))

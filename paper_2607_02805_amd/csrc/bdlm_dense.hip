@@ -1,0 +1,239 @@
+// bdlm_dense.hip -- gfx950 kernels around the products of the dense operators: operands laid out as
+// bf16 terms, the gradient of a projection's activation with the bias gradient's column sums, the
+// rows that count of a masked loss, and the merge of softmax records.  All are bound by the
+// bytes they move, and small beside the products they serve.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "bdlm.h"
+#include "bdlm_dense.h"
+#include "bdlm_dense_device.h"
+
+namespace bdlm {
+namespace {
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_a4;
+
+// Eight elements of a row from column c, zeros past cols.
+__device__ __forceinline__ void load8(const void *src, int64_t at, int n, bool bf16, float (&v)[8]) {
+    if (bf16) {
+        const uint16_t *p = static_cast<const uint16_t *>(src) + at;
+        if (n >= 8) {
+            const u32x4 u = *reinterpret_cast<const u32x4_a2 *>(p);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] = __uint_as_float(u[e] << 16);
+                v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? bf16_to_f32(static_cast<short>(p[e])) : 0.f;
+        }
+    } else {
+        const float *p = static_cast<const float *>(src) + at;
+        if (n >= 8) {
+            const u32x4 a = *reinterpret_cast<const u32x4_a4 *>(p), b = *reinterpret_cast<const u32x4_a4 *>(p + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(a[e]), v[4 + e] = __uint_as_float(b[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+        }
+    }
+}
+
+__device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, int terms, const float (&v)[8]) {
+    if (terms == 1) {
+        *reinterpret_cast<uint4 *>(dst) = uint4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]),
+                                                cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
+        return;
+    }
+    uint16_t h[8][3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) split_terms(v[e], h[e]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = h[2 * e][k] | uint32_t(h[2 * e + 1][k]) << 16;
+        *reinterpret_cast<uint4 *>(dst + k * plane) = uint4{u[0], u[1], u[2], u[3]};
+    }
+}
+
+// Thread: eight columns; a workgroup takes kPackRows rows of 64 x 8 columns with its four waves
+// (row r of every four).  The column sums are of the fp32 values, before they are rounded.
+template <bool GRAD>
+__global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
+    __shared__ float sums[4][64 * 8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = (blockIdx.x * 64 + lane) * 8;
+    const int rows = a.rows_dev ? *a.rows_dev : a.rows;
+    const int64_t r0 = int64_t(blockIdx.y) * kPackRows;
+    const int n = a.cols - c;
+    const bool here = c < a.ld_dst;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (here) {
+        for (int64_t r = r0 + wave; r < rows && r < r0 + kPackRows; r += 4) {
+            const int64_t from = a.row_of ? a.row_of[r] : r;
+            float v[8];
+            load8(a.src, from * a.ld + c, n, a.src_bf16, v);
+            if constexpr (GRAD) {
+                if (a.act != BDLM_ACT_NONE) {
+                    float z[8];
+                    load8(a.pre, from * a.ld_pre + c, n, a.pre_bf16, z);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = e < n ? v[e] * act_slope(z[e], a.act) : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[e];
+            }
+            if (a.dst) store_terms(a.dst + r * a.ld_dst + c, a.plane, a.terms, v);
+        }
+    }
+    if constexpr (GRAD) {
+        if (!a.colsum) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[wave][lane * 8 + e] = sum[e];
+        __syncthreads();
+        for (int x = threadIdx.x; x < 512; x += 256) {
+            const int col = blockIdx.x * 512 + x;
+            if (col < a.cols)
+                a.colsum[int64_t(blockIdx.y) * a.cols + col] = (sums[0][x] + sums[1][x]) + (sums[2][x] + sums[3][x]);
+        }
+    }
+}
+
+// Column sums of the blocks' partial sums: 64 columns a workgroup, four waves over the blocks.
+__global__ void __launch_bounds__(256) bdlm_colsum_kernel(const float *part, int blocks, int cols, float *out) {
+    __shared__ float sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int c = blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (c < cols)
+        for (int b = wave; b < blocks; b += 4) s += part[int64_t(b) * cols + c];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) out[c] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+}
+
+__device__ __forceinline__ bool counts(int64_t label, int64_t exclude, int vocab) {
+    return label >= 0 && label < vocab && label != exclude;
+}
+
+// One workgroup lists the rows that count, in order.
+__global__ void __launch_bounds__(1024) bdlm_rows_kernel(const RowsArgs a) {
+    __shared__ int wave_sum[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int base = 0;
+    for (int64_t r0 = 0; r0 < a.rows; r0 += 1024) {
+        const int64_t r = r0 + threadIdx.x;
+        const int64_t label = r < a.rows ? a.labels[r] : -1;
+        const bool ok = counts(label, a.exclude, a.vocab);
+        const uint64_t mask = __ballot(ok);
+        if (lane == 0) wave_sum[wave] = __popcll(mask);
+        __syncthreads();
+        int before = base, all = 0;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) before += wave_sum[w];
+            all += wave_sum[w];
+        }
+        if (ok) {
+            const int to = before + __popcll(mask & ((uint64_t(1) << lane) - 1));
+            a.row_of[to] = static_cast<int32_t>(r);
+            a.label[to] = static_cast<int32_t>(label);
+            if (a.dloss) {
+                a.weight_c[to] = a.dloss[r];
+                a.loss_c[to] = a.loss[r];
+                a.lse_c[to] = a.lse[r];
+            }
+        }
+        base += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *a.count = base;
+}
+
+// One wave per row merges its records.
+__global__ void __launch_bounds__(256) bdlm_finish_kernel(const FinishArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t i = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int n = a.count ? *a.count : a.rows;
+    if (a.labels && i < a.rows && !counts(a.labels[i], a.exclude, a.vocab) && lane == 0) {
+        a.loss[i] = 0.f;
+        a.lse[i] = 0.f;
+    }
+    if (i >= n) return;
+    Best m{-INFINITY, 0.f, kNoColumn};
+    for (int t = lane; t < a.ntile; t += 64) {
+        const int64_t o = i * a.ntile + t;
+        m = merge(m, Best{a.top[o], a.others[o], a.at[o]});
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const Best o{__shfl_xor(m.top, d, 64), __shfl_xor(m.others, d, 64), __shfl_xor(m.at, d, 64)};
+        m = merge(m, o);
+    }
+    if (lane != 0) return;
+    const float rest = log1pf(m.others);
+    if (a.labels) {
+        const int64_t r = a.row_of[i];
+        a.loss[r] = rest + (m.top - a.label_logit[i]);
+        a.lse[r] = m.top + rest;
+    } else {
+        a.token[i] = m.at == kNoColumn ? (a.exclude == 0 ? 1 : 0) : m.at;
+        a.logprob[i] = -rest;
+    }
+}
+
+__global__ void __launch_bounds__(256) bdlm_zero_rows_kernel(const int64_t *labels, int64_t exclude, int vocab,
+                                                             int rows, char *dx, int64_t ld, int cols, int esz) {
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        if (counts(labels[r], exclude, vocab)) continue;
+        for (int c = threadIdx.x; c < cols; c += 256) {
+            if (esz == 2) reinterpret_cast<uint16_t *>(dx)[r * ld + c] = 0;
+            else reinterpret_cast<float *>(dx)[r * ld + c] = 0.f;
+        }
+    }
+}
+
+int done() { return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH; }
+
+}  // namespace
+
+int launch_pack(const PackArgs &a, void *stream) {
+    if (a.rows <= 0) return BDLM_OK;
+    const dim3 g(static_cast<unsigned>((a.ld_dst + 511) / 512), static_cast<unsigned>(pack_row_blocks(a.rows)));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (a.act != BDLM_ACT_NONE || a.colsum) hipLaunchKernelGGL((bdlm_pack_kernel<true>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((bdlm_pack_kernel<false>), g, dim3(256), 0, s, a);
+    return done();
+}
+
+int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream) {
+    hipLaunchKernelGGL(bdlm_colsum_kernel, dim3((cols + 63) / 64), dim3(256), 0, static_cast<hipStream_t>(stream),
+                       part, blocks, cols, out);
+    return done();
+}
+
+int launch_rows(const RowsArgs &a, void *stream) {
+    hipLaunchKernelGGL(bdlm_rows_kernel, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(stream), a);
+    return done();
+}
+
+int launch_finish(const FinishArgs &a, void *stream) {
+    if (a.rows <= 0) return BDLM_OK;
+    hipLaunchKernelGGL(bdlm_finish_kernel, dim3((a.rows + 3) / 4), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    return done();
+}
+
+int launch_zero_rows(const int64_t *labels, int64_t exclude, int32_t vocab, int32_t rows, void *dx, int64_t ld,
+                     int32_t cols, int32_t bf16, void *stream) {
+    if (rows <= 0) return BDLM_OK;
+    hipLaunchKernelGGL(bdlm_zero_rows_kernel, dim3(rows < 4096 ? rows : 4096), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), labels, exclude, vocab, rows, static_cast<char *>(dx), ld,
+                       cols, bf16 ? 2 : 4);
+    return done();
+}
+
+}  // namespace bdlm
