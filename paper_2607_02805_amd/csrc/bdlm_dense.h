@@ -62,13 +62,15 @@ struct ProbArgs {
 
 // acc[row][col] = sum over k of row(row, k) * col(col, k), over `npair` pairs of planes.
 // The operand of `row` is [nrow][k] (or [k][nrow] if row_t), of `col` [ncol][k] ([k][ncol] if
-// col_t).  Operands are read in 16-byte pieces: ld a multiple of 8, bases 16-byte aligned, and
-// elements between a row's end and the next multiple of 8 zero (k) or readable (rows, columns).
+// col_t).  Operands are read in 16-byte pieces, 64 contraction indices at a time: ld a multiple of
+// 8, bases 16-byte aligned, rows readable up to a multiple of 8 columns; an operand whose
+// contraction index is contiguous holds zeros from k to the next multiple of 64, and if both
+// operands' is the slow one, `row` holds rows of zeros up to a multiple of 64.
 struct TileArgs {
     Mat row, col;
     int32_t nrow, ncol, k;
     const int32_t *nrow_dev, *k_dev;   // the count in device memory, at most nrow / k (null: nrow / k)
-    int32_t npair;                     // 1, 3 or 6
+    int32_t npair;                     // 1 or 6
     int32_t row_t, col_t;
     int32_t big;                       // 1: 256 x 256 tiles, 0: 128 x 128
     int32_t splits;                    // > 1: kTilePartial only
@@ -102,8 +104,8 @@ constexpr int32_t kSkinnyRows = 64;
 constexpr int32_t kSkinnyCols = 32;
 int launch_skinny(const SkinnyArgs &a, void *stream);
 
-// Copies an operand to bf16 terms: dst[p][r][0 .. width) from src rows (row_of: gathered),
-// zeros past cols.  terms 1 (bf16 source, or fp32 rounded to bf16) or 3 (fp32 source).
+// Copies an operand to bf16 terms: dst[p][r][0 .. ld_dst) from src rows (row_of: gathered),
+// zeros past cols, and rows of zeros past the last one up to a multiple of 64 (dst has them).  terms 1 (bf16 source, or fp32 rounded to bf16) or 3 (fp32 source).
 struct PackArgs {
     const void *src;
     int64_t ld;

@@ -74,7 +74,12 @@ __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
     const bool here = c < a.ld_dst;
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (here) {
-        for (int64_t r = r0 + wave; r < rows && r < r0 + kPackRows; r += 4) {
+        for (int64_t r = r0 + wave; r < (rows + 63) / 64 * 64 && r < r0 + kPackRows; r += 4) {
+            if (r >= rows) {
+                const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (a.dst) store_terms(a.dst + r * a.ld_dst + c, a.plane, a.terms, none);
+                continue;
+            }
             const int64_t from = a.row_of ? a.row_of[r] : r;
             float v[8];
             load8(a.src, from * a.ld + c, n, a.src_bf16, v);
@@ -175,13 +180,13 @@ __global__ void __launch_bounds__(256) bdlm_finish_kernel(const FinishArgs a) {
         m = merge(m, o);
     }
     if (lane != 0) return;
-    const float rest = log1pf(m.others);
+    const float rest = m.top == -INFINITY ? NAN : log1pf(m.others);
     if (a.labels) {
         const int64_t r = a.row_of[i];
         a.loss[r] = rest + (m.top - a.label_logit[i]);
         a.lse[r] = m.top + rest;
     } else {
-        a.token[i] = m.at == kNoColumn ? (a.exclude == 0 ? 1 : 0) : m.at;
+        a.token[i] = m.top == -INFINITY ? (a.exclude == 0 ? 1 : 0) : m.at;
         a.logprob[i] = -rest;
     }
 }

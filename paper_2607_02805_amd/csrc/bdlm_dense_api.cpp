@@ -97,7 +97,8 @@ Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split) {
     return best;
 }
 
-// An operand [rows][cols] of a tiled product: as it lies, or laid out anew as bf16 terms.
+// An operand [rows][cols] of a tiled product: as it lies, or laid out anew as bf16 terms (gathered,
+// fp32, or of strides and widths that the tiles do not take: whole buffers of 64 columns).
 struct Operand {
     const void *src;
     int64_t rows, cols, ld;
@@ -108,13 +109,13 @@ struct Operand {
 
     Operand(const void *p, int64_t r, int64_t c, int64_t s, int32_t dt, bool gather, Space &ws)
         : src(p), rows(r), cols(c), ld(s), dtype(dt) {
-        direct = !gather && dt == BDLM_DTYPE_BF16 && s % 8 == 0 && c % 8 == 0 && s <= kMaxDirect;
+        direct = !gather && dt == BDLM_DTYPE_BF16 && s % 8 == 0 && c % 64 == 0 && s <= kMaxDirect;
         if (direct) {
             mat = Mat{static_cast<const uint16_t *>(p), s, 0};
         } else {
             const int64_t w = up(c, 64);
-            copy = ws.take<uint16_t>(terms_of(dt) * r * w);
-            mat = Mat{copy, w, r * w};
+            copy = ws.take<uint16_t>(terms_of(dt) * up(r, 64) * w);
+            mat = Mat{copy, w, up(r, 64) * w};
         }
     }
     int lay(void *stream, const int32_t *row_of = nullptr, const int32_t *rows_dev = nullptr) const {
@@ -206,7 +207,7 @@ struct BackwardPlan {
         sx = shape_of(d.rows, d.in_features, steps_of(d.out_features, np), true);
         sw = shape_of(d.out_features, d.in_features, steps_of(d.rows, np), true);
         ld_dz = up(d.out_features, 64);
-        dz = ws.take<uint16_t>(terms_of(d.in_dtype) * d.rows * ld_dz);
+        dz = ws.take<uint16_t>(terms_of(d.in_dtype) * up(d.rows, 64) * ld_dz);
         sums = ws.take<float>(int64_t(pack_row_blocks(static_cast<int32_t>(d.rows))) * d.out_features);
         part = ws.take<float>(std::max(part_size(sx, d.rows, d.in_features),
                                        part_size(sw, d.out_features, d.in_features)));
@@ -293,7 +294,7 @@ struct LossBackwardPlan {
         sp = shape_of(d.rows, piece, steps_of(d.in_features, np), false);
         sx = shape_of(d.rows, d.in_features, steps_of(piece, np), true);
         sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true);
-        p = ws.take<uint16_t>(terms_of(d.in_dtype) * d.rows * piece);
+        p = ws.take<uint16_t>(terms_of(d.in_dtype) * up(d.rows, 64) * piece);
         part_x = ws.take<float>(sx.splits * d.rows * d.in_features);   // summed over the pieces
         part_w = ws.take<float>(part_size(sw, piece, d.in_features));
     }
@@ -474,8 +475,9 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int32_t dy
     // dy as it is, where it can be an operand; else dz (rounded to the inputs' type, as the
     // activations of the forward products are)
     const bool direct = act == BDLM_ACT_NONE && d->in_dtype == BDLM_DTYPE_BF16 && dy_dtype == BDLM_DTYPE_BF16 &&
-                        d->out_features % 8 == 0 && dy_stride % 8 == 0 && dy_stride <= kMaxDirect;
-    Mat dz{p.dz, p.ld_dz, d->rows * p.ld_dz};
+                        d->out_features % 64 == 0 && d->rows % 64 == 0 && dy_stride % 8 == 0 &&
+                        dy_stride <= kMaxDirect;
+    Mat dz{p.dz, p.ld_dz, up(d->rows, 64) * p.ld_dz};
     if (direct) dz = Mat{static_cast<const uint16_t *>(dy), dy_stride, 0};
     if (!direct || db) {
         PackArgs a{};
@@ -580,7 +582,7 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
                     stream));
     TRY(p.x.lay(stream, p.rows.row_of, p.rows.count));
     TRY(p.w.lay(stream));
-    const Mat pm{p.p, p.piece, d->rows * p.piece};
+    const Mat pm{p.p, p.piece, up(rows, 64) * p.piece};
     for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, vocab - v0);
         const Mat w_at{p.w.mat.p + v0 * p.w.mat.ld, p.w.mat.ld, p.w.mat.plane};

@@ -23,21 +23,41 @@ __device__ __forceinline__ void split_terms(float v, uint16_t (&t)[3]) {
     t[2] = static_cast<uint16_t>(bf16_bits(r1 - bf16_to_f32(static_cast<short>(t[1]))));
 }
 
+// The normal distribution's Phi(z), off by at most 3e-7, and e = exp(-z^2 / 2): with x = |z| / sqrt 2,
+// erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x) (Abramowitz and Stegun 7.1.26), on
+// the hardware's reciprocal and exponential.  The library's erfc costs three times as much, which
+// shows where a tile's epilogue is not hidden behind products.
+__device__ __forceinline__ float normal_cdf(float z, float &e) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+    e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
+    // half of erfc
+    const float h = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f),
+                                     0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
+    return z > 0.f ? 1.f - h : h;
+}
+// Values and slopes at infinities are the limits; a NaN stays one.
 __device__ __forceinline__ float act_value(float z, int act) {
-    if (act == BDLM_ACT_SILU) return z > -88.f ? z / (1.f + expf(-z)) : z != z ? z : 0.f;
-    if (act == BDLM_ACT_GELU) return fabsf(z) <= 3.4028234e38f ? 0.5f * z * erfcf(z * -0.70710678f) : (z < 0.f ? 0.f : z);
+    if (act == BDLM_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+        return z < -87.f ? 0.f : z * s;
+    }
+    if (act == BDLM_ACT_GELU) {
+        float e;
+        const float p = normal_cdf(z, e);
+        return z < -14.f ? 0.f : z * p;
+    }
     return z;
 }
 // d act / dz
 __device__ __forceinline__ float act_slope(float z, int act) {
     if (act == BDLM_ACT_SILU) {
-        const float c = fminf(fmaxf(z, -88.f), 88.f);
-        const float p = 1.f / (1.f + expf(-c));
-        return z != z ? z : p * (1.f + c * (1.f - p));
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+        return z < -87.f ? 0.f : z > 87.f ? 1.f : s * fmaf(z, 1.f - s, 1.f);
     }
     if (act == BDLM_ACT_GELU) {
-        const float c = fminf(fmaxf(z, -14.f), 14.f);
-        return z != z ? z : 0.5f * erfcf(c * -0.70710678f) + c * 0.39894228f * expf(-0.5f * c * c);
+        float e;
+        const float p = normal_cdf(z, e);
+        return z < -14.f ? 0.f : z > 14.f ? 1.f : fmaf(z * 0.39894228f, e, p);
     }
     return 1.f;
 }

@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(512) bdlm_skinny_kernel(const SkinnyArgs a) {
         f32x4 v = *reinterpret_cast<const f32x4 *>(part + r * kPitch + c);
         for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const f32x4 *>(part + (w * 16 * MT + r) * kPitch + c);
         if constexpr (OUT == kTileStore) {
-            if (r < a.nrow) store4(a.store, v, r, col0 + c, a.ncol);
+            if (r < a.nrow) store4(a.store, v, load_bias(a.store, col0 + c, a.ncol), r, col0 + c, a.ncol);
         } else {
             // eight consecutive lanes hold a row's 32 columns
             const BestArgs &b = a.best;

@@ -11,16 +11,22 @@ __device__ __forceinline__ float load_elem(const void *p, int64_t i, bool bf16) 
     return bf16 ? bf16_to_f32(static_cast<const short *>(p)[i]) : static_cast<const float *>(p)[i];
 }
 
-// Four consecutive columns of one row through a projection's epilogue.
-__device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, int64_t row, int col, int ncol) {
-    const int n = ncol - col < 4 ? ncol - col : 4;
-    if (n <= 0) return;
-    const int64_t ro = (s.row_of ? s.row_of[row] : row);
+__device__ __forceinline__ f32x4 load_bias(const StoreArgs &s, int col, int ncol) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (s.bias) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (e < n) v[e] += s.bias[col + e];
+            if (col + e < ncol) v[e] = s.bias[col + e];
     }
+    return v;
+}
+
+// Four consecutive columns of one row through a projection's epilogue.
+__device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, f32x4 bias, int64_t row, int col, int ncol) {
+    const int n = ncol - col < 4 ? ncol - col : 4;
+    if (n <= 0) return;
+    const int64_t ro = (s.row_of ? s.row_of[row] : row);
+    v += bias;
     if (s.pre) {
         const int64_t o = ro * s.ld_pre + col;
         if (s.pre_bf16) {

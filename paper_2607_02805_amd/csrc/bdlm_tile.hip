@@ -3,15 +3,14 @@
 // (bdlm_dense.h: the epilogue of a projection, partial sums, softmax records, loss gradients).
 //
 // One workgroup per tile (and split).  The operands go straight from memory to LDS in 16-byte
-// pieces, 64 contraction indices at a time into one of two buffers: while a buffer is multiplied
-// the next one fills.  `col` is the first MFMA operand, so a lane holds four consecutive
-// columns of one row and stores them together.
+// pieces, a stage of 64 contraction indices at a time into one of two buffers.  `col` is the
+// first MFMA operand, so a lane holds groups of four consecutive columns of one row.
 //
 // An operand whose contraction index is contiguous lies in LDS as [row][64] (eight pieces a
 // row) and is read 16 bytes a lane; one whose contraction index is the slow one lies as
 // [64][row] and is read with the LDS transpose read.  Both are permuted by the piece so that a
-// quarter wave meets every bank once; as the copy writes LDS in lane order, the permutation
-// is of the addresses in memory that the lanes read.
+// quarter wave meets every bank once (no conflicts counted); as the copy writes LDS in lane order,
+// the permutation is of the addresses in memory that the lanes read.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -23,14 +22,21 @@
 namespace bdlm {
 namespace {
 
-constexpr int kDepth = 64;   // contraction indices per buffer
+constexpr int kDepth = 64;    // contraction indices of a stage (a cache line of an operand's row)
+constexpr int kGroups = kDepth / 16;   // of products
 
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((address_space(1))) const void g_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-__device__ __forceinline__ void copy16(const char *from, uint4 *to) {
-    __builtin_amdgcn_global_load_lds((g_void *)from, (lds_void *)to, 16, 0, 0);
+// 16 bytes a lane from base + off to LDS at `to`, lane by lane.  Written out because the compiler
+// makes every LDS transpose read wait for the copies it knows of; nothing is returned in
+// registers, and step() waits for the copies before the barrier that hands a buffer over.
+__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint4 *to) {
+    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void *)to));
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(off), "s"(base), "s"(lds)
+                 : "memory", "m0");
 }
 __device__ __forceinline__ bf16x8 frag(const char *lds) {
     return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4 *>(lds));
@@ -38,20 +44,43 @@ __device__ __forceinline__ bf16x8 frag(const char *lds) {
 __device__ __forceinline__ s16x4 read_tr(const char *lds) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(const_cast<char *>(lds)));
 }
-__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// c += a b, in place: written out so that the accumulators stay in their registers (256 of them are
+// all the accumulation registers there are; given the builtin, the compiler rotates them
+// through copies).  The wait states cover an operand that the compiler has just moved; the
+// matrix pipeline is busy for longer than that.  At every edge of the control flow, where the
+// compiler may move accumulators, settle() waits for the last products' results.
+// 32 x 32 outputs a product: a wave issues an instruction every four cycles or so, and products of
+// 16 x 16 take 16 cycles, which leaves too few in between for the reads and copies.
+__device__ __forceinline__ void mma(bf16x8 a, bf16x8 b, f32x16 &c) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+// A product's results may be read by other instructions after at most 19 wait states.
+template <int FC, int FR>
+__device__ __forceinline__ void settle(f32x16 (&acc)[FC][FR]) {
+    asm volatile("s_nop 15\n\ts_nop 3");
+#pragma unroll
+    for (int i = 0; i < FC; ++i)
+#pragma unroll
+        for (int j = 0; j < FR; ++j) asm volatile("" : "+a"(acc[i][j]));
 }
 
-// One operand's share of a tile: R rows (or columns) from `first` on, 64 indices deep.
-template <int R, bool T, int WAVES>
+// The permutation of a contraction row's pieces (an operand whose contraction index is slow).
+__device__ __forceinline__ int piece_of(int t) { return 4 * (t & 3) ^ 2 * ((t >> 3) & 1); }
+
+// One operand's share of a tile: R rows (or columns) from `first` on, a stage deep.  REPEAT (T
+// only): contraction indices past the operand's end read another row again, as the other
+// operand is zero there.
+template <int R, bool T, int WAVES, bool REPEAT>
 struct Stage {
-    static constexpr int kPieces = R * kDepth / 8;        // 16-byte pieces of a buffer
+    static constexpr int kPieces = R * kDepth / 8;        // 16-byte pieces of a stage
     static constexpr int kLoads = kPieces / (64 * WAVES);   // per lane
     static_assert(kLoads * 64 * WAVES == kPieces, "whole loads");
     const char *base;      // the operand at (first, 0) of its first plane
     int64_t ld2;           // bytes of a row
     uint32_t off[kLoads];    // this lane's bytes from base
-    int32_t at[kLoads];      // contraction index of the piece within the buffer
+    int32_t at[T ? kLoads : 1];   // T: contraction index of the piece within the stage
 
     // rows past the operand's end repeat its last row, columns past it its first piece
     __device__ __forceinline__ void init(const Mat &m, int64_t first, int64_t size, int wave, int lane) {
@@ -63,73 +92,81 @@ struct Stage {
             if constexpr (T) {
                 constexpr int kRow = R / 8;
                 const int t = piece / kRow, pos = piece % kRow;
-                int c = pos ^ (2 * ((t & 3) | (((t >> 3) & 1) << 2)));
+                int c = pos ^ piece_of(t);
                 if (first + 8 * c >= size) c = 0;
                 at[i] = t;
                 off[i] = static_cast<uint32_t>(t * ld2 + c * 16);
             } else {
                 const int r = piece >> 3, c = (piece & 7) ^ ((r >> 1) & 7);
                 const int64_t rr = first + r < size ? r : size - 1 - first;
-                at[i] = 8 * c;
                 off[i] = static_cast<uint32_t>(rr * ld2 + c * 16);
             }
         }
     }
-    // left: contraction indices from this buffer's first to the operand's end
-    __device__ __forceinline__ void load(uint4 *lds, int64_t plane, int kt, int left, int wave) const {
-        const char *p = base + plane * 2 + (T ? kt * (kDepth * ld2) : kt * int64_t(2 * kDepth));
-        if (left >= kDepth) {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) copy16(p + off[i], lds + (i * WAVES + wave) * 64);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                copy16(at[i] < left ? p + off[i] : reinterpret_cast<const char *>(&kZeroChunk),
-                       lds + (i * WAVES + wave) * 64);
-        }
+    __device__ __forceinline__ const char *at_step(int64_t plane, int kt) const {
+        return base + plane * 2 + kt * stride();
+    }
+    __device__ __forceinline__ int64_t stride() const { return T ? kDepth * ld2 : 2 * kDepth; }   // of a stage
+    // left: contraction indices from the stage's first to the operand's end
+    __device__ __forceinline__ void copy(int i, const char *from, uint4 *lds, int left, int wave) const {
+        uint32_t o = off[i];
+        if constexpr (T && REPEAT) o = at[i] < left ? o : o - static_cast<uint32_t>(at[i] * ld2);
+        copy16(from, o, lds + (i * WAVES + wave) * 64);
     }
 };
 
-// Operand reads: fragment i (16 rows from `row0` + 16 i) of k step s (32 indices).
+// Operand reads: fragment i, 32 rows from `row0` + 32 i, of group g of the stage (16 indices).
+// Lane: row lane & 31, indices 8 (lane >> 5) .. + 7.
 template <int R, bool T, int F>
 struct Reader {
-    int off[T ? F : 2];
+    int off[T ? F : kGroups];
     __device__ __forceinline__ void init(int row0, int lane) {
-        const int kg = lane >> 4, s = lane & 15;
         if constexpr (T) {
-            const int t = 8 * kg + (s >> 2);
-            const int f = 2 * ((t & 3) | (((t >> 3) & 1) << 2));
+            const int s = lane & 15, t = 8 * (lane >> 5) + (s >> 2);
 #pragma unroll
             for (int i = 0; i < F; ++i) {
-                const int c = row0 / 8 + 2 * i + ((s & 3) >> 1);
-                off[i] = (t * (R / 8) + (c ^ f)) * 16 + (s & 1) * 8;
+                const int c = (row0 + 32 * i + (lane & 16)) / 8 + ((s & 3) >> 1);
+                off[i] = (t * (R / 8) + (c ^ piece_of(t))) * 16 + (s & 1) * 8;
             }
         } else {
+            const int r = row0 + (lane & 31);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) off[k] = (row0 + s) * 128 + (((4 * k + kg) ^ ((s >> 1) & 7)) * 16);
+            for (int g = 0; g < kGroups; ++g) off[g] = r * 128 + (((2 * g + (lane >> 5)) ^ ((r >> 1) & 7)) * 16);
         }
     }
-    __device__ __forceinline__ bf16x8 get(const char *lds, int i, int k) const {
+    __device__ __forceinline__ bf16x8 get(const char *lds, int i, int g) const {
         if constexpr (T) {
-            const char *p = lds + off[i] + k * (32 * 2 * R);
+            const char *p = lds + off[i] + g * (16 * 2 * R);
             const s16x4 a = read_tr(p), b = read_tr(p + 4 * 2 * R);
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            return frag(lds + off[k] + i * (16 * 128));
+            return frag(lds + off[g] + i * (32 * 128));
         }
     }
 };
 
-// Plane pairs in order of weight: pair i multiplies term kRowTerm[i] of `row` and kColTerm[i] of
-// `col`.  Three pairs: an fp32 row operand (gradients of the logits) with a bf16 one.
-__device__ __forceinline__ int row_term(int npair, int i) { return npair == 6 ? (0x010210 >> (4 * i)) & 15 : i; }
+// Plane pairs in order of weight: pair i multiplies term row_term(i) of `row` and col_term(i) of
+// `col`.
+__device__ __forceinline__ int row_term(int npair, int i) { return npair == 6 ? (0x010210 >> (4 * i)) & 15 : 0; }
 __device__ __forceinline__ int col_term(int npair, int i) { return npair == 6 ? (0x102010 >> (4 * i)) & 15 : 0; }
 
-// Four columns of one row of a tile, in its place.
+template <int V>
+struct Int {
+    static constexpr int value = V;
+};
+
+// What the epilogue needs of a row, kept in LDS from the start of the kernel.
+struct RowData {
+    float lse, g, hot;   // kTileProb: lse, weight, the label's gradient
+    int label;           // kTileProb, kTileBest
+};
+
+// Four columns of one row of a tile, in their place.
 template <int OUT>
-__device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, int64_t r, int c, int split) {
+__device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias, const RowData &d, int64_t r, int c,
+                                          int split) {
     if constexpr (OUT == kTileStore) {
-        store4(a.store, v, r, c, a.ncol);
+        store4(a.store, v, bias, r, c, a.ncol);
     } else if constexpr (OUT == kTilePartial) {
         float *to = a.part + (int64_t(split) * a.nrow + r) * a.ncol + c;
         if (c + 4 <= a.ncol && a.ncol % 4 == 0) {
@@ -142,14 +179,12 @@ __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, int64_t r,
     } else {
         const ProbArgs &b = a.prob;
         if (c >= b.width) return;
-        const float lse = b.lse[r], g = b.weight[r];
-        const int label = b.label[r] - b.col0, exclude = b.exclude - b.col0;
+        const int exclude = b.exclude - b.col0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float x = v[e] - lse;
-            v[e] = g * (b.terms == 1 ? __expf(x) : expf(x));
-            // the label's probability less one is exp(-loss) - 1, without cancellation
-            if (c + e == label) v[e] = g * expm1f(-b.loss[r]);
+            const float x = v[e] - d.lse;
+            v[e] = d.g * (b.terms == 1 ? __expf(x) : expf(x));
+            if (c + e == d.label) v[e] = d.hot;
             if (c + e >= a.ncol || c + e == exclude) v[e] = 0.f;
         }
         uint16_t *to = b.p + r * b.ld + c;
@@ -167,12 +202,61 @@ __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, int64_t r,
     }
 }
 
+// The softmax record of a row's columns col1 .. + cols - 1, which lie in LDS as quads permuted by
+// `swap`.  The largest value's place is overwritten, so that the others are all the rest.
+__device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap, int cols, int col1) {
+    int n = a.ncol - col1 < cols ? a.ncol - col1 : cols;   // columns that there are
+    n = n < 0 ? 0 : n;
+    const int nq = (n + 3) >> 2;
+    auto place = [&](int c) { return reinterpret_cast<float *>(row + ((c >> 2) ^ swap)) + (c & 3); };
+    for (int c = n; c < 4 * nq; ++c) *place(c) = -INFINITY;
+    const int x = a.best.exclude - col1;
+    if (x >= 0 && x < n) *place(x) = -INFINITY;
+    Best m{-INFINITY, 0.f, kNoColumn};
+    int first = -1;
+#pragma unroll 8
+    for (int q = 0; q < nq; ++q) {
+        const f32x4 v = row[q ^ swap];
+        const float t = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));   // (passes over a NaN)
+        first = t > m.top ? q : first;
+        m.top = fmaxf(m.top, t);
+    }
+    if (first >= 0) {
+        const f32x4 v = row[first ^ swap];
+        const int e = v[0] == m.top ? 0 : v[1] == m.top ? 1 : v[2] == m.top ? 2 : 3;
+        m.at = col1 + 4 * first + e;
+        *place(4 * first + e) = -INFINITY;
+    }
+    // -infinities add nothing, also where there is nothing else
+    const float ref = m.top == -INFINITY ? 0.f : m.top;
+#pragma unroll 8
+    for (int q = 0; q < nq; ++q) {
+        const f32x4 v = row[q ^ swap];
+        float s[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = __builtin_amdgcn_exp2f((v[e] - ref) * kLog2e);
+        m.others += (s[0] + s[1]) + (s[2] + s[3]);
+    }
+    return m;
+}
+
+// Four waves of (E / 2) x (E / 2) outputs.  A stage is four groups of products, each from one of two
+// sets of registers while the other fills with the next group's operands from LDS.  With
+// the last group's operands read, and the next stage arrived in the other buffer, the waves
+// meet; then the stage after it is copied into this buffer, half of it during the last group
+// and half during the next stage's first.
+//
+// E 256: one wave on each SIMD, 256 accumulators a lane.  E 128: two workgroups on a CU, so that
+// one's epilogue meets the other's products.
 template <int E, int WR, int WC, bool ROWT, bool COLT, int OUT>
-__global__ void __launch_bounds__(64 * WR * WC) bdlm_tile_kernel(const TileArgs a) {
-    constexpr int WAVES = WR * WC;
-    constexpr int FR = E / WR / 16, FC = E / WC / 16;   // fragments of a wave
-    constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's buffer
+__global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileArgs a) {
+    constexpr int WAVES = WR * WC, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
+    constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's stage
+    constexpr int kRec = OUT == kTileBest ? E : 1;
     __shared__ uint4 sm[2][2 * kBuf];                    // [buffer][col, then row]
+    __shared__ RowData rows[OUT == kTileProb || OUT == kTileBest ? E : 1];
+    __shared__ float top[WC][kRec], others[WC][kRec];    // softmax records of the waves' columns
+    __shared__ int at[WC][kRec];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nrow = a.nrow_dev ? *a.nrow_dev : a.nrow;
@@ -195,12 +279,12 @@ __global__ void __launch_bounds__(64 * WR * WC) bdlm_tile_kernel(const TileArgs 
     const int64_t row0 = int64_t(tile_r) * E, col0 = int64_t(tile_c) * E;
 
     const int nkt = (K + kDepth - 1) / kDepth;
-    const int steps = nkt * a.npair;
-    const int it0 = static_cast<int>(int64_t(steps) * split / a.splits);
-    const int it1 = static_cast<int>(int64_t(steps) * (split + 1) / a.splits);
+    const int64_t steps = int64_t(nkt) * a.npair;
+    const int it0 = static_cast<int>(steps * split / a.splits);
+    const int n = static_cast<int>(steps * (split + 1) / a.splits) - it0;
 
-    Stage<E, COLT, WAVES> sc;
-    Stage<E, ROWT, WAVES> sr;
+    Stage<E, COLT, WAVES, true> sc;
+    Stage<E, ROWT, WAVES, false> sr;
     sc.init(a.col, col0, a.ncol, wave, lane);
     sr.init(a.row, row0, nrow, wave, lane);
     const int wr = wave % WR, wc = wave / WR;
@@ -209,124 +293,195 @@ __global__ void __launch_bounds__(64 * WR * WC) bdlm_tile_kernel(const TileArgs 
     rc.init(wc * (E / WC), lane);
     rr.init(wr * (E / WR), lane);
 
-    f32x4 acc[FC][FR];
+    if constexpr (OUT == kTileProb) {
+        const ProbArgs &b = a.prob;
+        for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
+            // rows past the last one up to a multiple of 64 are zeros: they are summed over as they lie
+            const int64_t r = row0 + x;
+            RowData d{INFINITY, 0.f, 0.f, -1};
+            if (r < nrow) {
+                const float g = b.weight[r];
+                // the label's probability less one is exp(-loss) - 1, without cancellation
+                d = RowData{b.lse[r], g, g * expm1f(-b.loss[r]), b.label[r] - b.col0};
+            }
+            rows[x] = d;
+        }
+    } else if constexpr (OUT == kTileBest) {
+        if (a.best.label)
+            for (int x = threadIdx.x; x < E; x += 64 * WAVES) rows[x].label = row0 + x < nrow ? a.best.label[row0 + x] : -1;
+    }
+
+    f32x16 acc[FC][FR];   // [column fragment][row fragment]
 #pragma unroll
     for (int i = 0; i < FC; ++i)
 #pragma unroll
-        for (int j = 0; j < FR; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < FR; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
+    // where the next stage's contents come from, and the one's before it, half of which is copied later
+    struct From {
+        const char *c, *r;
+        int left;
+    };
     int pair = it0 / (nkt > 0 ? nkt : 1), kt = it0 - pair * nkt;
-    auto fill = [&](int buf) {
-        const int left = K - kt * kDepth;
-        sc.load(sm[buf], col_term(a.npair, pair) * a.col.plane, kt, left, wave);
-        sr.load(sm[buf] + kBuf, row_term(a.npair, pair) * a.row.plane, kt, left, wave);
-        if (++kt == nkt) {
+    From next{sc.at_step(col_term(a.npair, pair) * a.col.plane, kt),
+              sr.at_step(row_term(a.npair, pair) * a.row.plane, kt), K - kt * kDepth};
+    From prev = next;
+    auto advance = [&]() {
+        prev = next;
+        next = From{next.c + sc.stride(), next.r + sr.stride(), next.left - kDepth};
+        if (++kt == nkt) {   // (more than one pair of planes)
             kt = 0;
             ++pair;
+            next = From{sc.at_step(col_term(a.npair, pair) * a.col.plane, 0),
+                        sr.at_step(row_term(a.npair, pair) * a.row.plane, 0), K};
         }
     };
-    if (it0 < it1) fill(0);
-    for (int it = it0; it < it1; ++it) {
-        const int buf = (it - it0) & 1;
-        // this buffer's copies have landed in every wave, and every wave is done with the other
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    constexpr int kLoads = Stage<E, COLT, WAVES, true>::kLoads;   // of either operand
+    auto copy = [&](int i, int buf, const From &f) {
+        if (i < kLoads) sc.copy(i, f.c, sm[buf], f.left, wave);
+        else sr.copy(i - kLoads, f.r, sm[buf] + kBuf, f.left, wave);
+    };
+    bf16x8 fc[2][FC], fr[2][FR];
+    // in the order that products use them: column 0, the rows, the other columns
+    auto order = [](int k) { return k == 0 ? 0 : k <= FR ? FC + k - 1 : k - FR; };
+    auto read = [&](int x, int buf, int g) {
+        if (x < FC) fc[g & 1][x] = rc.get(reinterpret_cast<const char *>(sm[buf]), x, g);
+        else fr[g & 1][x - FC] = rr.get(reinterpret_cast<const char *>(sm[buf] + kBuf), x - FC, g);
+    };
+    constexpr int kProducts = FC * FR, kReads = FC + FR;   // of a group
+    // Copies of a stage, by the group that they are made in: the last of the stage before the one
+    // before it (where its buffer becomes free), then the next one's first two.  All at once they
+    // would come faster than they are served (64 bytes a cycle), and the products would wait.
+    constexpr int kCopies = 2 * kLoads, kC1 = kCopies * 7 / 16, kC0 = kCopies * 7 / 16, kC3 = kCopies - kC0 - kC1;
+    // Group g of the stage in buffer `buf`.  Between its products: the reads of the next group (of the
+    // last one: the next stage's first, or nothing's where there is none), and, if `copies`, a
+    // part of a stage's copies.  No product lies in a branch, so that no accumulator is moved.
+    auto group = [&](auto g_, int buf, bool copies) {
+        constexpr int g = decltype(g_)::value;
+        constexpr bool last = g == kGroups - 1;
+        constexpr int copies_from = g == 0 ? kC3 : kC3 + kC0, count = last ? kC3 : g == 0 ? kC0 : g == 1 ? kC1 : 0;
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int kMeet = kProducts * 6 / 16;   // products before the waves meet, in the last group
+#pragma unroll
+        for (int x = 0; x < kProducts; ++x) {
+            mma(fc[g & 1][x / FR], fr[g & 1][x % FR], acc[x / FR][x % FR]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (last) {
+                if (x + 1 == kMeet) {
+                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                }
+            }
+            constexpr int from = last ? kMeet - 1 : 0, slots = kProducts - from;
+            const int s = x - from;
+            if (s >= 0) {
+#pragma unroll
+                for (int k = 0; k < kReads; ++k)
+                    if (k * slots / kReads == s) read(order(k), last ? buf ^ 1 : buf, (g + 1) % kGroups);
+#pragma unroll
+                for (int k = 0; k < count; ++k)
+                    if (k * slots / count == s && copies)
+                        copy(last ? k : copies_from + k, last ? buf : buf ^ 1, last ? next : prev);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (n > 0) {
+#pragma unroll
+        for (int k = 0; k < kCopies; ++k) copy(k, 0, next);
+        if (n > 1) {
+            advance();
+#pragma unroll
+            for (int k = 0; k < kC3; ++k) copy(k, 1, next);
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kC3) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        }
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (it + 1 < it1) fill(buf ^ 1);
-        const char *lc = reinterpret_cast<const char *>(sm[buf]);
-        const char *lr = reinterpret_cast<const char *>(sm[buf] + kBuf);
 #pragma unroll
-        for (int k = 0; k < kDepth / 32; ++k) {
-            bf16x8 fc[FC], fr[FR];
-#pragma unroll
-            for (int i = 0; i < FC; ++i) fc[i] = rc.get(lc, i, k);
-#pragma unroll
-            for (int j = 0; j < FR; ++j) fr[j] = rr.get(lr, j, k);
-#pragma unroll
-            for (int i = 0; i < FC; ++i)
-#pragma unroll
-                for (int j = 0; j < FR; ++j) acc[i][j] = mma(fc[i], fr[j], acc[i][j]);
-        }
+        for (int x = 0; x < kReads; ++x) read(x, 0, 0);
     }
+    for (int s = 0; s < n; ++s) {
+        const int buf = s & 1;
+        prev = next;
+        if (s + 2 < n) advance();
+        group(Int<0>{}, buf, s + 1 < n);
+        group(Int<1>{}, buf, s + 1 < n);
+        group(Int<2>{}, buf, false);
+        group(Int<3>{}, buf, s + 2 < n);
+        settle(acc);
+    }
+    __syncthreads();   // every wave has read the last stage
 
-    // lane: row r0 + 16 j, columns c0 + 16 i .. + 3
-    const int64_t r0 = row0 + wr * (E / WR) + (lane & 15);
-    const int c0 = static_cast<int>(col0) + wc * (E / WC) + 4 * (lane >> 4);
-    __syncthreads();   // every wave has read the last buffer
-    if constexpr (OUT == kTileBest) {
-        const BestArgs &b = a.best;
-        float *top = reinterpret_cast<float *>(sm[0]);   // [WC][E], then others, at
-        float *oth = top + WC * E;
-        int *at = reinterpret_cast<int *>(oth + WC * E);
+    // 64 rows of the wave at a time through LDS (a region of its own): consecutive lanes then store
+    // consecutive columns, or a lane has a whole row; quads are permuted by the row against bank
+    // conflicts.
+    constexpr int kCols = E / WC, kQuads = kCols / 4, kRows = 64 / kQuads;   // rows of one pass of the wave
+    static_assert(WAVES * 64 * kCols * 4 == int(sizeof(sm)), "the waves' regions fill the buffers");
+    f32x4 *mine = reinterpret_cast<f32x4 *>(sm) + wave * 64 * kQuads;
+    const int rows_out = OUT == kTileProb ? (nrow + 63) / 64 * 64 : nrow;
+    const int col1 = static_cast<int>(col0) + wc * kCols;   // the wave's first column
+    const int quad = lane % kQuads, sub = lane / kQuads;
+    f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (OUT == kTileStore) bias = load_bias(a.store, col1 + 4 * quad, a.ncol);
+    auto part = [&](auto j0_) {
+        constexpr int j0 = decltype(j0_)::value;
+        const int r1 = wr * (E / WR) + 32 * j0;   // the part's first row in the tile
+        if (row0 + r1 >= rows_out) return;
 #pragma unroll
-        for (int j = 0; j < FR; ++j) {
-            const int64_t r = r0 + 16 * j;
-            const int label = b.label && r < nrow ? b.label[r] : -1;
-            Best m{-INFINITY, 0.f, kNoColumn};
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int i = 0; i < FC; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int c = c0 + 16 * i + e;
-                    if (c >= a.ncol || c == b.exclude) acc[i][j][e] = -INFINITY;
-                    else if (beats(acc[i][j][e], c, m)) m.top = acc[i][j][e], m.at = c;
-                    if (c == label) b.label_logit[r] = acc[i][j][e];
+                    const f32x16 &v = acc[i][j0 + j];
+                    mine[(32 * j + (lane & 31)) * kQuads + ((8 * i + 2 * e + (lane >> 5)) ^ (lane & 15))] =
+                        f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
                 }
-            // the four lane groups of a row
-#pragma unroll
-            for (int d = 16; d < 64; d *= 2) {
-                const float v = __shfl_xor(m.top, d, 64);
-                const int w = __shfl_xor(m.at, d, 64);
-                if (beats(v, w, m)) m.top = v, m.at = w;
+        __builtin_amdgcn_wave_barrier();
+        if constexpr (OUT == kTileBest) {
+            const Best m = row_best(a, mine + lane * kQuads, lane & 15, kCols, col1);
+            top[wc][r1 + lane] = m.top;
+            others[wc][r1 + lane] = m.others;
+            at[wc][r1 + lane] = m.at;
+            if (a.best.label) {
+                const int label = rows[r1 + lane].label, x = label - col1;
+                if (x >= 0 && x < kCols && label < a.ncol) {
+                    // (the largest value is no longer in its place)
+                    const float v = mine[lane * kQuads + ((x >> 2) ^ (lane & 15))][x & 3];
+                    a.best.label_logit[row0 + r1 + lane] = label == m.at ? m.top : v;
+                }
             }
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < FC; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c0 + 16 * i + e != m.at) s += share(acc[i][j][e], m.top);
-            s += __shfl_xor(s, 16, 64);
-            s += __shfl_xor(s, 32, 64);
-            if (lane < 16) {
-                const int x = wc * E + wr * (E / WR) + 16 * j + lane;
-                top[x] = m.top;
-                oth[x] = s;
-                at[x] = m.at;
+        } else {
+            const int most = static_cast<int>(rows_out - row0) - r1;
+#pragma unroll 4
+            for (int x = sub; x < 64; x += kRows) {
+                const f32x4 v = mine[x * kQuads + (quad ^ (x & 15))];
+                RowData d{};
+                if constexpr (OUT == kTileProb) d = rows[r1 + x];
+                if (x < most) tile_quad<OUT>(a, v, bias, d, row0 + r1 + x, col1 + 4 * quad, split);
             }
         }
+        __builtin_amdgcn_wave_barrier();
+    };
+    part(Int<0>{});
+    if constexpr (FR > 2) part(Int<2>{});
+    static_assert(FR == 2 || FR == 4, "parts of 64 rows");
+    if constexpr (OUT == kTileBest) {
         __syncthreads();
         for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
             if (row0 + x >= nrow) continue;
-            Best m{top[x], oth[x], at[x]};
+            Best m{top[0][x], others[0][x], at[0][x]};
 #pragma unroll
-            for (int w = 1; w < WC; ++w) m = merge(m, Best{top[w * E + x], oth[w * E + x], at[w * E + x]});
-            const int64_t o = (row0 + x) * b.ntile + tile_c;
-            b.top[o] = m.top;
-            b.others[o] = m.others;
-            b.at[o] = m.at;
-        }
-    } else {
-        // Sixteen rows at a time through LDS (a region of the wave's own), so that whole rows of
-        // the wave's columns are stored by consecutive lanes.
-        constexpr int kCols = E / WC, kPitch = kCols + 4, kQuads = kCols / 4;
-        static_assert(WAVES * 16 * kPitch * 4 <= int(sizeof(sm)), "the waves' regions fit");
-        float *mine = reinterpret_cast<float *>(sm) + wave * 16 * kPitch;
-        const int64_t wrow0 = row0 + wr * (E / WR);
-        const int wcol0 = static_cast<int>(col0) + wc * kCols;
-#pragma unroll
-        for (int j = 0; j < FR; ++j) {
-            if (wrow0 + 16 * j >= nrow) break;
-#pragma unroll
-            for (int i = 0; i < FC; ++i)
-                *reinterpret_cast<f32x4 *>(mine + (lane & 15) * kPitch + 16 * i + 4 * (lane >> 4)) = acc[i][j];
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-            for (int x = lane; x < 16 * kQuads; x += 64) {
-                const int64_t r = wrow0 + 16 * j + x / kQuads;
-                const int c = wcol0 + x % kQuads * 4;
-                if (r < nrow) tile_quad<OUT>(a, *reinterpret_cast<const f32x4 *>(mine + x / kQuads * kPitch + x % kQuads * 4), r, c, split);
-            }
-            __builtin_amdgcn_wave_barrier();
+            for (int w = 1; w < WC; ++w) m = merge(m, Best{top[w][x], others[w][x], at[w][x]});
+            const int64_t o = (row0 + x) * a.best.ntile + tile_c;
+            a.best.top[o] = m.top;
+            a.best.others[o] = m.others;
+            a.best.at[o] = m.at;
         }
     }
 }
@@ -356,7 +511,7 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
                 for (int e = 0; e < 4; ++e)
                     if (c + e < ncol) v[e] += p[k * slice + e];
         }
-        store4(s, v, r, c, ncol);
+        store4(s, v, load_bias(s, c, ncol), r, c, ncol);
     }
 }
 
