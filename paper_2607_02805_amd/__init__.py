@@ -906,6 +906,9 @@ def projection(x, w, bias=None, act=None, residual=None, out=None, pre=None, str
     [..., out_features].  ``pre`` keeps x w^T + bias in x's dtype for the gradient: None (no),
     True (allocate) or a tensor.  Returns out, or (out, pre) if ``pre`` was asked for.
     """
+    got = _native().projection(x, w, bias, act, residual, out, pre, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_projection")
     torch = _torch()
     code = _act_code(act)
     d, lead = _dense(x, w)
@@ -940,6 +943,9 @@ def projection_backward(dy, x, w, pre=None, act=None, dx=True, dw=True, db=None,
     (allocate), None (not wanted) or a tensor; dx and dw have x's dtype, db is float32.
     The residual's gradient is dy.
     """
+    got = _native().projection_backward(dy, x, w, pre, act, dx, dw, db, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_projection_backward")
     torch = _torch()
     code = _act_code(act)
     d, lead = _dense(x, w)
@@ -979,6 +985,9 @@ def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, worksp
     ``labels`` int64.  A row whose label is not a token that the softmax ranges over (negative, past
     the vocabulary, or ``exclude``) is left out: its loss and lse are 0.  The logits are never
     in memory."""
+    got = _native().head_loss(x, w, labels, exclude, loss, lse, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_head_loss")
     torch = _torch()
     d, lead = _dense(x, w)
     _vector(labels, lead, torch.int64, x.device, "labels")
@@ -996,6 +1005,10 @@ def head_loss_backward(dloss, x, w, labels, loss, lse, exclude=-1, dx=True, dw=T
     ``dloss`` float32 is the gradient of the result by each row's loss (the weights of the block
     objective); ``loss`` and ``lse`` are what :func:`head_loss` returned for the same x, w,
     labels and exclude.  ``dx``, ``dw``: True (allocate), None (not wanted) or a tensor."""
+    got = _native().head_loss_backward(dloss, x, w, labels, loss, lse, exclude, dx, dw, stream,
+                                       workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_head_loss_backward")
     torch = _torch()
     d, lead = _dense(x, w)
     _vector(labels, lead, torch.int64, x.device, "labels")
@@ -1017,6 +1030,9 @@ def head_select(x, w, exclude=-1, token=None, logprob=None, stream=None, workspa
     """The head of a denoising step: (token, logprob) for hidden states x [..., in_features] and the
     vocabulary's weights w [tokens, in_features]: the most probable token (int64; the lowest of
     equals) but ``exclude``, and the log of its probability (float32)."""
+    got = _native().head_select(x, w, exclude, token, logprob, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_head_select")
     torch = _torch()
     d, lead = _dense(x, w)
     token = _vector(_place(token, lead, torch.int64, x.device, "token"), lead, torch.int64, x.device, "token")

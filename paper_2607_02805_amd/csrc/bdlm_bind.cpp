@@ -22,6 +22,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -459,12 +460,220 @@ BDLM_ENTRY(gated_rmsnorm, 7) {
     });
 } BDLM_END
 
+// ---- dense operators.  The plain case here: tensors on the current device, its current stream.
+
+// The rows of a [..., cols] tensor: how many, and the stride between them (the leading dimensions
+// have to lie at one stride; rows of one element count as unit stride).
+int64_t row_stride(const at::Tensor &t, int64_t rows) {
+    const int64_t d = t.dim(), cols = t.size(d - 1);
+    need(rows > 0 && (cols <= 1 || t.stride(d - 1) == 1));
+    int64_t stride = -1, span = 1;
+    for (int64_t i = d - 2; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (stride < 0) stride = t.stride(i), span = t.size(i);
+        else {
+            need(t.stride(i) == stride * span);
+            span *= t.size(i);
+        }
+    }
+    return stride < 0 ? cols : stride;
+}
+struct Dense {
+    const at::Tensor &x, &w;
+    bdlm_dense_desc_t d;
+    at::ScalarType type;
+    Dense(PyObject *px, PyObject *pw) : x(tensor(px)), w(tensor(pw)) {
+        type = x.scalar_type();
+        need(x.dim() >= 1 && w.dim() == 2 && w.scalar_type() == type && (type == at::kBFloat16 || type == at::kFloat));
+        d.in_features = w.size(1);
+        d.out_features = w.size(0);
+        need(d.in_features > 0 && d.out_features > 0 && x.size(x.dim() - 1) == d.in_features);
+        d.rows = x.numel() / d.in_features;
+        d.x_stride = row_stride(x, d.rows);
+        d.w_stride = row_stride(w, d.out_features);
+        d.in_dtype = code(type);
+        d.reserved = 0;
+        need(x.get_device() == c10::hip::current_device() && here(w));
+    }
+    static int32_t code(at::ScalarType t) { return t == at::kBFloat16 ? BDLM_DTYPE_BF16 : BDLM_DTYPE_F32; }
+    bool here(const at::Tensor &t) const { return t.get_device() == x.get_device(); }
+    at::IntArrayRef lead() const { return x.sizes().slice(0, x.dim() - 1); }
+    bool leads(const at::Tensor &t) const { return t.dim() == x.dim() && t.sizes().slice(0, t.dim() - 1) == lead(); }
+    c10::SmallVector<int64_t, 5> shape(int64_t cols) const {
+        c10::SmallVector<int64_t, 5> s(lead().begin(), lead().end());
+        s.push_back(cols);
+        return s;
+    }
+    // An input of x's leading shape.
+    const at::Tensor &input(PyObject *o, int64_t cols) const {
+        const at::Tensor &t = tensor(o);
+        need(here(t) && t.dim() >= 1 && t.size(t.dim() - 1) == cols && leads(t));
+        need(t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kFloat);
+        return t;
+    }
+    // An output: new for None (where that asks for one) and True, else the given tensor.
+    at::Tensor output(PyObject *o, at::IntArrayRef shape, at::ScalarType ty) const {
+        if (o == Py_None || o == Py_True) {
+            const Unlocked u;
+            return at::empty(shape, x.options().dtype(ty));
+        }
+        const at::Tensor &t = tensor(o);
+        need(here(t) && t.scalar_type() == ty && t.sizes() == shape);
+        return t;
+    }
+    at::Tensor wanted(PyObject *o, at::IntArrayRef shape, at::ScalarType ty) const {
+        return o == Py_None ? at::Tensor() : output(o, shape, ty);
+    }
+    // A contiguous tensor of one value per row.
+    at::Tensor values(PyObject *o, at::ScalarType ty, bool make) const {
+        at::Tensor t = make ? output(o, lead(), ty) : tensor(o);
+        need(here(t) && t.scalar_type() == ty && t.sizes() == lead() && t.is_contiguous());
+        return t;
+    }
+};
+template <class F>
+int64_t bytes_of(F query, const bdlm_dense_desc_t &d) {
+    int64_t n = 0;
+    need(query(&d, &n) == BDLM_OK);
+    return n;
+}
+int32_t act_of(PyObject *o) {
+    if (o == Py_None) return BDLM_ACT_NONE;
+    need(PyUnicode_CheckExact(o));
+    if (PyUnicode_CompareWithASCIIString(o, "none") == 0) return BDLM_ACT_NONE;
+    if (PyUnicode_CompareWithASCIIString(o, "silu") == 0) return BDLM_ACT_SILU;
+    need(PyUnicode_CompareWithASCIIString(o, "gelu") == 0);
+    return BDLM_ACT_GELU;
+}
+// The workspace, on x's device.
+Workspace dense_space(PyObject *o, int64_t bytes, const Dense &t) {
+    Workspace ws(o, bytes, t.x);
+    need(!ws.t.defined() || t.here(ws.t));
+    return ws;
+}
+
+// x w bias act residual out pre stream workspace
+BDLM_ENTRY(projection, 9) {
+    const Dense t(a[0], a[1]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[7] == Py_None);
+    const float *bias = nullptr;
+    if (a[2] != Py_None) {
+        bias = vec(a[2], d.out_features);
+        need(t.here(tensor(a[2])));
+    }
+    const int32_t act = act_of(a[3]);
+    const at::Tensor res = a[4] == Py_None ? at::Tensor() : t.input(a[4], d.out_features);
+    const auto full = t.shape(d.out_features);
+    need(a[5] != Py_True);
+    const at::Tensor out = a[5] == Py_None ? t.output(Py_None, full, res.defined() ? res.scalar_type() : t.type)
+                                           : t.input(a[5], d.out_features);
+    need(!res.defined() || res.scalar_type() == out.scalar_type());
+    const at::Tensor pre = t.wanted(a[6], full, t.type);
+    const int64_t ldo = row_stride(out, d.rows), ldr = res.defined() ? row_stride(res, d.rows) : 0,
+                  ldp = pre.defined() ? row_stride(pre, d.rows) : 0;
+    const Workspace ws = dense_space(a[8], bytes_of(bdlm_projection_workspace, d), t);
+    void *s = stream_of(a[7]);
+    const int32_t odt = Dense::code(out.scalar_type());
+    const void *x = ptr(t.x), *w = ptr(t.w), *rp = res.defined() ? ptr(res) : nullptr;
+    void *op = ptr(out), *pp = pre.defined() ? ptr(pre) : nullptr;
+    return enqueue(pre.defined() ? pair(out, pre) : item(out), [&] {
+        return bdlm_projection(&d, act, odt, x, w, bias, rp, ldr, op, ldo, pp, ldp, ws.p, ws.bytes, s);
+    });
+} BDLM_END
+
+// dy x w pre act dx dw db stream workspace
+BDLM_ENTRY(projection_backward, 10) {
+    const Dense t(a[1], a[2]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[8] == Py_None);
+    const at::Tensor &dy = t.input(a[0], d.out_features);
+    const int32_t act = act_of(a[4]);
+    const at::Tensor pre = act == BDLM_ACT_NONE ? at::Tensor() : t.input(a[3], d.out_features);
+    need(!pre.defined() || pre.scalar_type() == t.type);
+    const at::Tensor dx = t.wanted(a[5], t.x.sizes(), t.type), dw = t.wanted(a[6], t.w.sizes(), t.type),
+                     db = t.wanted(a[7], {d.out_features}, at::kFloat);
+    need(!db.defined() || db.is_contiguous());
+    const int64_t ldy = row_stride(dy, d.rows), ldp = pre.defined() ? row_stride(pre, d.rows) : 0,
+                  ldx = dx.defined() ? row_stride(dx, d.rows) : 0,
+                  ldw = dw.defined() ? row_stride(dw, d.out_features) : 0;
+    const Workspace ws = dense_space(a[9], bytes_of(bdlm_projection_backward_workspace, d), t);
+    void *s = stream_of(a[8]);
+    const int32_t ydt = Dense::code(dy.scalar_type());
+    const void *yp = ptr(dy), *x = ptr(t.x), *w = ptr(t.w), *pp = pre.defined() ? ptr(pre) : nullptr;
+    void *xp = dx.defined() ? ptr(dx) : nullptr, *wp = dw.defined() ? ptr(dw) : nullptr;
+    float *bp = opt_ptr(db);
+    PyObject *r = PyTuple_New(3);
+    if (!r) general();
+    PyTuple_SET_ITEM(r, 0, item(dx));
+    PyTuple_SET_ITEM(r, 1, item(dw));
+    PyTuple_SET_ITEM(r, 2, item(db));
+    return enqueue(r, [&] {
+        return bdlm_projection_backward(&d, act, ydt, yp, ldy, x, w, pp, ldp, xp, ldx, wp, ldw, bp, ws.p, ws.bytes, s);
+    });
+} BDLM_END
+
+// x w labels exclude loss lse stream workspace
+BDLM_ENTRY(head_loss, 8) {
+    const Dense t(a[0], a[1]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[6] == Py_None);
+    const at::Tensor labels = t.values(a[2], at::kLong, false);
+    const int64_t exclude = integer(a[3]);
+    const at::Tensor loss = t.values(a[4], at::kFloat, true), lse = t.values(a[5], at::kFloat, true);
+    const Workspace ws = dense_space(a[7], bytes_of(bdlm_head_loss_workspace, d), t);
+    void *s = stream_of(a[6]);
+    const int64_t *lp = ptr<int64_t>(labels);
+    const void *x = ptr(t.x), *w = ptr(t.w);
+    float *op = ptr<float>(loss), *ep = ptr<float>(lse);
+    return enqueue(pair(loss, lse), [&] { return bdlm_head_loss(&d, lp, exclude, x, w, op, ep, ws.p, ws.bytes, s); });
+} BDLM_END
+
+// dloss x w labels loss lse exclude dx dw stream workspace
+BDLM_ENTRY(head_loss_backward, 11) {
+    const Dense t(a[1], a[2]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[9] == Py_None);
+    const at::Tensor dloss = t.values(a[0], at::kFloat, false), labels = t.values(a[3], at::kLong, false),
+                     loss = t.values(a[4], at::kFloat, false), lse = t.values(a[5], at::kFloat, false);
+    const int64_t exclude = integer(a[6]);
+    const at::Tensor dx = t.wanted(a[7], t.x.sizes(), t.type), dw = t.wanted(a[8], t.w.sizes(), t.type);
+    const int64_t ldx = dx.defined() ? row_stride(dx, d.rows) : 0,
+                  ldw = dw.defined() ? row_stride(dw, d.out_features) : 0;
+    const Workspace ws = dense_space(a[10], bytes_of(bdlm_head_loss_backward_workspace, d), t);
+    void *s = stream_of(a[9]);
+    const int64_t *lp = ptr<int64_t>(labels);
+    const void *x = ptr(t.x), *w = ptr(t.w);
+    const float *gp = ptr<float>(dloss), *op = ptr<float>(loss), *ep = ptr<float>(lse);
+    void *xp = dx.defined() ? ptr(dx) : nullptr, *wp = dw.defined() ? ptr(dw) : nullptr;
+    return enqueue(pair(dx, dw), [&] {
+        return bdlm_head_loss_backward(&d, lp, exclude, x, w, op, ep, gp, xp, ldx, wp, ldw, ws.p, ws.bytes, s);
+    });
+} BDLM_END
+
+// x w exclude token logprob stream workspace
+BDLM_ENTRY(head_select, 7) {
+    const Dense t(a[0], a[1]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[5] == Py_None);
+    const int64_t exclude = integer(a[2]);
+    const at::Tensor token = t.values(a[3], at::kLong, true), logprob = t.values(a[4], at::kFloat, true);
+    const Workspace ws = dense_space(a[6], bytes_of(bdlm_head_select_workspace, d), t);
+    void *s = stream_of(a[5]);
+    const void *x = ptr(t.x), *w = ptr(t.w);
+    int64_t *tp = ptr<int64_t>(token);
+    float *lp = ptr<float>(logprob);
+    return enqueue(pair(token, logprob), [&] { return bdlm_head_select(&d, exclude, x, w, tp, lp, ws.p, ws.bytes, s); });
+} BDLM_END
+
 #define BDLM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     BDLM_METHOD(scan_block_step), BDLM_METHOD(scan_block_step_sep), BDLM_METHOD(commit_boundary),
     BDLM_METHOD(commit_step), BDLM_METHOD(conv_block_step), BDLM_METHOD(conv_commit_boundary),
     BDLM_METHOD(scan_full_window), BDLM_METHOD(prefill),
-    BDLM_METHOD(prefill_noalloc), BDLM_METHOD(gated_rmsnorm), {nullptr, nullptr, 0, nullptr}};
+    BDLM_METHOD(prefill_noalloc), BDLM_METHOD(gated_rmsnorm), BDLM_METHOD(projection),
+    BDLM_METHOD(projection_backward), BDLM_METHOD(head_loss), BDLM_METHOD(head_loss_backward),
+    BDLM_METHOD(head_select), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

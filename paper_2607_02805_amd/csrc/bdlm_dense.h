@@ -73,20 +73,32 @@ struct TileArgs {
     int32_t npair;                     // 1 or 6
     int32_t row_t, col_t;
     int32_t big;                       // 1: 256 x 256 tiles, 0: 128 x 128
-    int32_t splits;                    // > 1: kTilePartial only
+    int32_t splits;                    // > 1: kTilePartial only; 0: as many as fill the chip with
+                                       // the rows that count (split_count)
     int32_t add;                       // kTilePartial: add onto the slices
-    float *part;                       // [splits][nrow][ncol]
+    float *part;                       // [splits][nrow][ncol]; splits 0: [split_count][nrow counted][ncol]
     int32_t out;                       // TileOut
     StoreArgs store;
     BestArgs best;
     ProbArgs prob;
 };
 int launch_tile(const TileArgs &a, void *stream);
+constexpr int32_t kChip = 256;   // workgroups of large tiles that run at once
+constexpr int32_t kMostSplits = 16;
+// Splits of a product whose row count is known on the device alone, by its tiles.
+#ifdef __HIPCC__
+__host__ __device__
+#endif
+inline int32_t split_count(int64_t tiles) {
+    const int64_t s = tiles > 0 ? kChip / tiles : 1;
+    return static_cast<int32_t>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
+}
 // Columns of a tile (what kTileBest's ntile counts).
 inline int32_t tile_edge(bool big) { return big ? 256 : 128; }
 
-// out = epilogue(sum of the partial slices)
-int launch_join(const float *part, int32_t splits, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
+// out = epilogue(sum of the partial slices); splits 0: as many as a tiled product of these sizes
+// made (big: its tiles)
+int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
                 const StoreArgs &s, void *stream);
 
 // Few rows (at most 64): the weights stream through once.  x [nrow][k], w [ncol][k], both bf16
@@ -122,8 +134,8 @@ struct PackArgs {
     float *colsum;             // [pack_row_blocks(rows)][cols] partial column sums of dst, or null
 };
 int launch_pack(const PackArgs &a, void *stream);
-constexpr int32_t kPackRows = 64;   // rows per workgroup when column sums are taken
-inline int32_t pack_row_blocks(int32_t rows) { return (rows + kPackRows - 1) / kPackRows; }
+constexpr int32_t kPackRows = 32;   // rows per workgroup
+inline int32_t pack_row_blocks(int32_t rows) { return (rows + 63) / 64 * (64 / kPackRows); }
 // out[c] = sum over the blocks of part[b][c]
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream);
 

@@ -15,36 +15,41 @@ namespace {
 typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_a4;
 
-// Eight elements of a row from column c, zeros past cols.
-__device__ __forceinline__ void load8(const void *src, int64_t at, int n, bool bf16, float (&v)[8]) {
-    if (bf16) {
-        const uint16_t *p = static_cast<const uint16_t *>(src) + at;
-        if (n >= 8) {
-            const u32x4 u = *reinterpret_cast<const u32x4_a2 *>(p);
+// Eight consecutive elements of a row as they lie, zeros past the n that there are.
+template <bool BF16>
+struct Eight {
+    u32x4 u[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void *src, int64_t at, int n) {
+        if constexpr (BF16) {
+            const uint16_t *p = static_cast<const uint16_t *>(src) + at;
+            if (n >= 8) {
+                u[0] = *reinterpret_cast<const u32x4_a2 *>(p);
+            } else {
+                uint32_t h[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[2 * e] = __uint_as_float(u[e] << 16);
-                v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+                for (int e = 0; e < 8; ++e) h[e] = e < n ? p[e] : 0u;
+                u[0] = u32x4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
             }
         } else {
+            const float *p = static_cast<const float *>(src) + at;
+            if (n >= 8) {
+                u[0] = *reinterpret_cast<const u32x4_a4 *>(p);
+                u[1] = *reinterpret_cast<const u32x4_a4 *>(p + 4);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? bf16_to_f32(static_cast<short>(p[e])) : 0.f;
-        }
-    } else {
-        const float *p = static_cast<const float *>(src) + at;
-        if (n >= 8) {
-            const u32x4 a = *reinterpret_cast<const u32x4_a4 *>(p), b = *reinterpret_cast<const u32x4_a4 *>(p + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(a[e]), v[4 + e] = __uint_as_float(b[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? p[e] : 0.f;
+                for (int e = 0; e < 8; ++e) u[e >> 2][e & 3] = e < n ? __float_as_uint(p[e]) : 0u;
+            }
         }
     }
-}
+    __device__ __forceinline__ float value(int e) const {
+        if constexpr (BF16) return e & 1 ? __uint_as_float(u[0][e >> 1] & 0xffff0000u) : __uint_as_float(u[0][e >> 1] << 16);
+        else return __uint_as_float(u[e >> 2][e & 3]);
+    }
+};
 
-__device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, int terms, const float (&v)[8]) {
-    if (terms == 1) {
+template <int TERMS>
+__device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, const float (&v)[8]) {
+    if constexpr (TERMS == 1) {
         *reinterpret_cast<uint4 *>(dst) = uint4{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]),
                                                 cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7])};
         return;
@@ -61,39 +66,49 @@ __device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, int te
     }
 }
 
-// Thread: eight columns; a workgroup takes kPackRows rows of 64 x 8 columns with its four waves
-// (row r of every four).  The column sums are of the fp32 values, before they are rounded.
-template <bool GRAD>
+// Thread: eight columns of kPackBatch rows at a time, all asked for before any is used (with one row
+// at a time, 1,003 x 1,934 fp32 took 33 us instead of 8); a workgroup takes kPackRows rows of 64 x 8
+// columns with its four waves (row r of every four).  The column sums are of the fp32 values,
+// before they are rounded.
+constexpr int kPackBatch = 4;
+static_assert(kPackRows % (4 * kPackBatch) == 0, "whole batches");
+template <bool GRAD, bool BF16, bool PRE16, int TERMS>
 __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
     __shared__ float sums[4][64 * 8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = (blockIdx.x * 64 + lane) * 8;
-    const int rows = a.rows_dev ? *a.rows_dev : a.rows;
+    const int64_t rows = a.rows_dev ? *a.rows_dev : a.rows, rows_up = (rows + 63) / 64 * 64;
     const int64_t r0 = int64_t(blockIdx.y) * kPackRows;
     const int n = a.cols - c;
-    const bool here = c < a.ld_dst;
+    const bool slope = GRAD && a.act != BDLM_ACT_NONE;
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (here) {
-        for (int64_t r = r0 + wave; r < (rows + 63) / 64 * 64 && r < r0 + kPackRows; r += 4) {
-            if (r >= rows) {
-                const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (a.dst) store_terms(a.dst + r * a.ld_dst + c, a.plane, a.terms, none);
-                continue;
-            }
-            const int64_t from = a.row_of ? a.row_of[r] : r;
-            float v[8];
-            load8(a.src, from * a.ld + c, n, a.src_bf16, v);
-            if constexpr (GRAD) {
-                if (a.act != BDLM_ACT_NONE) {
-                    float z[8];
-                    load8(a.pre, from * a.ld_pre + c, n, a.pre_bf16, z);
+    if (c < a.ld_dst) {
+        for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += 4 * kPackBatch) {
+            Eight<BF16> v[kPackBatch];
+            Eight<PRE16> z[kPackBatch];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = e < n ? v[e] * act_slope(z[e], a.act) : 0.f;
+            for (int k = 0; k < kPackBatch; ++k) {
+                const int64_t r = q + 4 * k;
+                const int64_t from = r >= rows ? 0 : a.row_of ? a.row_of[r] : r;
+                v[k].load(a.src, from * a.ld + c, r < rows ? n : 0);
+                if (slope) z[k].load(a.pre, from * a.ld_pre + c, r < rows ? n : 0);
+            }
+#pragma unroll
+            for (int k = 0; k < kPackBatch; ++k) {
+                const int64_t r = q + 4 * k;
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = v[k].value(e);
+                if constexpr (GRAD) {
+                    if (slope) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = r < rows && e < n ? f[e] * act_slope(z[k].value(e), a.act) : 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] += f[e];
                 }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += v[e];
+                if (a.dst && r < rows_up) store_terms<TERMS>(a.dst + r * a.ld_dst + c, a.plane, f);
             }
-            if (a.dst) store_terms(a.dst + r * a.ld_dst + c, a.plane, a.terms, v);
         }
     }
     if constexpr (GRAD) {
@@ -109,17 +124,29 @@ __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
     }
 }
 
-// Column sums of the blocks' partial sums: 64 columns a workgroup, four waves over the blocks.
-__global__ void __launch_bounds__(256) bdlm_colsum_kernel(const float *part, int blocks, int cols, float *out) {
-    __shared__ float sums[4][64];
+// Column sums of the blocks' partial sums: 64 columns a workgroup, sixteen waves over the blocks,
+// eight loads in flight in each.
+__global__ void __launch_bounds__(1024) bdlm_colsum_kernel(const float *part, int blocks, int cols, float *out) {
+    __shared__ float sums[16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = blockIdx.x * 64 + lane;
     float s = 0.f;
-    if (c < cols)
-        for (int b = wave; b < blocks; b += 4) s += part[int64_t(b) * cols + c];
+    if (c < cols) {
+        for (int b = wave; b < blocks; b += 128) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = b + 16 * k < blocks ? part[int64_t(b + 16 * k) * cols + c] : 0.f;
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+    }
     sums[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && c < cols) out[c] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    if (wave == 0 && c < cols) {
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += sums[w][lane];
+        out[c] = s;
+    }
 }
 
 __device__ __forceinline__ bool counts(int64_t label, int64_t exclude, int vocab) {
@@ -159,27 +186,39 @@ __global__ void __launch_bounds__(1024) bdlm_rows_kernel(const RowsArgs a) {
     if (threadIdx.x == 0) *a.count = base;
 }
 
-// One wave per row merges its records.
+// One workgroup per row merges its records, four to a lane at a time.
 __global__ void __launch_bounds__(256) bdlm_finish_kernel(const FinishArgs a) {
-    const int lane = threadIdx.x & 63;
-    const int64_t i = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    __shared__ Best waves[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i = blockIdx.x;
     const int n = a.count ? *a.count : a.rows;
-    if (a.labels && i < a.rows && !counts(a.labels[i], a.exclude, a.vocab) && lane == 0) {
+    if (a.labels && threadIdx.x == 0 && !counts(a.labels[i], a.exclude, a.vocab)) {
         a.loss[i] = 0.f;
         a.lse[i] = 0.f;
     }
     if (i >= n) return;
     Best m{-INFINITY, 0.f, kNoColumn};
-    for (int t = lane; t < a.ntile; t += 64) {
-        const int64_t o = i * a.ntile + t;
-        m = merge(m, Best{a.top[o], a.others[o], a.at[o]});
+    for (int t = threadIdx.x; t < a.ntile; t += 1024) {
+        Best o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t at = i * a.ntile + t + 256 * k;
+            const bool here = t + 256 * k < a.ntile;
+            o[k] = here ? Best{a.top[at], a.others[at], a.at[at]} : Best{-INFINITY, 0.f, kNoColumn};
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m = merge(m, o[k]);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
         const Best o{__shfl_xor(m.top, d, 64), __shfl_xor(m.others, d, 64), __shfl_xor(m.at, d, 64)};
         m = merge(m, o);
     }
-    if (lane != 0) return;
+    if (lane == 0) waves[wave] = m;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = merge(m, waves[w]);
     const float rest = m.top == -INFINITY ? NAN : log1pf(m.others);
     if (a.labels) {
         const int64_t r = a.row_of[i];
@@ -210,13 +249,26 @@ int launch_pack(const PackArgs &a, void *stream) {
     if (a.rows <= 0) return BDLM_OK;
     const dim3 g(static_cast<unsigned>((a.ld_dst + 511) / 512), static_cast<unsigned>(pack_row_blocks(a.rows)));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (a.act != BDLM_ACT_NONE || a.colsum) hipLaunchKernelGGL((bdlm_pack_kernel<true>), g, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((bdlm_pack_kernel<false>), g, dim3(256), 0, s, a);
+    const dim3 b(256);
+    const bool grad = a.act != BDLM_ACT_NONE || a.colsum;
+    // (dy may be fp32 where the projection's inputs, and pre, are bf16; not the other way round
+    // for a plain copy)
+    const int kind = (a.terms == 3 ? 4 : 0) + (a.src_bf16 ? 2 : 0) + (grad ? 1 : 0);
+    switch (kind) {
+        case 3: hipLaunchKernelGGL((bdlm_pack_kernel<true, true, true, 1>), g, b, 0, s, a); break;
+        case 1: hipLaunchKernelGGL((bdlm_pack_kernel<true, false, true, 1>), g, b, 0, s, a); break;
+        case 7: hipLaunchKernelGGL((bdlm_pack_kernel<true, true, false, 3>), g, b, 0, s, a); break;
+        case 5: hipLaunchKernelGGL((bdlm_pack_kernel<true, false, false, 3>), g, b, 0, s, a); break;
+        case 2: hipLaunchKernelGGL((bdlm_pack_kernel<false, true, true, 1>), g, b, 0, s, a); break;
+        case 0: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, true, 1>), g, b, 0, s, a); break;
+        case 4: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, false, 3>), g, b, 0, s, a); break;
+        case 6: hipLaunchKernelGGL((bdlm_pack_kernel<false, true, false, 3>), g, b, 0, s, a); break;
+    }
     return done();
 }
 
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream) {
-    hipLaunchKernelGGL(bdlm_colsum_kernel, dim3((cols + 63) / 64), dim3(256), 0, static_cast<hipStream_t>(stream),
+    hipLaunchKernelGGL(bdlm_colsum_kernel, dim3((cols + 63) / 64), dim3(1024), 0, static_cast<hipStream_t>(stream),
                        part, blocks, cols, out);
     return done();
 }
@@ -228,7 +280,7 @@ int launch_rows(const RowsArgs &a, void *stream) {
 
 int launch_finish(const FinishArgs &a, void *stream) {
     if (a.rows <= 0) return BDLM_OK;
-    hipLaunchKernelGGL(bdlm_finish_kernel, dim3((a.rows + 3) / 4), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(bdlm_finish_kernel, dim3(a.rows), dim3(256), 0, static_cast<hipStream_t>(stream), a);
     return done();
 }
 

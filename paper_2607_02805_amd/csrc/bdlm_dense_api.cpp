@@ -164,7 +164,7 @@ int store_product(TileArgs a, const StoreArgs &s, float *part, void *stream) {
     a.out = kTilePartial;
     a.part = part;
     const int rc = launch_tile(a, stream);
-    return rc != BDLM_OK ? rc : launch_join(part, a.splits, a.nrow, a.ncol, a.nrow_dev, s, stream);
+    return rc != BDLM_OK ? rc : launch_join(part, a.splits, a.big, a.nrow, a.ncol, a.nrow_dev, s, stream);
 }
 int64_t part_size(const Shape &s, int64_t nrow, int64_t ncol) { return s.splits > 1 ? s.splits * nrow * ncol : 0; }
 
@@ -271,8 +271,10 @@ struct LossPlan {
           rec(d.rows, d.out_features, tile_edge(shape.big), ws), label_logit(ws.take<float>(d.rows)) {}
 };
 
-// The vocabulary goes in pieces whose logit gradients (rows x piece, bf16 terms) stay within 256 MB:
-// they are written once and read twice, mostly from the memory-side cache.
+// The vocabulary goes in pieces whose logit gradients (rows x piece, bf16 terms) stay within 512 MB:
+// they are written once and read twice, mostly from the memory-side cache where half of the
+// rows count.  The number of rows that count is known on the device alone, so the product over the
+// vocabulary (dx) is split there.
 struct LossBackwardPlan {
     Space ws;
     Rows rows;
@@ -286,16 +288,18 @@ struct LossBackwardPlan {
           w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
         const int32_t np = pairs_of(d.in_dtype);
         const int64_t per = std::max<int64_t>(d.rows, 1) * 2 * terms_of(d.in_dtype);
-        piece = std::max<int64_t>((int64_t(256) << 20) / per / 256 * 256, 4096);
+        piece = std::max<int64_t>((int64_t(512) << 20) / per / 256 * 256, 4096);
         piece = std::min(piece, up(d.out_features, 256));
         // pieces of nearly equal width
         const int64_t n = (d.out_features + piece - 1) / piece;
         piece = up((d.out_features + n - 1) / n, 256);
         sp = shape_of(d.rows, piece, steps_of(d.in_features, np), false);
-        sx = shape_of(d.rows, d.in_features, steps_of(piece, np), true);
+        sx = Shape{true, 0};
         sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true);
         p = ws.take<uint16_t>(terms_of(d.in_dtype) * up(d.rows, 64) * piece);
-        part_x = ws.take<float>(sx.splits * d.rows * d.in_features);   // summed over the pieces
+        // summed over the pieces: what the splits of any number of rows take
+        const int64_t e = tile_edge(true), cols = (d.in_features + e - 1) / e;
+        part_x = ws.take<float>(std::max(d.rows, std::min(d.rows * kMostSplits, kChip / std::min<int64_t>(cols, kChip) * e)) * d.in_features);
         part_w = ws.take<float>(part_size(sw, piece, d.in_features));
     }
 };
@@ -611,7 +615,7 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
     if (dx) {
         StoreArgs s = plain_store(dx, dx_stride, d->in_dtype);
         s.row_of = p.rows.row_of;
-        TRY(launch_join(p.part_x, p.sx.splits, rows, static_cast<int32_t>(K), p.rows.count, s, stream));
+        TRY(launch_join(p.part_x, 0, 1, rows, static_cast<int32_t>(K), p.rows.count, s, stream));
         TRY(launch_zero_rows(labels, exclude, vocab, rows, dx, dx_stride, static_cast<int32_t>(K),
                              d->in_dtype == BDLM_DTYPE_BF16, stream));
     }

@@ -164,11 +164,11 @@ struct RowData {
 // Four columns of one row of a tile, in their place.
 template <int OUT>
 __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias, const RowData &d, int64_t r, int c,
-                                          int split) {
+                                          int nrow, int split) {
     if constexpr (OUT == kTileStore) {
         store4(a.store, v, bias, r, c, a.ncol);
     } else if constexpr (OUT == kTilePartial) {
-        float *to = a.part + (int64_t(split) * a.nrow + r) * a.ncol + c;
+        float *to = a.part + (int64_t(split) * (a.splits ? a.nrow : nrow) + r) * a.ncol + c;
         if (c + 4 <= a.ncol && a.ncol % 4 == 0) {
             if (a.add) v += *reinterpret_cast<const f32x4 *>(to);
             *reinterpret_cast<f32x4 *>(to) = v;
@@ -265,7 +265,8 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
     // Consecutive workgroups go to the eight XCDs in turn: each XCD takes a run of the tile
     // order, four tile rows by all columns at a time, so that the tiles that run together on it
     // share rows and columns in its L2.
-    const uint32_t total = static_cast<uint32_t>(tr) * tc * a.splits;
+    const int splits = a.splits ? a.splits : split_count(int64_t(tr) * tc);
+    const uint32_t total = static_cast<uint32_t>(tr) * tc * splits;
     const uint32_t id = blockIdx.x;
     if (id >= total) return;
     const uint32_t q = total >> 3, rem = total & 7, xcd = id & 7;
@@ -280,8 +281,8 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
 
     const int nkt = (K + kDepth - 1) / kDepth;
     const int64_t steps = int64_t(nkt) * a.npair;
-    const int it0 = static_cast<int>(steps * split / a.splits);
-    const int n = static_cast<int>(steps * (split + 1) / a.splits) - it0;
+    const int it0 = static_cast<int>(steps * split / splits);
+    const int n = static_cast<int>(steps * (split + 1) / splits) - it0;
 
     Stage<E, COLT, WAVES, true> sc;
     Stage<E, ROWT, WAVES, false> sr;
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
                 const f32x4 v = mine[x * kQuads + (quad ^ (x & 15))];
                 RowData d{};
                 if constexpr (OUT == kTileProb) d = rows[r1 + x];
-                if (x < most) tile_quad<OUT>(a, v, bias, d, row0 + r1 + x, col1 + 4 * quad, split);
+                if (x < most) tile_quad<OUT>(a, v, bias, d, row0 + r1 + x, col1 + 4 * quad, nrow, split);
             }
         }
         __builtin_amdgcn_wave_barrier();
@@ -494,11 +495,12 @@ hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
 }
 
 // out = epilogue(sum of the slices), four columns per thread
-__global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int splits, int nrow, int ncol,
+__global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int splits, int edge, int nrow, int ncol,
                                                         const int32_t *nrow_dev, const StoreArgs s) {
     const int quads = (ncol + 3) / 4;
     const int64_t rows = nrow_dev ? *nrow_dev : nrow;
-    const int64_t slice = int64_t(nrow) * ncol;
+    const int64_t slice = (splits ? int64_t(nrow) : rows) * ncol;
+    if (splits == 0) splits = split_count(((rows + edge - 1) / edge) * ((ncol + edge - 1) / edge));
     for (int64_t x = blockIdx.x * int64_t(256) + threadIdx.x; x < rows * quads; x += gridDim.x * int64_t(256)) {
         const int64_t r = x / quads;
         const int c = static_cast<int>(x - r * quads) * 4;
@@ -520,7 +522,9 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
 int launch_tile(const TileArgs &a, void *stream) {
     if (a.nrow <= 0 || a.ncol <= 0) return BDLM_OK;
     const int64_t e = tile_edge(a.big);
-    const int64_t tiles = ((a.nrow + e - 1) / e) * ((a.ncol + e - 1) / e) * a.splits;
+    int64_t tiles = ((a.nrow + e - 1) / e) * ((a.ncol + e - 1) / e);
+    // (splits 0: fewer rows make more splits, never more than the chip holds)
+    tiles = a.splits ? tiles * a.splits : tiles > kChip ? tiles : kChip;
     if (tiles > (int64_t(1) << 30)) return BDLM_E_SHAPE;
     const dim3 g(static_cast<unsigned>(tiles));
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -541,13 +545,13 @@ int launch_tile(const TileArgs &a, void *stream) {
     return r == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }
 
-int launch_join(const float *part, int32_t splits, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
+int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
                 const StoreArgs &s, void *stream) {
     if (nrow <= 0 || ncol <= 0) return BDLM_OK;
     const int64_t blocks = (int64_t(nrow) * ((ncol + 3) / 4) + 255) / 256;
     const dim3 g(static_cast<unsigned>(blocks < 8192 ? blocks : 8192));
-    hipLaunchKernelGGL(bdlm_join_kernel, g, dim3(256), 0, static_cast<hipStream_t>(stream), part, splits, nrow,
-                       ncol, nrow_dev, s);
+    hipLaunchKernelGGL(bdlm_join_kernel, g, dim3(256), 0, static_cast<hipStream_t>(stream), part, splits,
+                       tile_edge(big), nrow, ncol, nrow_dev, s);
     return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }
 
