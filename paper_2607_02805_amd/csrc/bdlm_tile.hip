@@ -248,12 +248,12 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
 //
 // E 256: one wave on each SIMD, 256 accumulators a lane.  E 128: two workgroups on a CU, so that
 // one's epilogue meets the other's products.
-template <int E, int WR, int WC, bool ROWT, bool COLT, int OUT>
-__global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileArgs a) {
+template <int E, int WR, int WC, int BUFS, bool ROWT, bool COLT, int OUT>
+__global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_kernel(const TileArgs a) {
     constexpr int WAVES = WR * WC, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
     constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's stage
     constexpr int kRec = OUT == kTileBest ? E : 1;
-    __shared__ uint4 sm[2][2 * kBuf];                    // [buffer][col, then row]
+    __shared__ uint4 sm[BUFS][2 * kBuf];                 // [buffer][col, then row]
     __shared__ RowData rows[OUT == kTileProb || OUT == kTileBest ? E : 1];
     __shared__ float top[WC][kRec], others[WC][kRec];    // softmax records of the waves' columns
     __shared__ int at[WC][kRec];
@@ -359,9 +359,10 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
     // Group g of the stage in buffer `buf`.  Between its products: the reads of the next group (of the
     // last one: the next stage's first, or nothing's where there is none), and, if `copies`, a
     // part of a stage's copies.  No product lies in a branch, so that no accumulator is moved.
-    auto group = [&](auto g_, int buf, bool copies) {
+    auto group = [&](auto g_, int s, bool copies) {
         constexpr int g = decltype(g_)::value;
         constexpr bool last = g == kGroups - 1;
+        const int buf = s % BUFS, after = (s + 1) % BUFS, before = (s + BUFS - 1) % BUFS;
         constexpr int copies_from = g == 0 ? kC3 : kC3 + kC0, count = last ? kC3 : g == 0 ? kC0 : g == 1 ? kC1 : 0;
         __builtin_amdgcn_sched_barrier(0);
         constexpr int kMeet = kProducts * 6 / 16;   // products before the waves meet, in the last group
@@ -371,49 +372,51 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (last) {
                 if (x + 1 == kMeet) {
-                    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                    // the next stage has arrived: only later ones' copies may be on their way
+                    if (BUFS > 2 && s + BUFS <= n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
                 }
             }
             constexpr int from = last ? kMeet - 1 : 0, slots = kProducts - from;
-            const int s = x - from;
-            if (s >= 0) {
+            const int slot = x - from;
+            if (slot >= 0) {
 #pragma unroll
                 for (int k = 0; k < kReads; ++k)
-                    if (k * slots / kReads == s) read(order(k), last ? buf ^ 1 : buf, (g + 1) % kGroups);
+                    if (k * slots / kReads == slot) read(order(k), last ? after : buf, (g + 1) % kGroups);
 #pragma unroll
                 for (int k = 0; k < count; ++k)
-                    if (k * slots / count == s && copies)
-                        copy(last ? k : copies_from + k, last ? buf : buf ^ 1, last ? next : prev);
+                    if (k * slots / count == slot && copies)
+                        copy(last ? k : copies_from + k, last ? buf : before, last ? next : prev);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     if (n > 0) {
+        // all of the first stages, and a first part of the one in the last buffer
 #pragma unroll
-        for (int k = 0; k < kCopies; ++k) copy(k, 0, next);
-        if (n > 1) {
-            advance();
+        for (int s = 0; s < BUFS; ++s) {
+            if (s >= n) break;
+            if (s > 0) advance();
 #pragma unroll
-            for (int k = 0; k < kC3; ++k) copy(k, 1, next);
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kC3) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            for (int k = 0; k < (s + 1 < BUFS ? kCopies : kC3); ++k) copy(k, s, next);
         }
+        if (n >= BUFS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies + kC3) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int x = 0; x < kReads; ++x) read(x, 0, 0);
     }
     for (int s = 0; s < n; ++s) {
-        const int buf = s & 1;
+        // stage s + BUFS is copied over stage s: from the last group on, through the next stage's first two
         prev = next;
-        if (s + 2 < n) advance();
-        group(Int<0>{}, buf, s + 1 < n);
-        group(Int<1>{}, buf, s + 1 < n);
-        group(Int<2>{}, buf, false);
-        group(Int<3>{}, buf, s + 2 < n);
+        if (s + BUFS < n) advance();
+        group(Int<0>{}, s, s + BUFS - 1 < n);
+        group(Int<1>{}, s, s + BUFS - 1 < n);
+        group(Int<2>{}, s, false);
+        group(Int<3>{}, s, s + BUFS < n);
         settle(acc);
     }
     __syncthreads();   // every wave has read the last stage
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
     // consecutive columns, or a lane has a whole row; quads are permuted by the row against bank
     // conflicts.
     constexpr int kCols = E / WC, kQuads = kCols / 4, kRows = 64 / kQuads;   // rows of one pass of the wave
-    static_assert(WAVES * 64 * kCols * 4 == int(sizeof(sm)), "the waves' regions fill the buffers");
+    static_assert(WAVES * 64 * kCols * 4 <= int(sizeof(sm)), "the waves' regions fit");
     f32x4 *mine = reinterpret_cast<f32x4 *>(sm) + wave * 64 * kQuads;
     const int rows_out = OUT == kTileProb ? (nrow + 63) / 64 * 64 : nrow;
     const int col1 = static_cast<int>(col0) + wc * kCols;   // the wave's first column
@@ -489,8 +492,12 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) bdlm_tile_kernel(const TileAr
 
 template <bool ROWT, bool COLT, int OUT>
 hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
-    if (a.big) hipLaunchKernelGGL((bdlm_tile_kernel<256, 2, 4, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, ROWT, COLT, OUT>), g, dim3(256), 0, s, a);
+    // Small tiles that leave a CU one workgroup take four buffers, so that copies have three stages to
+    // arrive (a stage of theirs is 512 cycles of products).
+    if (a.big) hipLaunchKernelGGL((bdlm_tile_kernel<256, 2, 4, 2, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
+    else if (g.x <= static_cast<unsigned>(kChip))
+        hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 4, ROWT, COLT, OUT>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, ROWT, COLT, OUT>), g, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
