@@ -53,7 +53,7 @@ struct BestArgs {
 struct ProbArgs {
     uint16_t *p;               // [terms][nrow][ld]
     int64_t ld, plane;
-    int32_t terms;             // 1 or 3
+    int32_t terms;             // 1, 2 or 3
     const float *lse, *loss, *weight;   // [nrow]
     const int32_t *label;      // [nrow], counted from column 0 of the vocabulary
     int32_t exclude, col0;     // col0: the vocabulary column of the call's column 0
@@ -70,7 +70,7 @@ struct TileArgs {
     Mat row, col;
     int32_t nrow, ncol, k;
     const int32_t *nrow_dev, *k_dev;   // the count in device memory, at most nrow / k (null: nrow / k)
-    int32_t npair;                     // 1 or 6
+    int32_t npair;                     // pairs of planes: 1, 2 (two terms of row) or 6 (three of each)
     int32_t row_t, col_t;
     int32_t big;                       // 1: 256 x 256 tiles, 0: 128 x 128
     int32_t splits;                    // > 1: kTilePartial only; 0: as many as fill the chip with
@@ -117,7 +117,7 @@ constexpr int32_t kSkinnyCols = 32;
 int launch_skinny(const SkinnyArgs &a, void *stream);
 
 // Copies an operand to bf16 terms: dst[p][r][0 .. ld_dst) from src rows (row_of: gathered),
-// zeros past cols, and rows of zeros past the last one up to a multiple of 64 (dst has them).  terms 1 (bf16 source, or fp32 rounded to bf16) or 3 (fp32 source).
+// X
 struct PackArgs {
     const void *src;
     int64_t ld;
@@ -134,7 +134,7 @@ struct PackArgs {
     float *colsum;             // [pack_row_blocks(rows)][cols] partial column sums of dst, or null
 };
 int launch_pack(const PackArgs &a, void *stream);
-constexpr int32_t kPackRows = 32;   // rows per workgroup
+constexpr int32_t kPackRows = 16;   // rows per workgroup
 inline int32_t pack_row_blocks(int32_t rows) { return (rows + 63) / 64 * (64 / kPackRows); }
 // out[c] = sum over the blocks of part[b][c]
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream);

@@ -58,7 +58,7 @@ __device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, const 
 #pragma unroll
     for (int e = 0; e < 8; ++e) split_terms(v[e], h[e]);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < TERMS; ++k) {
         uint32_t u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = h[2 * e][k] | uint32_t(h[2 * e + 1][k]) << 16;
@@ -253,16 +253,20 @@ int launch_pack(const PackArgs &a, void *stream) {
     const bool grad = a.act != BDLM_ACT_NONE || a.colsum;
     // (dy may be fp32 where the projection's inputs, and pre, are bf16; not the other way round
     // for a plain copy)
-    const int kind = (a.terms == 3 ? 4 : 0) + (a.src_bf16 ? 2 : 0) + (grad ? 1 : 0);
+    const int kind = (a.terms - 1) * 4 + (a.src_bf16 ? 2 : 0) + (grad ? 1 : 0);
     switch (kind) {
         case 3: hipLaunchKernelGGL((bdlm_pack_kernel<true, true, true, 1>), g, b, 0, s, a); break;
         case 1: hipLaunchKernelGGL((bdlm_pack_kernel<true, false, true, 1>), g, b, 0, s, a); break;
-        case 7: hipLaunchKernelGGL((bdlm_pack_kernel<true, true, false, 3>), g, b, 0, s, a); break;
-        case 5: hipLaunchKernelGGL((bdlm_pack_kernel<true, false, false, 3>), g, b, 0, s, a); break;
+        case 7: hipLaunchKernelGGL((bdlm_pack_kernel<true, true, true, 2>), g, b, 0, s, a); break;
+        case 5: hipLaunchKernelGGL((bdlm_pack_kernel<true, false, true, 2>), g, b, 0, s, a); break;
+        case 4: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, true, 2>), g, b, 0, s, a); break;
+        case 11: hipLaunchKernelGGL((bdlm_pack_kernel<true, true, false, 3>), g, b, 0, s, a); break;
+        case 9: hipLaunchKernelGGL((bdlm_pack_kernel<true, false, false, 3>), g, b, 0, s, a); break;
         case 2: hipLaunchKernelGGL((bdlm_pack_kernel<false, true, true, 1>), g, b, 0, s, a); break;
         case 0: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, true, 1>), g, b, 0, s, a); break;
-        case 4: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, false, 3>), g, b, 0, s, a); break;
-        case 6: hipLaunchKernelGGL((bdlm_pack_kernel<false, true, false, 3>), g, b, 0, s, a); break;
+        case 8: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, false, 3>), g, b, 0, s, a); break;
+        case 10: hipLaunchKernelGGL((bdlm_pack_kernel<false, true, false, 3>), g, b, 0, s, a); break;
+        default: return BDLM_E_LAUNCH;
     }
     return done();
 }

@@ -22,14 +22,20 @@ int64_t elem_size(int32_t dt) { return dt == BDLM_DTYPE_BF16 ? 2 : 4; }
 bool known(int32_t dt) { return dt == BDLM_DTYPE_F32 || dt == BDLM_DTYPE_BF16; }
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// [p, p + bytes): the memory of rows x cols elements with a row stride
+// The memory of rows x cols elements with a row stride: `row` bytes every `ld`, `bytes` in all.
 struct Span {
-    uintptr_t p;
-    uintptr_t bytes;
-    Span(const void *q, int64_t rows, int64_t cols, int64_t ld, int64_t es)
+    uintptr_t p, bytes, row, ld;
+    Span(const void *q, int64_t rows, int64_t cols, int64_t stride, int64_t es)
         : p(reinterpret_cast<uintptr_t>(q)),
-          bytes(q && rows > 0 && cols > 0 ? static_cast<uintptr_t>(((rows - 1) * ld + cols) * es) : 0) {}
-    bool meets(const Span &o) const { return bytes && o.bytes && p < o.p + o.bytes && o.p < p + bytes; }
+          bytes(q && rows > 0 && cols > 0 ? static_cast<uintptr_t>(((rows - 1) * stride + cols) * es) : 0),
+          row(static_cast<uintptr_t>(cols * es)), ld(static_cast<uintptr_t>(stride * es)) {}
+    bool meets(const Span &o) const {
+        if (!bytes || !o.bytes || p >= o.p + o.bytes || o.p >= p + bytes) return false;
+        if (ld != o.ld || ld == 0) return true;
+        // column slices of one matrix: apart if the other's columns lie between this one's rows
+        const uintptr_t at = o.p >= p ? (o.p - p) % ld : (ld - (p - o.p) % ld) % ld;
+        return at < row || at + o.row > ld;
+    }
 };
 
 int check_desc(const bdlm_dense_desc_t *d) {
@@ -151,6 +157,13 @@ TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, int64_t
     a.splits = s.splits;
     return a;
 }
+// Terms of a gradient's first operand (dz, or the logits' gradients).  With bf16 inputs they are
+// rounded to bf16, as the activations of the forward products are; of few rows, where an
+// output's errors do not average out and the weights' bytes bound the products, two terms are kept.
+int grad_terms(const bdlm_dense_desc_t &d) {
+    return d.in_dtype != BDLM_DTYPE_BF16 ? 3 : d.rows <= kSkinnyRows ? 2 : 1;
+}
+int32_t grad_pairs(int terms) { return terms == 3 ? 6 : terms; }
 int32_t pairs_of(int32_t dtype) { return dtype == BDLM_DTYPE_BF16 ? 1 : 6; }
 int64_t steps_of(int64_t k, int32_t npair) { return (k + 63) / 64 * npair; }
 
@@ -203,11 +216,11 @@ struct BackwardPlan {
     BackwardPlan(const bdlm_dense_desc_t &d, const void *px, const void *pw, void *p)
         : ws(p), x(px, d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
           w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
-        const int32_t np = pairs_of(d.in_dtype);
+        const int32_t np = grad_pairs(grad_terms(d));
         sx = shape_of(d.rows, d.in_features, steps_of(d.out_features, np), true);
         sw = shape_of(d.out_features, d.in_features, steps_of(d.rows, np), true);
         ld_dz = up(d.out_features, 64);
-        dz = ws.take<uint16_t>(terms_of(d.in_dtype) * up(d.rows, 64) * ld_dz);
+        dz = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * ld_dz);
         sums = ws.take<float>(int64_t(pack_row_blocks(static_cast<int32_t>(d.rows))) * d.out_features);
         part = ws.take<float>(std::max(part_size(sx, d.rows, d.in_features),
                                        part_size(sw, d.out_features, d.in_features)));
@@ -286,17 +299,17 @@ struct LossBackwardPlan {
     LossBackwardPlan(const bdlm_dense_desc_t &d, const void *px, const void *pw, void *mem)
         : ws(mem), rows(d.rows, true, ws), x(px, d.rows, d.in_features, d.x_stride, d.in_dtype, true, ws),
           w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
-        const int32_t np = pairs_of(d.in_dtype);
-        const int64_t per = std::max<int64_t>(d.rows, 1) * 2 * terms_of(d.in_dtype);
+        const int32_t np = grad_pairs(grad_terms(d));
+        const int64_t per = std::max<int64_t>(d.rows, 1) * 2 * grad_terms(d);
         piece = std::max<int64_t>((int64_t(512) << 20) / per / 256 * 256, 4096);
         piece = std::min(piece, up(d.out_features, 256));
         // pieces of nearly equal width
         const int64_t n = (d.out_features + piece - 1) / piece;
         piece = up((d.out_features + n - 1) / n, 256);
-        sp = shape_of(d.rows, piece, steps_of(d.in_features, np), false);
+        sp = shape_of(d.rows, piece, steps_of(d.in_features, pairs_of(d.in_dtype)), false);
         sx = Shape{true, 0};
         sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true);
-        p = ws.take<uint16_t>(terms_of(d.in_dtype) * up(d.rows, 64) * piece);
+        p = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * piece);
         // summed over the pieces: what the splits of any number of rows take
         const int64_t e = tile_edge(true), cols = (d.in_features + e - 1) / e;
         part_x = ws.take<float>(std::max(d.rows, std::min(d.rows * kMostSplits, kChip / std::min<int64_t>(cols, kChip) * e)) * d.in_features);
@@ -475,12 +488,12 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int32_t dy
     TRY(bdlm_check_projection_backward(d, act, dy_dtype, dy, dy_stride, x, w, pre, pre_stride, dx, dx_stride, dw,
                                        dw_stride, db, ws, ws_bytes));
     BackwardPlan p(*d, x, w, ws);
-    const int32_t np = pairs_of(d->in_dtype);
-    // dy as it is, where it can be an operand; else dz (rounded to the inputs' type, as the
-    // activations of the forward products are)
-    const bool direct = act == BDLM_ACT_NONE && d->in_dtype == BDLM_DTYPE_BF16 && dy_dtype == BDLM_DTYPE_BF16 &&
-                        d->out_features % 64 == 0 && d->rows % 64 == 0 && dy_stride % 8 == 0 &&
+    // dy as it is, where it can be an operand; else dz (a bf16 dy without an activation is one term)
+    const bool exact = act == BDLM_ACT_NONE && d->in_dtype == BDLM_DTYPE_BF16 && dy_dtype == BDLM_DTYPE_BF16;
+    const int terms = exact ? 1 : grad_terms(*d);
+    const bool direct = exact && d->out_features % 64 == 0 && d->rows % 64 == 0 && dy_stride % 8 == 0 &&
                         dy_stride <= kMaxDirect;
+    const int32_t np = grad_pairs(terms);
     Mat dz{p.dz, p.ld_dz, up(d->rows, 64) * p.ld_dz};
     if (direct) dz = Mat{static_cast<const uint16_t *>(dy), dy_stride, 0};
     if (!direct || db) {
@@ -493,7 +506,7 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int32_t dy
         a.dst = direct || (!dx && !dw) ? nullptr : p.dz;
         a.ld_dst = p.ld_dz;
         a.plane = dz.plane;
-        a.terms = terms_of(d->in_dtype);
+        a.terms = terms;
         a.act = act;
         a.pre = pre;
         a.ld_pre = pre_stride;
@@ -579,7 +592,7 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
     if (!dx && !dw) return BDLM_OK;
     LossBackwardPlan p(*d, x, w, ws);
     const int32_t rows = static_cast<int32_t>(d->rows), vocab = static_cast<int32_t>(d->out_features);
-    const int32_t none = token_or_none(d, exclude), np = pairs_of(d->in_dtype), terms = terms_of(d->in_dtype);
+    const int32_t none = token_or_none(d, exclude), terms = grad_terms(*d), np = grad_pairs(terms);
     const int64_t K = d->in_features;
     TRY(launch_rows(RowsArgs{labels, rows, vocab, exclude, p.rows.count, p.rows.row_of, p.rows.label, dloss, loss,
                              lse, p.rows.weight, p.rows.loss, p.rows.lse},
@@ -590,7 +603,7 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
     for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, vocab - v0);
         const Mat w_at{p.w.mat.p + v0 * p.w.mat.ld, p.w.mat.ld, p.w.mat.plane};
-        TileArgs a = product(p.x.mat, false, w_at, false, rows, n, K, np, p.sp);
+        TileArgs a = product(p.x.mat, false, w_at, false, rows, n, K, pairs_of(d->in_dtype), p.sp);
         a.nrow_dev = p.rows.count;
         a.out = kTileProb;
         a.prob = ProbArgs{p.p, pm.ld, pm.plane, terms, p.rows.lse, p.rows.loss, p.rows.weight, p.rows.label, none,

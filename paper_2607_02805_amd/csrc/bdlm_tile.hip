@@ -145,9 +145,9 @@ struct Reader {
     }
 };
 
-// Plane pairs in order of weight: pair i multiplies term row_term(i) of `row` and col_term(i) of
-// `col`.
-__device__ __forceinline__ int row_term(int npair, int i) { return npair == 6 ? (0x010210 >> (4 * i)) & 15 : 0; }
+// Pair i of planes multiplies term row_term(i) of `row` and col_term(i) of `col`: of two fp32
+// operands the six of weight 2^-16 or more, of a `row` in two terms and a bf16 `col` both.
+__device__ __forceinline__ int row_term(int npair, int i) { return npair == 6 ? (0x010210 >> (4 * i)) & 15 : i; }
 __device__ __forceinline__ int col_term(int npair, int i) { return npair == 6 ? (0x102010 >> (4 * i)) & 15 : 0; }
 
 template <int V>
@@ -179,13 +179,21 @@ __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias
     } else {
         const ProbArgs &b = a.prob;
         if (c >= b.width) return;
-        const int exclude = b.exclude - b.col0;
+        if (b.terms == 3) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float x = v[e] - d.lse;
-            v[e] = d.g * (b.terms == 1 ? __expf(x) : expf(x));
-            if (c + e == d.label) v[e] = d.hot;
-            if (c + e >= a.ncol || c + e == exclude) v[e] = 0.f;
+            for (int e = 0; e < 4; ++e) v[e] = d.g * expf(v[e] - d.lse);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = d.g * __builtin_amdgcn_exp2f((v[e] - d.lse) * kLog2e);
+        }
+        // few quads hold a label, the excluded token or columns past the end
+        const unsigned label = d.label - c, exclude = b.exclude - b.col0 - c;
+        if (label < 4u || exclude < 4u || c + 4 > a.ncol) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (label == static_cast<unsigned>(e)) v[e] = d.hot;
+                if (c + e >= a.ncol || exclude == static_cast<unsigned>(e)) v[e] = 0.f;
+            }
         }
         uint16_t *to = b.p + r * b.ld + c;
         if (b.terms == 1) {
@@ -196,8 +204,9 @@ __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias
             for (int e = 0; e < 4; ++e) split_terms(v[e], h[e]);
 #pragma unroll
             for (int k = 0; k < 3; ++k)
-                *reinterpret_cast<uint2 *>(to + k * b.plane) =
-                    uint2{h[0][k] | uint32_t(h[1][k]) << 16, h[2][k] | uint32_t(h[3][k]) << 16};
+                if (k < b.terms)
+                    *reinterpret_cast<uint2 *>(to + k * b.plane) =
+                        uint2{h[0][k] | uint32_t(h[1][k]) << 16, h[2][k] | uint32_t(h[3][k]) << 16};
         }
     }
 }

@@ -124,3 +124,422 @@ def test_head_loss(size, dtype):
         want_dx, want_dw = du.head_loss_backward64(dloss, x, w, labels, exclude)
         near(dx, want_dx, "dx")
         near(dw, want_dw, "dw")
+
+
+# ------------------------------------------------------------------ layouts
+def test_strided_views_and_mixed_types():
+    """Row slices of wider matrices whose strides and padding are odd (the padding holds NaN), bf16
+    inputs with an fp32 residual stream, fp32 inputs with a bf16 output, and the residual
+    updated in place."""
+    import paper_2607_02805_amd as bd
+    r = gen(11)
+    for m, k, n in ((70, 130, 257), (5, 130, 257), (200, 192, 64), (33, 64, 40)):
+        for dtype, other in ((BF, F32), (F32, BF)):
+            say("strided", m, k, n, dtype)
+            wide = torch.full((m, k + 45), float("nan"), dtype=dtype, device=DEV)
+            wide[:, 16:16 + k] = r(m, k).to(dtype)
+            ww = torch.full((n, k + 9), float("nan"), dtype=dtype, device=DEV)
+            ww[:, :k] = (r(n, k) / k ** 0.5).to(dtype)
+            x, w = wide[:, 16:16 + k], ww[:, :k]
+            x3 = x
+            if x.data_ptr() % 16:
+                x3 = x.clone()
+            res = torch.full((m, n + 11), 7.0, dtype=other, device=DEV)
+            res[:, :n] = r(m, n).to(other)
+            keep = res.clone()
+            pre = torch.full((m, n + 3), 5.0, dtype=dtype, device=DEV)
+            got = bd.projection(x3, w, act="silu", residual=res[:, :n], out=res[:, :n], pre=pre[:, :n])
+            torch.cuda.synchronize()
+            assert got[0].data_ptr() == res.data_ptr()
+            want, want_pre = du.projection64(x, w, None, "silu", keep[:, :n], out_dtype=other)
+            near(res[:, :n], want, "out")
+            near(pre[:, :n], want_pre, "pre")
+            assert bool((res[:, n:] == 7.0).all()) and bool((pre[:, n:] == 5.0).all())
+            # the gradient's dy in the other type, its outputs in slices
+            dx = torch.full((m, k + 5), 3.0, dtype=dtype, device=DEV)
+            dw = torch.full((n, k + 7), 3.0, dtype=dtype, device=DEV)
+            dy = torch.full((m, n + 1), float("nan"), dtype=other, device=DEV)
+            dy[:, :n] = r(m, n).to(other)
+            out = bd.projection_backward(dy[:, :n], x3, w, pre=pre[:, :n], act="silu", dx=dx[:, :k], dw=dw[:, :k],
+                                         db=True)
+            torch.cuda.synchronize()
+            for g, want, what in zip(out, du.projection_backward64(dy[:, :n], x, w, pre[:, :n], "silu"),
+                                     ("dx", "dw", "db")):
+                near(g, want, what)
+            assert bool((dx[:, k:] == 3.0).all()) and bool((dw[:, k:] == 3.0).all())
+
+
+def test_leading_dimensions_and_repeated_rows():
+    """[batch, length, features] as rows, a token slice of a longer sequence where it lies at one
+    stride, and a row repeated by a stride of 0."""
+    import paper_2607_02805_amd as bd
+    r = gen(12)
+    x = r(2, 50, 128).to(BF).to(DEV)
+    w = (r(96, 128) / 11).to(BF).to(DEV)
+    out = bd.projection(x, w)
+    assert out.shape == (2, 50, 96)
+    near(out, du.projection64(x, w)[0], "3-d")
+    one = x[:1, :1].expand(1, 70, 128)
+    near(bd.projection(one, w), du.projection64(one, w)[0], "repeated")
+    token, logprob = bd.head_select(x, w)
+    assert token.shape == logprob.shape == (2, 50)
+    step = x[:, 4:8]        # two runs of rows: not one stride
+    with pytest.raises(ValueError, match="one stride"):
+        bd.projection(step, w)
+    near(bd.projection(step.contiguous(), w), du.projection64(step, w)[0], "slice")
+
+
+def test_only_what_is_asked_for():
+    import paper_2607_02805_amd as bd
+    r = gen(13)
+    for m in (9, 140):
+        x, w = r(m, 72).to(BF).to(DEV), (r(130, 72) / 8).to(BF).to(DEV)
+        dy = r(m, 130).to(BF).to(DEV)
+        full = bd.projection_backward(dy, x, w, db=True)
+        for keep in range(3):
+            want = [True if i == keep else None for i in range(3)]
+            got = bd.projection_backward(dy, x, w, dx=want[0], dw=want[1], db=want[2])
+            for i in range(3):
+                assert (got[i] is None) == (i != keep)
+                if i == keep:
+                    assert torch.equal(got[i], full[i])
+        labels = torch.arange(m, device=DEV) % 130
+        loss, lse = bd.head_loss(x, w, labels)
+        g = torch.ones(m, device=DEV)
+        dx, dw = bd.head_loss_backward(g, x, w, labels, loss, lse)
+        a, none = bd.head_loss_backward(g, x, w, labels, loss, lse, dw=None)
+        assert none is None and torch.equal(a, dx)
+        none, b = bd.head_loss_backward(g, x, w, labels, loss, lse, dx=None)
+        assert none is None and torch.equal(b, dw)
+
+
+def test_rows_far_apart():
+    """Offsets past 32 bits: rows 2^31 elements apart, and 1,100,000 rows of 2,048."""
+    import paper_2607_02805_amd as bd
+    r = gen(14)
+    big = torch.zeros(2 * 2 ** 31 + 4096, dtype=BF, device=DEV)
+    w = (r(80, 256) / 16).to(BF).to(DEV)
+    for base in (0, 64):
+        x = big.as_strided((3, 256), (2 ** 31, 1), base)
+        x.copy_(r(3, 256).to(BF))
+        say("rows 2^31 elements apart")
+        near(bd.projection(x, w), du.projection64(x, w)[0], "few rows")
+        dx, dw, _ = bd.projection_backward(r(3, 80).to(BF).to(DEV), x, w)
+        assert bool(torch.isfinite(dw).all())
+        out = big.as_strided((3, 80), (2 ** 31, 1), 2048)
+        bd.projection(x, w, out=out)
+        near(out, du.projection64(x, w)[0], "far outputs")
+    del big
+    rows = 1_100_000
+    x = torch.randn(rows, 2048, device=DEV, dtype=BF)
+    w = (r(64, 2048) / 45).to(BF).to(DEV)
+    say("1,100,000 rows")
+    out = bd.projection(x, w)
+    at = torch.tensor([0, 1, 255, 256, 524_287, 524_288, 1_048_575, 1_048_577, rows - 1], device=DEV)
+    near(out[at], du.projection64(x[at], w)[0], "rows")
+    assert bool(torch.isfinite(out).all())
+
+
+# ------------------------------------------------------------------ heads: ties, exclusions, non-finite
+@pytest.mark.parametrize("m", [3, 40, 90])
+def test_ties_go_to_the_lowest_token(m):
+    import paper_2607_02805_amd as bd
+    r = gen(15)
+    n, k = 1100, 64
+    w = (0.1 * r(n, k)).to(BF)
+    x = r(m, k).to(BF)
+    same = [37, 38, 300, 511, 512, 1024, 1099]
+    w[same] = (4 * x[0]).to(BF)                      # the same logits for every row
+    x = x[:1].expand(m, k).contiguous()
+    x, w = x.to(DEV), w.to(DEV)
+    for out, want in ((-1, 37), (37, 38), (500, 37)):
+        token, logprob = bd.head_select(x, w, exclude=out)
+        assert bool((token == want).all()), (out, token)
+        left = len(same) - (1 if out in same else 0)
+        assert bool((logprob + torch.log(torch.tensor(float(left)))).abs().max() < 1e-3)
+    labels = torch.full((m,), 512, device=DEV)
+    loss, _ = bd.head_loss(x, w, labels)
+    assert bool((loss - torch.log(torch.tensor(7.0))).abs().max() < 1e-3)
+
+
+@pytest.mark.parametrize("m", [4, 100])
+def test_sure_rows_keep_their_digits(m):
+    """A token ahead of the others by 12 and more: -log p of 1e-4 and less, to fp32's digits."""
+    import paper_2607_02805_amd as bd
+    r = gen(16)
+    n, k = 700, 64
+    w = (r(n, k) / 8).to(F32)
+    x = (14.0 + torch.arange(m)[:, None] % 7) * w[100:100 + m] / (w[100:100 + m] ** 2).sum(1, keepdim=True)
+    x, w = x.to(DEV), w.to(DEV)
+    labels = torch.arange(100, 100 + m, device=DEV)
+    loss, lse = bd.head_loss(x, w, labels)
+    token, logprob = bd.head_select(x, w)
+    l, e = du.head64(x, w)
+    want = torch.logsumexp(l, 1) - l.gather(1, labels.cpu()[:, None])[:, 0]
+    others = (l - l.gather(1, labels.cpu()[:, None])).exp().sum(1) - 1
+    assert torch.equal(token, labels)
+    for got in (loss, -logprob):
+        err = (got.double().cpu() - torch.log1p(others)).abs() / torch.log1p(others)
+        assert float(err.max()) < 2 * float(e.max()) + 1e-5, float(err.max())
+    assert float(want.max()) < 1.0
+
+
+def test_non_finite_values():
+    """NaN logits: never the token, and the row's loss and logprob are NaN; -infinity adds nothing;
+    rows beside them are untouched."""
+    import paper_2607_02805_amd as bd
+    r = gen(17)
+    n, k = 600, 64
+    for m in (6, 80):
+        x, w = r(m, k).to(BF).to(DEV), (r(n, k) / 8).to(BF).to(DEV)
+        clean_t, clean_p = bd.head_select(x, w)
+        labels = torch.arange(m, device=DEV) + 5
+        clean_l, clean_s = bd.head_loss(x, w, labels)
+        bad = x.clone()
+        bad[2, 3] = float("nan")
+        t, p = bd.head_select(bad, w)
+        loss, lse = bd.head_loss(bad, w, labels)
+        rest = torch.arange(m) != 2
+        assert torch.equal(t.cpu()[rest], clean_t.cpu()[rest]) and torch.equal(p.cpu()[rest], clean_p.cpu()[rest])
+        assert torch.equal(loss.cpu()[rest], clean_l.cpu()[rest]) and torch.equal(lse.cpu()[rest], clean_s.cpu()[rest])
+        assert int(t[2]) == 0 and bool(p[2].isnan()) and bool(loss[2].isnan())
+        assert int(bd.head_select(bad, w, exclude=0)[0][2]) == 1
+        # one vocabulary row far below: its share is 0
+        low = w.clone()
+        low[7] = 0
+        low[7, 0] = float("-inf")
+        pos = x.clone()
+        pos[:, 0] = 1.0
+        t, p = bd.head_select(pos, low)
+        t2, p2 = bd.head_select(pos, low, exclude=7)
+        assert torch.equal(t, t2) and bool(torch.isfinite(p).all())
+        assert float((p - p2).abs().max()) < 1e-6
+        # a row that is left out may hold anything
+        labels[2] = -100
+        loss, lse = bd.head_loss(bad, w, labels)
+        dx, dw = bd.head_loss_backward(torch.ones(m, device=DEV), bad, w, labels, loss, lse)
+        assert bool(torch.isfinite(loss).all()) and bool(torch.isfinite(dw).all())
+        assert bool((dx[2] == 0).all()) and bool(torch.isfinite(dx).all())
+
+
+def test_activations_far_out():
+    """Pre-activations of 1e4 and more, both ways, and infinities: values and slopes are the limits."""
+    import paper_2607_02805_amd as bd
+    z = torch.tensor([[-3e38, -1e4, -90.0, -20.0, -5.0, -1e-4, 0.0, 1e-4, 5.0, 20.0, 90.0, 1e4, 3e38,
+                       float("inf"), float("-inf"), float("nan")]])
+    n = z.shape[1]
+    x, w = torch.zeros(1, 8, device=DEV), torch.zeros(n, 8, device=DEV)
+    for m in (1, 70):
+        for act in ("silu", "gelu"):
+            bias = z[0].to(DEV)
+            out = bd.projection(x.expand(m, 8), w, bias, act=act)[0].cpu().double()
+            want = du.act64(z[0].double(), act)
+            want = torch.where(torch.isinf(z[0]) & (z[0] < 0), torch.zeros_like(want), want)
+            ok = torch.isfinite(want)
+            assert bool(((out - want)[ok].abs() <= 24 * du.F * z[0].double()[ok].abs() + 1e-37).all()), (act, out, want)
+            assert bool(out[13].isinf()) and bool(out[15].isnan())
+            dy = torch.ones(m, n, device=DEV)
+            _, _, db = bd.projection_backward(dy, x.expand(m, 8), w, pre=z.expand(m, n).contiguous().to(DEV),
+                                              act=act, dx=None, dw=None, db=True)
+            slope = torch.where(z[0].abs() > 100, (z[0] > 0).double(), du.slope64(z[0].double(), act))
+            got = db.cpu().double() / m
+            assert bool(((got - slope)[:15].abs() <= 32 * du.F).all()), (act, got, slope)
+            assert bool(db[15].isnan())
+
+
+def test_infinities_through_products():
+    import paper_2607_02805_amd as bd
+    r = gen(18)
+    for m in (5, 100):
+        for dtype in (BF, F32):
+            x, w = r(m, 64).to(dtype).to(DEV), r(40, 64).to(dtype).to(DEV)
+            x[1, 5] = float("inf")
+            out = bd.projection(x, w).cpu()
+            assert not bool(torch.isfinite(out[1]).any())
+            rest = torch.arange(m) != 1
+            assert bool(torch.isfinite(out[rest]).all())
+            x[1, 5] = 3.39e38                            # the last values that a bf16 term holds
+            w[:, 5] = 1e-38 if dtype == F32 else 1.0
+            assert bool(torch.isfinite(bd.projection(x * 0.5, w, out=torch.empty(m, 40, device=DEV))).all())
+
+
+# ------------------------------------------------------------------ nothing to do, nothing that counts
+def test_no_rows():
+    import paper_2607_02805_amd as bd
+    for dtype in (BF, F32):
+        x, w = torch.empty(0, 72, dtype=dtype, device=DEV), torch.ones(130, 72, dtype=dtype, device=DEV)
+        out, pre = bd.projection(x, w, act="gelu", pre=True)
+        assert out.shape == pre.shape == (0, 130)
+        dx, dw, db = bd.projection_backward(torch.empty(0, 130, dtype=dtype, device=DEV), x, w, db=True)
+        assert dx.shape == (0, 72) and bool((dw == 0).all()) and bool((db == 0).all())
+        labels = torch.empty(0, dtype=torch.int64, device=DEV)
+        loss, lse = bd.head_loss(x, w, labels)
+        dx, dw = bd.head_loss_backward(torch.empty(0, device=DEV), x, w, labels, loss, lse)
+        assert loss.shape == lse.shape == (0,) and dx.shape == (0, 72) and bool((dw == 0).all())
+        token, logprob = bd.head_select(x, w)
+        assert token.shape == logprob.shape == (0,)
+
+
+@pytest.mark.parametrize("m", [1, 7, 65, 200])
+def test_no_row_counts(m):
+    import paper_2607_02805_amd as bd
+    r = gen(19)
+    x, w = r(m, 72).to(BF).to(DEV), r(130, 72).to(BF).to(DEV)
+    x[0, 0] = float("nan")
+    for label in (-1, 130, 2 ** 40, -2 ** 62, 9):
+        labels = torch.full((m,), label, device=DEV)
+        loss, lse = bd.head_loss(x, w, labels, exclude=9)
+        dx, dw = bd.head_loss_backward(torch.ones(m, device=DEV), x, w, labels, loss, lse, exclude=9)
+        for t in (loss, lse, dx, dw):
+            assert bool((t == 0).all())
+
+
+def test_a_few_rows_count_of_many():
+    """Counts on both sides of the tiles and of the device's choice of splits."""
+    import paper_2607_02805_amd as bd
+    m, k, n = 1500, 136, 2100
+    for count in (1, 63, 64, 65, 256, 257, 700, 1499, 1500):
+        x, w, _, dloss = head_inputs(m, k, n, BF, 20)
+        g = torch.Generator().manual_seed(count)
+        labels = torch.full((m,), -1)
+        at = torch.randperm(m, generator=g)[:count]
+        labels[at] = torch.randint(0, n, (count,), generator=g)
+        labels = labels.to(DEV)
+        say("rows that count", count)
+        loss, lse = bd.head_loss(x, w, labels)
+        dx, dw = bd.head_loss_backward(dloss, x, w, labels, loss, lse)
+        near(loss, du.head_loss64(x, w, labels)[0], "loss")
+        want_dx, want_dw = du.head_loss_backward64(dloss, x, w, labels)
+        near(dx, want_dx, "dx")
+        near(dw, want_dw, "dw")
+
+
+def test_the_vocabulary_in_pieces():
+    """Rows enough that the logits' gradients go in several pieces: against the plain form in
+    fp32 on the GPU, on sampled rows and tokens in 64 bits."""
+    import paper_2607_02805_amd as bd
+    m, k, n = 9000, 64, 70001
+    g = torch.Generator(device=DEV).manual_seed(21)
+    x = torch.randn(m, k, generator=g, device=DEV).to(BF)
+    w = (torch.randn(n, k, generator=g, device=DEV) / 8).to(BF)
+    labels = torch.randint(0, n, (m,), generator=g, device=DEV)
+    dloss = torch.rand(m, generator=g, device=DEV) / m
+    loss, lse = bd.head_loss(x, w, labels)
+    dx, dw = bd.head_loss_backward(dloss, x, w, labels, loss, lse)
+    rows = torch.tensor([0, 1, 4095, 4096, 8999], device=DEV)
+    near(loss[rows], du.head_loss64(x[rows], w, labels[rows])[0], "loss")
+    near(dx[rows], du.head_loss_backward64(dloss[rows], x[rows], w, labels[rows])[0], "dx")
+    at = torch.tensor([0, 1, 16383, 16384, 23551, 29183, 29184, 35001, 70000, int(labels[5])], device=DEV)
+    ref = torch.zeros(len(at), k, dtype=torch.float64, device=DEV)
+    size = torch.zeros_like(ref)
+    for r0 in range(0, m, 1000):
+        xs = x[r0:r0 + 1000].double()
+        p = torch.exp(xs @ w[at].double().t() - lse[r0:r0 + 1000].double()[:, None])
+        p -= (labels[r0:r0 + 1000, None] == at).double()
+        p *= dloss[r0:r0 + 1000].double()[:, None]
+        ref += p.t().contiguous() @ xs
+        size += p.abs().t().contiguous() @ xs.abs()
+    tol = (2.0 ** -8 + 2e-5) * size + 2.0 ** -8 * ref.abs()
+    assert bool(((dw[at].double() - ref).abs() <= tol).all())
+
+
+# ------------------------------------------------------------------ streams, graphs, repeats
+def _all_calls(dtype, m, k, n, ws=None):
+    import paper_2607_02805_amd as bd
+    x, w, labels, dloss = head_inputs(m, k, n, dtype, 30)
+    r = gen(31)
+    dy, pre, bias = r(m, n).to(dtype).to(DEV), r(m, n).to(dtype).to(DEV), r(n).to(DEV)
+
+    def run():
+        out, kept = bd.projection(x, w, bias, act="gelu", residual=dy, pre=True)
+        grads = bd.projection_backward(dy, x, w, pre=pre, act="silu", db=True)
+        loss, lse = bd.head_loss(x, w, labels)
+        more = bd.head_loss_backward(dloss, x, w, labels, loss, lse)
+        return (out, kept, *grads, loss, lse, *more, *bd.head_select(x, w))
+    return run, (x, w)
+
+
+@pytest.mark.parametrize("size", [(9, 72, 300), (300, 200, 1100)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_repeats_streams_and_graphs_agree(dtype, size):
+    """The same bits on every call: again, on another stream, and in a captured graph that is
+    replayed several times with eager work of the program in between; changed inputs change
+    the replay."""
+    run, (x, w) = _all_calls(dtype, *size)
+    want = run()
+    torch.cuda.synchronize()
+    for a, b in zip(want, run()):
+        assert torch.equal(a, b)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = run()
+    s.synchronize()
+    for a, b in zip(want, other):
+        assert torch.equal(a, b)
+    with torch.cuda.stream(s):
+        run()
+    torch.cuda.synchronize()
+    graph, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    with torch.cuda.graph(second):
+        got2 = run()
+    for turn in range(4):
+        for t in (*got, *got2):
+            t.fill_(3)
+        graph.replay()
+        run()
+        torch.randn(1000, device=DEV).sum()
+        second.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(want, got, got2):
+            assert torch.equal(a, b) and torch.equal(a, c), turn
+    x.mul_(0.5)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(run(), got):
+        assert torch.equal(a, b)
+
+
+def test_given_stream_and_workspace():
+    import paper_2607_02805_amd as bd
+    r = gen(32)
+    x, w = r(100, 72).to(BF).to(DEV), (r(130, 72) / 8).to(BF).to(DEV)
+    want = bd.projection(x, w)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device=DEV)
+    got = bd.projection(x, w, stream=s, workspace=ws)
+    s.synchronize()
+    assert torch.equal(got, want)
+    got = bd.projection(x, w, stream=s)          # a workspace of its own, kept until the stream is done
+    s.synchronize()
+    assert torch.equal(got, want)
+    with pytest.raises(bd.BdlmError) as e:
+        bd.projection(x, w, workspace=ws[:256])
+    assert e.value.code == bd.E_WORKSPACE
+
+
+def test_canaries_around_the_workspace():
+    """A workspace of exactly the size asked for: nothing is written past it."""
+    import ctypes
+    import paper_2607_02805_amd as bd
+    for m, k, n in ((100, 72, 130), (300, 448, 1100)):
+        x, w, labels, dloss = head_inputs(m, k, n, F32, 33)
+        d, _ = bd._dense(x, w)
+        loss, lse = bd.head_loss(x, w, labels)
+        dy = torch.randn(m, n, device=DEV)
+        for name, call in (("projection", lambda ws: bd.projection(x, w, workspace=ws)),
+                           ("projection_backward", lambda ws: bd.projection_backward(dy, x, w, workspace=ws, db=True)),
+                           ("head_loss", lambda ws: bd.head_loss(x, w, labels, workspace=ws)),
+                           ("head_loss_backward",
+                            lambda ws: bd.head_loss_backward(dloss, x, w, labels, loss, lse, workspace=ws)),
+                           ("head_select", lambda ws: bd.head_select(x, w, workspace=ws))):
+            need = ctypes.c_int64(0)
+            assert getattr(bd.lib(), f"bdlm_{name}_workspace")(ctypes.byref(d), ctypes.byref(need)) == 0
+            buf = torch.full((need.value + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+            say("canary", name, m, need.value)
+            call(buf[:need.value])
+            torch.cuda.synchronize()
+            assert bool((buf[need.value:] == 0xA5).all())
