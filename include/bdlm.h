@@ -442,11 +442,12 @@ int bdlm_gated_rmsnorm(int64_t batch, int64_t len, int64_t nheads, int64_t ngrou
  * in_dtype with unit innermost stride and row strides x_stride, w_stride in elements (rows of x and
  * w may repeat or overlap; outputs' rows may not).  A row is a token: batch and block
  * dimensions are one axis.  bdlm_dense_desc_init fills contiguous strides.
- *   sizes      rows 0 .. 2^22, features 1 .. 2^22, any stride up to 2^40.
+ *   sizes      rows 0 .. 2^22, features 1 .. 2^22, any stride up to 2^40, and no product of more
+ *              than 2^23 - 1 tiles of 256 x 256 (BDLM_E_SHAPE).
  *   alignment  x, w, residual, pre, dy and the matrices written: base pointers 16-byte
- *              aligned (strides are free, and bf16 matrices whose strides and in_features are
- *              multiples of 8 are read as they lie; others are laid out anew in the
- *              workspace).
+ *              aligned (strides are free; bf16 matrices whose strides are multiples of 8 and
+ *              whose columns are a multiple of 64 are read as they lie, others are laid
+ *              out anew in the workspace).
  *   workspace  device memory, 256-byte aligned, of at least the size the query returns for
  *              the same descriptor; its contents are scratch.  Calls that share one must
  *              not run concurrently (captured graphs that share one neither).

@@ -135,6 +135,9 @@ struct PackArgs {
 };
 int launch_pack(const PackArgs &a, void *stream);
 constexpr int32_t kPackRows = 16;   // rows per workgroup
+#ifdef __HIPCC__
+__host__ __device__
+#endif
 inline int32_t pack_row_blocks(int32_t rows) { return (rows + 63) / 64 * (64 / kPackRows); }
 // out[c] = sum over the blocks of part[b][c]
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream);

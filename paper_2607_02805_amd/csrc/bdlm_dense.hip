@@ -76,50 +76,53 @@ template <bool GRAD, bool BF16, bool PRE16, int TERMS>
 __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
     __shared__ float sums[4][64 * 8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = (blockIdx.x * 64 + lane) * 8;
     const int64_t rows = a.rows_dev ? *a.rows_dev : a.rows, rows_up = (rows + 63) / 64 * 64;
-    const int64_t r0 = int64_t(blockIdx.y) * kPackRows;
-    const int n = a.cols - c;
     const bool slope = GRAD && a.act != BDLM_ACT_NONE;
-    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (c < a.ld_dst) {
-        for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += 4 * kPackBatch) {
-            Eight<BF16> v[kPackBatch];
-            Eight<PRE16> z[kPackBatch];
+    const int64_t across = (a.ld_dst + 511) / 512, blocks = across * pack_row_blocks(a.rows);
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const int64_t down = block / across;
+        const int c0 = static_cast<int>(block - down * across) * 512, c = c0 + lane * 8;
+        const int64_t r0 = down * kPackRows;
+        const int n = a.cols - c;
+        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (c < a.ld_dst) {
+            for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += 4 * kPackBatch) {
+                Eight<BF16> v[kPackBatch];
+                Eight<PRE16> z[kPackBatch];
 #pragma unroll
-            for (int k = 0; k < kPackBatch; ++k) {
-                const int64_t r = q + 4 * k;
-                const int64_t from = r >= rows ? 0 : a.row_of ? a.row_of[r] : r;
-                v[k].load(a.src, from * a.ld + c, r < rows ? n : 0);
-                if (slope) z[k].load(a.pre, from * a.ld_pre + c, r < rows ? n : 0);
-            }
-#pragma unroll
-            for (int k = 0; k < kPackBatch; ++k) {
-                const int64_t r = q + 4 * k;
-                float f[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = v[k].value(e);
-                if constexpr (GRAD) {
-                    if (slope) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) f[e] = r < rows && e < n ? f[e] * act_slope(z[k].value(e), a.act) : 0.f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] += f[e];
+                for (int k = 0; k < kPackBatch; ++k) {
+                    const int64_t r = q + 4 * k;
+                    const int64_t from = r >= rows ? 0 : a.row_of ? a.row_of[r] : r;
+                    v[k].load(a.src, from * a.ld + c, r < rows ? n : 0);
+                    if (slope) z[k].load(a.pre, from * a.ld_pre + c, r < rows ? n : 0);
                 }
-                if (a.dst && r < rows_up) store_terms<TERMS>(a.dst + r * a.ld_dst + c, a.plane, f);
+#pragma unroll
+                for (int k = 0; k < kPackBatch; ++k) {
+                    const int64_t r = q + 4 * k;
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] = v[k].value(e);
+                    if constexpr (GRAD) {
+                        if (slope) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[e] = r < rows && e < n ? f[e] * act_slope(z[k].value(e), a.act) : 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[e] += f[e];
+                    }
+                    if (a.dst && r < rows_up) store_terms<TERMS>(a.dst + r * a.ld_dst + c, a.plane, f);
+                }
             }
         }
-    }
-    if constexpr (GRAD) {
-        if (!a.colsum) return;
+        if constexpr (GRAD) {
+            if (!a.colsum) continue;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[wave][lane * 8 + e] = sum[e];
-        __syncthreads();
-        for (int x = threadIdx.x; x < 512; x += 256) {
-            const int col = blockIdx.x * 512 + x;
-            if (col < a.cols)
-                a.colsum[int64_t(blockIdx.y) * a.cols + col] = (sums[0][x] + sums[1][x]) + (sums[2][x] + sums[3][x]);
+            for (int e = 0; e < 8; ++e) sums[wave][lane * 8 + e] = sum[e];
+            __syncthreads();
+            for (int x = threadIdx.x; x < 512; x += 256)
+                if (c0 + x < a.cols)
+                    a.colsum[down * a.cols + c0 + x] = (sums[0][x] + sums[1][x]) + (sums[2][x] + sums[3][x]);
+            __syncthreads();
         }
     }
 }
@@ -247,7 +250,8 @@ int done() { return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH; }
 
 int launch_pack(const PackArgs &a, void *stream) {
     if (a.rows <= 0) return BDLM_OK;
-    const dim3 g(static_cast<unsigned>((a.ld_dst + 511) / 512), static_cast<unsigned>(pack_row_blocks(a.rows)));
+    const int64_t blocks = (a.ld_dst + 511) / 512 * pack_row_blocks(a.rows);
+    const dim3 g(static_cast<unsigned>(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const dim3 b(256);
     const bool grad = a.act != BDLM_ACT_NONE || a.colsum;

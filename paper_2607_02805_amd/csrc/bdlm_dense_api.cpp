@@ -82,21 +82,26 @@ int terms_of(int32_t dtype) { return dtype == BDLM_DTYPE_BF16 ? 1 : 3; }
 struct Shape {
     bool big;
     int32_t splits;
+    bool fits = true;   // in one launch (fewer than 2^32 threads)
 };
+bool launch_fits(bool big, int64_t tiles) { return tiles < (big ? int64_t(1) << 23 : int64_t(1) << 24); }
+// The tiles and splits of the least time: a step of a large tile takes 1.75 us (one workgroup on a
+// CU), of a small one 0.9 (two), and a tile about six steps more to begin and to end; partial
+// sums are written and read again at 4 TB/s, by a launch of their own.
 Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split) {
-    Shape best{false, 1};
+    Shape best{true, 1, false};
     double least = 1e300;
     for (int big = 0; big < 2; ++big) {
         const int64_t e = tile_edge(big), per = big ? 256 : 512;
         const int64_t tiles = ((nrow + e - 1) / e) * ((ncol + e - 1) / e);
-        for (int s = 1; s <= (may_split ? 16 : 1); ++s) {
-            if (s > 1 && steps / s < 4) break;
+        for (int s = 1; s <= (may_split ? kMostSplits : 1); ++s) {
+            if ((s > 1 && steps / s < 4) || !launch_fits(big, tiles * s)) break;
             const double rounds = double((tiles * s + per - 1) / per);
-            double us = rounds * ((double((steps + s - 1) / s) + 3.0) * (big ? 1.4 : 0.9));
+            double us = rounds * ((double((steps + s - 1) / s) + (big ? 5.0 : 4.0)) * (big ? 1.75 : tiles * s <= kChip ? 0.6 : 0.9));
             if (s > 1) us += 3.0 + double(s + 1) * nrow * ncol * 4.0 / 4.0e6;
             if (us < least) {
                 least = us;
-                best = Shape{big != 0, s};
+                best = Shape{big != 0, s, true};
             }
         }
     }
@@ -200,10 +205,11 @@ struct ProjectionPlan {
         : skinny(d.rows <= kSkinnyRows), ws(p),
           x(px, skinny ? 0 : d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
           w(pw, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
-        shape = skinny ? Shape{false, 1}
+        shape = skinny ? Shape{false, 1, true}
                        : shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), true);
         part = ws.take<float>(part_size(shape, d.rows, d.out_features));
     }
+    bool fits() const { return shape.fits; }
 };
 
 struct BackwardPlan {
@@ -225,6 +231,7 @@ struct BackwardPlan {
         part = ws.take<float>(std::max(part_size(sx, d.rows, d.in_features),
                                        part_size(sw, d.out_features, d.in_features)));
     }
+    bool fits() const { return sx.fits && sw.fits; }
 };
 
 // The rows that count of a masked loss.
@@ -268,6 +275,7 @@ struct SelectPlan {
           w(pw, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
           shape(shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), false)),
           rec(d.rows, d.out_features, skinny ? kSkinnyCols : tile_edge(shape.big), ws) {}
+    bool fits() const { return skinny || shape.fits; }
 };
 
 struct LossPlan {
@@ -282,6 +290,7 @@ struct LossPlan {
           w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
           shape(shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), false)),
           rec(d.rows, d.out_features, tile_edge(shape.big), ws), label_logit(ws.take<float>(d.rows)) {}
+    bool fits() const { return shape.fits; }
 };
 
 // The vocabulary goes in pieces whose logit gradients (rows x piece, bf16 terms) stay within 512 MB:
@@ -307,7 +316,7 @@ struct LossBackwardPlan {
         const int64_t n = (d.out_features + piece - 1) / piece;
         piece = up((d.out_features + n - 1) / n, 256);
         sp = shape_of(d.rows, piece, steps_of(d.in_features, pairs_of(d.in_dtype)), false);
-        sx = Shape{true, 0};
+        sx = Shape{true, 0, launch_fits(true, (d.rows + 255) / 256 * ((d.in_features + 255) / 256))};
         sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true);
         p = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * piece);
         // summed over the pieces: what the splits of any number of rows take
@@ -315,6 +324,7 @@ struct LossBackwardPlan {
         part_x = ws.take<float>(std::max(d.rows, std::min(d.rows * kMostSplits, kChip / std::min<int64_t>(cols, kChip) * e)) * d.in_features);
         part_w = ws.take<float>(part_size(sw, piece, d.in_features));
     }
+    bool fits() const { return sp.fits && sx.fits && sw.fits; }
 };
 
 template <class P>
@@ -327,9 +337,9 @@ int query(const bdlm_dense_desc_t *d, int64_t *bytes) {
 }
 template <class P>
 int check_workspace(const bdlm_dense_desc_t *d, const void *ws, int64_t bytes) {
-    int64_t need = 0;
-    const int rc = query<P>(d, &need);
-    if (rc != BDLM_OK) return rc;
+    const P plan(*d, nullptr, nullptr, nullptr);
+    if (!plan.fits()) return BDLM_E_SHAPE;
+    const int64_t need = plan.ws.used;
     if (need == 0) return BDLM_OK;
     if (!ws || bytes < need) return BDLM_E_WORKSPACE;
     return aligned(ws, 256) ? BDLM_OK : BDLM_E_ALIGN;

@@ -541,7 +541,6 @@ int launch_tile(const TileArgs &a, void *stream) {
     int64_t tiles = ((a.nrow + e - 1) / e) * ((a.ncol + e - 1) / e);
     // (splits 0: fewer rows make more splits, never more than the chip holds)
     tiles = a.splits ? tiles * a.splits : tiles > kChip ? tiles : kChip;
-    if (tiles > (int64_t(1) << 30)) return BDLM_E_SHAPE;
     const dim3 g(static_cast<unsigned>(tiles));
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t r = hipErrorInvalidValue;

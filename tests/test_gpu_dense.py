@@ -543,3 +543,66 @@ def test_canaries_around_the_workspace():
             call(buf[:need.value])
             torch.cuda.synchronize()
             assert bool((buf[need.value:] == 0xA5).all())
+
+
+# ------------------------------------------------------------------ marshalling
+def test_native_and_python_marshalling_agree(monkeypatch):
+    """Every call through the native module and with it left out: the same bits, the same refusals."""
+    import numpy as np
+    import paper_2607_02805_amd as bd
+
+    class Absent:
+        def __getattr__(self, name):
+            return lambda *a: NotImplemented
+
+    class Counting:
+        taken = 0
+
+        def __getattr__(self, name):
+            f = getattr(real, name)
+
+            def run(*a):
+                got = f(*a)
+                Counting.taken += got is not NotImplemented
+                return got
+            return run
+    real = bd._native()
+    x, w, labels, dloss = head_inputs(70, 72, 130, BF, 40)
+    r = gen(41)
+    dy, bias = r(70, 130).to(BF).to(DEV), r(130).to(DEV)
+    loss, lse = bd.head_loss(x, w, labels)
+    buf = torch.empty(70, 130, dtype=F32, device=DEV)
+    cases = {   # name: (call, whether the native module takes it)
+        "plain": (lambda: bd.projection(x, w), True),
+        "all": (lambda: bd.projection(x, w, bias, act="gelu", residual=dy, pre=True), True),
+        "out": (lambda: bd.projection(x, w, out=buf), True),
+        "3d": (lambda: bd.projection(x.view(7, 10, 72), w, act="none"), True),
+        "back": (lambda: bd.projection_backward(dy, x, w, pre=dy, act="silu", db=True), True),
+        "loss": (lambda: bd.head_loss(x, w, labels, exclude=3), True),
+        "grad": (lambda: bd.head_loss_backward(dloss, x, w, labels, loss, lse), True),
+        "select": (lambda: bd.head_select(x, w, exclude=129), True),
+        "stream": (lambda: bd.projection(x, w, stream=torch.cuda.current_stream()), False),
+        "rows": (lambda: bd.projection(x.view(7, 10, 72)[:, :4], w), False),
+        "half": (lambda: bd.projection(x.half(), w.half()), False),
+        "act": (lambda: bd.projection(x, w, act="tanh"), False),
+        "bias": (lambda: bd.projection(x, w, bias.double()), False),
+        "numpy": (lambda: bd.head_select(x, w, exclude=np.int64(5)), False),
+        "cpu": (lambda: bd.projection(x.cpu(), w.cpu()), False),
+        "bad": (lambda: bd.projection(x, w, out=x.new_empty(70, 131)[:, 1:]), True),
+        "labels": (lambda: bd.head_loss(x, w, labels.int()), False),
+    }
+    for name, (call, native) in cases.items():
+        got = []
+        for m in (Counting(), Absent()):
+            monkeypatch.setattr(bd, "_marshal", m)
+            Counting.taken = 0
+            try:
+                out = call()
+            except Exception as e:      # compared between the two sides
+                out = (type(e), str(e))
+            torch.cuda.synchronize()
+            got.append(out if isinstance(out, tuple) else (out,))
+            if isinstance(m, Counting):
+                assert Counting.taken == native, name
+        for a, b in zip(*got):
+            assert torch.equal(a, b) if torch.is_tensor(a) else a == b, (name, a, b)
