@@ -479,7 +479,7 @@ int bdlm_dense_desc_init(bdlm_dense_desc_t *desc, int64_t rows, int64_t in_featu
  * residual     device [rows][out_features], out_dtype, or NULL; may be out (same stride).
  * out          device [rows][out_features], out_dtype (BDLM_DTYPE_F32 or BDLM_DTYPE_BF16).
  * pre          device [rows][out_features], in_dtype, or NULL: kept for the gradient.
- * Up to 64 rows need no workspace.
+ * Up to 32 rows (fp32: 64) need no workspace.
  * Errors: BDLM_E_NULL, BDLM_E_SHAPE (also an unknown act), BDLM_E_DTYPE, BDLM_E_ALIGN,
  * BDLM_E_WORKSPACE, BDLM_E_LAUNCH.  rows == 0 enqueues nothing.
  */

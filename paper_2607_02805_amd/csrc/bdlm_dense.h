@@ -101,19 +101,24 @@ inline int32_t tile_edge(bool big) { return big ? 256 : 128; }
 int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
                 const StoreArgs &s, void *stream);
 
-// Few rows (at most 64): the weights stream through once.  x [nrow][k], w [ncol][k], both bf16
-// or both fp32, any stride; out kTileStore or kTileBest (one record per skinny_cols(nrow) columns).
+// Few rows (skinny_rows): the weights stream through once.  x [nrow][k], w [ncol][k], both bf16
+// or both fp32, any stride; out kTileStore or kTileBest (one record per skinny_cols columns).
 struct SkinnyArgs {
     const void *x, *w;
     int64_t ldx, ldw;
     int32_t nrow, ncol, k;
+    const int32_t *nrow_dev, *row_of;  // the rows that count: how many, and row r's row of x (null: all)
     int32_t bf16;
     int32_t out;
     StoreArgs store;
     BestArgs best;
 };
-constexpr int32_t kSkinnyRows = 64;
-constexpr int32_t kSkinnyCols = 32;
+// Above that many rows the tiles are faster: over 50,257 columns of 1,024 in bf16, 32 rows take 34
+// us here and 29 there, 64 rows 54 and 34; in fp32, where the tiles lay the weights out anew, 64
+// rows take 115 and 220.
+inline int32_t skinny_rows(bool bf16) { return bf16 ? 32 : 64; }
+// Columns of a workgroup: fewer where there are not two workgroups for every CU.
+inline int32_t skinny_cols(int64_t ncol) { return ncol >= 32 * 512 ? 32 : 16; }
 int launch_skinny(const SkinnyArgs &a, void *stream);
 
 // Copies an operand to bf16 terms: dst[p][r][0 .. ld_dst) from src rows (row_of: gathered),

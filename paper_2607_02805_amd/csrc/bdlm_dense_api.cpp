@@ -75,6 +75,10 @@ struct Space {
     }
 };
 
+// A call whose rows the weights stream past.
+bool few(const bdlm_dense_desc_t &d) { return d.rows <= skinny_rows(d.in_dtype == BDLM_DTYPE_BF16); }
+constexpr int64_t kFewRows = 64;   // whose gradients keep two terms
+
 int terms_of(int32_t dtype) { return dtype == BDLM_DTYPE_BF16 ? 1 : 3; }
 
 // Tiles of a product and how its contraction is split over workgroups.  steps: contraction
@@ -85,9 +89,11 @@ struct Shape {
     bool fits = true;   // in one launch (fewer than 2^32 threads)
 };
 bool launch_fits(bool big, int64_t tiles) { return tiles < (big ? int64_t(1) << 23 : int64_t(1) << 24); }
-// The tiles and splits of the least time: a step of a large tile takes 1.75 us (one workgroup on a
-// CU), of a small one 0.9 (two), and a tile about six steps more to begin and to end; partial
-// sums are written and read again at 4 TB/s, by a launch of their own.
+// The tiles and splits of the least time, as measured: a step of a large tile takes 1.85 us (one
+// workgroup on a CU), of a small one 1.15 (two), or 0.75 alone on its CU, and a tile five or four
+// steps more to begin and to end.  16,384 x 4,096 over 1,024 takes 148 us in large tiles and 200 in
+// small ones, 4,096 x 832 over 1,664 takes 45 and 22.  Partial sums are written and read again
+// at 4 TB/s, by a launch of their own.
 Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split) {
     Shape best{true, 1, false};
     double least = 1e300;
@@ -97,7 +103,7 @@ Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split) {
         for (int s = 1; s <= (may_split ? kMostSplits : 1); ++s) {
             if ((s > 1 && steps / s < 4) || !launch_fits(big, tiles * s)) break;
             const double rounds = double((tiles * s + per - 1) / per);
-            double us = rounds * ((double((steps + s - 1) / s) + (big ? 5.0 : 4.0)) * (big ? 1.75 : tiles * s <= kChip ? 0.6 : 0.9));
+            double us = rounds * ((double((steps + s - 1) / s) + (big ? 5.0 : 4.0)) * (big ? 1.85 : tiles * s <= kChip ? 0.75 : 1.15));
             if (s > 1) us += 3.0 + double(s + 1) * nrow * ncol * 4.0 / 4.0e6;
             if (us < least) {
                 least = us;
@@ -166,7 +172,7 @@ TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, int64_t
 // rounded to bf16, as the activations of the forward products are; of few rows, where an
 // output's errors do not average out and the weights' bytes bound the products, two terms are kept.
 int grad_terms(const bdlm_dense_desc_t &d) {
-    return d.in_dtype != BDLM_DTYPE_BF16 ? 3 : d.rows <= kSkinnyRows ? 2 : 1;
+    return d.in_dtype != BDLM_DTYPE_BF16 ? 3 : d.rows <= kFewRows ? 2 : 1;
 }
 int32_t grad_pairs(int terms) { return terms == 3 ? 6 : terms; }
 int32_t pairs_of(int32_t dtype) { return dtype == BDLM_DTYPE_BF16 ? 1 : 6; }
@@ -202,7 +208,7 @@ struct ProjectionPlan {
     Shape shape;
     float *part;
     ProjectionPlan(const bdlm_dense_desc_t &d, const void *px, const void *pw, void *p)
-        : skinny(d.rows <= kSkinnyRows), ws(p),
+        : skinny(few(d)), ws(p),
           x(px, skinny ? 0 : d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
           w(pw, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
         shape = skinny ? Shape{false, 1, true}
@@ -263,6 +269,20 @@ struct Records {
     }
 };
 
+SkinnyArgs few_rows(const bdlm_dense_desc_t &d, const void *x, const void *w, int32_t out) {
+    SkinnyArgs a{};
+    a.x = x;
+    a.w = w;
+    a.ldx = d.x_stride;
+    a.ldw = d.w_stride;
+    a.nrow = static_cast<int32_t>(d.rows);
+    a.ncol = static_cast<int32_t>(d.out_features);
+    a.k = static_cast<int32_t>(d.in_features);
+    a.bf16 = d.in_dtype == BDLM_DTYPE_BF16;
+    a.out = out;
+    return a;
+}
+
 struct SelectPlan {
     bool skinny;
     Space ws;
@@ -270,15 +290,16 @@ struct SelectPlan {
     Shape shape;
     Records rec;
     SelectPlan(const bdlm_dense_desc_t &d, const void *px, const void *pw, void *p)
-        : skinny(d.rows <= kSkinnyRows), ws(p),
+        : skinny(few(d)), ws(p),
           x(px, skinny ? 0 : d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
           w(pw, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
           shape(shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), false)),
-          rec(d.rows, d.out_features, skinny ? kSkinnyCols : tile_edge(shape.big), ws) {}
+          rec(d.rows, d.out_features, skinny ? skinny_cols(d.out_features) : tile_edge(shape.big), ws) {}
     bool fits() const { return skinny || shape.fits; }
 };
 
 struct LossPlan {
+    bool skinny;
     Space ws;
     Rows rows;
     Operand x, w;
@@ -286,11 +307,13 @@ struct LossPlan {
     Records rec;
     float *label_logit;
     LossPlan(const bdlm_dense_desc_t &d, const void *px, const void *pw, void *p)
-        : ws(p), rows(d.rows, false, ws), x(px, d.rows, d.in_features, d.x_stride, d.in_dtype, true, ws),
-          w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
+        : skinny(few(d)), ws(p), rows(d.rows, false, ws),
+          x(px, skinny ? 0 : d.rows, d.in_features, d.x_stride, d.in_dtype, true, ws),
+          w(pw, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
           shape(shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), false)),
-          rec(d.rows, d.out_features, tile_edge(shape.big), ws), label_logit(ws.take<float>(d.rows)) {}
-    bool fits() const { return shape.fits; }
+          rec(d.rows, d.out_features, skinny ? skinny_cols(d.out_features) : tile_edge(shape.big), ws),
+          label_logit(ws.take<float>(d.rows)) {}
+    bool fits() const { return skinny || shape.fits; }
 };
 
 // The vocabulary goes in pieces whose logit gradients (rows x piece, bf16 terms) stay within 512 MB:
@@ -316,11 +339,13 @@ struct LossBackwardPlan {
         const int64_t n = (d.out_features + piece - 1) / piece;
         piece = up((d.out_features + n - 1) / n, 256);
         sp = shape_of(d.rows, piece, steps_of(d.in_features, pairs_of(d.in_dtype)), false);
-        sx = Shape{true, 0, launch_fits(true, (d.rows + 255) / 256 * ((d.in_features + 255) / 256))};
+        // (few rows: the small tile, half of which they would leave empty in the large one)
+        const bool big = d.rows > tile_edge(false);
+        const int64_t e = tile_edge(big), cols = (d.in_features + e - 1) / e;
+        sx = Shape{big, 0, launch_fits(big, (d.rows + e - 1) / e * cols)};
         sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true);
         p = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * piece);
         // summed over the pieces: what the splits of any number of rows take
-        const int64_t e = tile_edge(true), cols = (d.in_features + e - 1) / e;
         part_x = ws.take<float>(std::max(d.rows, std::min(d.rows * kMostSplits, kChip / std::min<int64_t>(cols, kChip) * e)) * d.in_features);
         part_w = ws.take<float>(part_size(sw, piece, d.in_features));
     }
@@ -442,16 +467,7 @@ int bdlm_projection(const bdlm_dense_desc_t *d, int32_t act, int32_t out_dtype, 
     s.pre_bf16 = d->in_dtype == BDLM_DTYPE_BF16;
     s.act = act;
     if (p.skinny) {
-        SkinnyArgs a{};
-        a.x = x;
-        a.w = w;
-        a.ldx = d->x_stride;
-        a.ldw = d->w_stride;
-        a.nrow = static_cast<int32_t>(d->rows);
-        a.ncol = static_cast<int32_t>(d->out_features);
-        a.k = static_cast<int32_t>(d->in_features);
-        a.bf16 = d->in_dtype == BDLM_DTYPE_BF16;
-        a.out = kTileStore;
+        SkinnyArgs a = few_rows(*d, x, w, kTileStore);
         a.store = s;
         return launch_skinny(a, stream);
     }
@@ -561,14 +577,23 @@ int bdlm_head_loss(const bdlm_dense_desc_t *d, const int64_t *labels, int64_t ex
     TRY(launch_rows(RowsArgs{labels, rows, vocab, exclude, p.rows.count, p.rows.row_of, p.rows.label, nullptr,
                              nullptr, nullptr, nullptr, nullptr, nullptr},
                     stream));
-    TRY(p.x.lay(stream, p.rows.row_of, p.rows.count));
-    TRY(p.w.lay(stream));
-    TileArgs a = product(p.x.mat, false, p.w.mat, false, d->rows, vocab, d->in_features, pairs_of(d->in_dtype),
-                         p.shape);
-    a.nrow_dev = p.rows.count;
-    a.out = kTileBest;
-    a.best = BestArgs{p.rec.top, p.rec.others, p.rec.at, p.label_logit, p.rows.label, p.rec.ntile, none};
-    TRY(launch_tile(a, stream));
+    const BestArgs best{p.rec.top, p.rec.others, p.rec.at, p.label_logit, p.rows.label, p.rec.ntile, none};
+    if (p.skinny) {
+        SkinnyArgs a = few_rows(*d, x, w, kTileBest);
+        a.nrow_dev = p.rows.count;
+        a.row_of = p.rows.row_of;
+        a.best = best;
+        TRY(launch_skinny(a, stream));
+    } else {
+        TRY(p.x.lay(stream, p.rows.row_of, p.rows.count));
+        TRY(p.w.lay(stream));
+        TileArgs a = product(p.x.mat, false, p.w.mat, false, d->rows, vocab, d->in_features, pairs_of(d->in_dtype),
+                             p.shape);
+        a.nrow_dev = p.rows.count;
+        a.out = kTileBest;
+        a.best = best;
+        TRY(launch_tile(a, stream));
+    }
     return launch_finish(FinishArgs{p.rec.top, p.rec.others, p.rec.at, p.rec.ntile, rows, vocab, none, p.rows.count,
                                     p.rows.row_of, labels, p.label_logit, loss, lse, nullptr, nullptr},
                          stream);
@@ -638,7 +663,7 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
     if (dx) {
         StoreArgs s = plain_store(dx, dx_stride, d->in_dtype);
         s.row_of = p.rows.row_of;
-        TRY(launch_join(p.part_x, 0, 1, rows, static_cast<int32_t>(K), p.rows.count, s, stream));
+        TRY(launch_join(p.part_x, 0, p.sx.big, rows, static_cast<int32_t>(K), p.rows.count, s, stream));
         TRY(launch_zero_rows(labels, exclude, vocab, rows, dx, dx_stride, static_cast<int32_t>(K),
                              d->in_dtype == BDLM_DTYPE_BF16, stream));
     }
@@ -665,16 +690,7 @@ int bdlm_head_select(const bdlm_dense_desc_t *d, int64_t exclude, const void *x,
     const int32_t rows = static_cast<int32_t>(d->rows), vocab = static_cast<int32_t>(d->out_features);
     const BestArgs best{p.rec.top, p.rec.others, p.rec.at, nullptr, nullptr, p.rec.ntile, token_or_none(d, exclude)};
     if (p.skinny) {
-        SkinnyArgs a{};
-        a.x = x;
-        a.w = w;
-        a.ldx = d->x_stride;
-        a.ldw = d->w_stride;
-        a.nrow = rows;
-        a.ncol = vocab;
-        a.k = static_cast<int32_t>(d->in_features);
-        a.bf16 = d->in_dtype == BDLM_DTYPE_BF16;
-        a.out = kTileBest;
+        SkinnyArgs a = few_rows(*d, x, w, kTileBest);
         a.best = best;
         TRY(launch_skinny(a, stream));
     } else {

@@ -2,8 +2,8 @@
 // matrix: out[row][col] = sum over k of x[row][k] * w[col][k], at most 64 rows.
 //
 // Bound by the weights' bytes: every weight is read once, straight into the registers that the
-// matrix instructions take it from.  A workgroup owns 32 columns; its waves share out the
-// contraction in runs of 128 indices, so that a wave has 16 loads of 16 bytes a lane in flight
+// matrix instructions take it from.  A workgroup owns 16 or 32 columns; its waves share out the
+// contraction in runs of 128 indices, so that a wave has 4 or 8 loads of 16 bytes a lane in flight
 // and four lanes read 256 contiguous bytes of a weight row.  x is small and comes from the caches.
 // The waves' partial tiles meet in LDS, in a fixed order.
 //
@@ -22,7 +22,6 @@ namespace {
 
 constexpr int kRun = 128;    // contraction indices of a wave's turn
 constexpr int kSteps = kRun / 32;
-constexpr int kGroups = kSkinnyCols / 16;
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_a4;
@@ -79,46 +78,50 @@ __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// MT: tiles of 16 rows.  Lane: weight column (lane & 15) of a group, or row (lane & 15) of x.
-template <int MT, bool BF16, int OUT>
-__global__ void __launch_bounds__(512) bdlm_skinny_kernel(const SkinnyArgs a) {
+// MT: tiles of 16 rows; G: groups of 16 columns.  Lane: weight column (lane & 15) of a group, or row (lane & 15) of x.
+template <int MT, int G, bool BF16, int OUT>
+__global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const SkinnyArgs a) {
+    constexpr int kCols = 16 * G;
     constexpr int TERMS = BF16 ? 1 : 3;
-    constexpr int kPitch = kSkinnyCols + 4;                // floats of a row of sums
+    constexpr int kPitch = kCols + 4;                // floats of a row of sums
     extern __shared__ float part[];                        // [waves][16 MT][kPitch]
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
     const int s = lane & 15, kg = lane >> 4;
-    const int col0 = blockIdx.x * kSkinnyCols;
+    const int col0 = blockIdx.x * kCols;
     const int esz = BF16 ? 2 : 4;
-    const char *wrow[kGroups], *xrow[MT];
+    const int nrow = a.nrow_dev ? *a.nrow_dev : a.nrow;
+    if (nrow <= 0) return;
+    const char *wrow[G], *xrow[MT];
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
+    for (int g = 0; g < G; ++g) {
         const int c = col0 + 16 * g + s;
         wrow[g] = static_cast<const char *>(a.w) + int64_t(c < a.ncol ? c : a.ncol - 1) * a.ldw * esz;
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         const int r = 16 * m + s;
-        xrow[m] = static_cast<const char *>(a.x) + int64_t(r < a.nrow ? r : a.nrow - 1) * a.ldx * esz;
+        const int rr = r < nrow ? r : nrow - 1;
+        xrow[m] = static_cast<const char *>(a.x) + int64_t(a.row_of ? a.row_of[rr] : rr) * a.ldx * esz;
     }
-    f32x4 acc[kGroups][MT];
+    f32x4 acc[G][MT];
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[g][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     auto run = [&](int k0, bool whole) {
-        Piece<BF16> w[kGroups][kSteps];
+        Piece<BF16> w[G][kSteps];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g)
+        for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int u = 0; u < kSteps; ++u) w[g][u].load(wrow[g], k0 + 32 * u + 8 * kg, a.k, whole);
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
-            bf16x8 wt[kGroups][TERMS];
+            bf16x8 wt[G][TERMS];
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) w[g][u].terms(wt[g]);
+            for (int g = 0; g < G; ++g) w[g][u].terms(wt[g]);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 Piece<BF16> x;
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(512) bdlm_skinny_kernel(const SkinnyArgs a) {
                 bf16x8 xt[TERMS];
                 x.terms(xt);
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g)
+                for (int g = 0; g < G; ++g)
 #pragma unroll
                     for (int i = 0; i < TERMS; ++i)
 #pragma unroll
@@ -141,22 +144,22 @@ __global__ void __launch_bounds__(512) bdlm_skinny_kernel(const SkinnyArgs a) {
 
     // lane: row 16 m + s, columns 16 g + 4 kg .. + 3
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g)
+    for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int m = 0; m < MT; ++m)
             *reinterpret_cast<f32x4 *>(part + (wave * 16 * MT + 16 * m + s) * kPitch + 16 * g + 4 * kg) = acc[g][m];
     __syncthreads();
-    constexpr int kQuads = kSkinnyCols / 4;
+    constexpr int kQuads = kCols / 4;
     for (int x = threadIdx.x; x < 16 * MT * kQuads; x += blockDim.x) {
         const int r = x / kQuads, c = x % kQuads * 4;
         f32x4 v = *reinterpret_cast<const f32x4 *>(part + r * kPitch + c);
         for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const f32x4 *>(part + (w * 16 * MT + r) * kPitch + c);
         if constexpr (OUT == kTileStore) {
-            if (r < a.nrow) store4(a.store, v, load_bias(a.store, col0 + c, a.ncol), r, col0 + c, a.ncol);
+            if (r < nrow) store4(a.store, v, load_bias(a.store, col0 + c, a.ncol), r, col0 + c, a.ncol);
         } else {
             // eight consecutive lanes hold a row's 32 columns
             const BestArgs &b = a.best;
-            const int label = b.label && r < a.nrow ? b.label[r] : -1;
+            const int label = b.label && r < nrow ? b.label[r] : -1;
             Best m{-INFINITY, 0.f, kNoColumn};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -177,7 +180,7 @@ __global__ void __launch_bounds__(512) bdlm_skinny_kernel(const SkinnyArgs a) {
                 if (col0 + c + e != m.at) sum += share(v[e], m.top);
 #pragma unroll
             for (int d = 1; d < kQuads; d *= 2) sum += __shfl_xor(sum, d, 64);
-            if (c == 0 && r < a.nrow) {
+            if (c == 0 && r < nrow) {
                 const int64_t o = int64_t(r) * b.ntile + blockIdx.x;
                 b.top[o] = m.top;
                 b.others[o] = sum;
@@ -187,17 +190,22 @@ __global__ void __launch_bounds__(512) bdlm_skinny_kernel(const SkinnyArgs a) {
     }
 }
 
-template <int MT, bool BF16>
-hipError_t launch_rows_of(const SkinnyArgs &a, hipStream_t s) {
+template <int MT, int G, bool BF16>
+hipError_t launch_cols_of(const SkinnyArgs &a, hipStream_t s) {
     // a run for every wave, as far as the workgroup goes
     int waves = (a.k + kRun - 1) / kRun;
-    const int most = MT >= 4 ? 4 : 8;   // LDS for the partial tiles
+    constexpr int kMost = BF16 ? 16 : 8, kRoom = 32 / (MT * G);   // registers; LDS
+    constexpr int most = kMost < kRoom ? kMost : kRoom;
     waves = waves < 1 ? 1 : waves > most ? most : waves;
-    const dim3 g((a.ncol + kSkinnyCols - 1) / kSkinnyCols), blk(64 * waves);
-    const size_t lds = size_t(waves) * 16 * MT * (kSkinnyCols + 4) * 4;
-    if (a.out == kTileStore) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, BF16, kTileStore>), g, blk, lds, s, a);
-    else hipLaunchKernelGGL((bdlm_skinny_kernel<MT, BF16, kTileBest>), g, blk, lds, s, a);
+    const dim3 g((a.ncol + 16 * G - 1) / (16 * G)), blk(64 * waves);
+    const size_t lds = size_t(waves) * 16 * MT * (16 * G + 4) * 4;   // at most 40 KB
+    if (a.out == kTileStore) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileStore>), g, blk, lds, s, a);
+    else hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileBest>), g, blk, lds, s, a);
     return hipGetLastError();
+}
+template <int MT, bool BF16>
+hipError_t launch_rows_of(const SkinnyArgs &a, hipStream_t s) {
+    return skinny_cols(a.ncol) == 32 ? launch_cols_of<MT, 2, BF16>(a, s) : launch_cols_of<MT, 1, BF16>(a, s);
 }
 
 }  // namespace
@@ -206,9 +214,7 @@ int launch_skinny(const SkinnyArgs &a, void *stream) {
     if (a.nrow <= 0 || a.ncol <= 0) return BDLM_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t r;
-    if (a.bf16)
-        r = a.nrow <= 16 ? launch_rows_of<1, true>(a, s) : a.nrow <= 32 ? launch_rows_of<2, true>(a, s)
-                                                                       : launch_rows_of<4, true>(a, s);
+    if (a.bf16) r = a.nrow <= 16 ? launch_rows_of<1, true>(a, s) : launch_rows_of<2, true>(a, s);
     else
         r = a.nrow <= 16 ? launch_rows_of<1, false>(a, s) : a.nrow <= 32 ? launch_rows_of<2, false>(a, s)
                                                                         : launch_rows_of<4, false>(a, s);

@@ -117,8 +117,10 @@ def test_projection_arguments():
     assert projection(wide, out=X + 264 * 2, ldo=400, res=None, pre=None) == bd.OK
     # few rows need no workspace
     need = ctypes.c_int64(-1)
-    assert bd.lib().bdlm_projection_workspace(ctypes.byref(desc(rows=64)), ctypes.byref(need)) == 0
-    assert need.value == 0 and projection(desc(rows=64), ws=None, size=0) == bd.OK
+    assert bd.lib().bdlm_projection_workspace(ctypes.byref(desc(rows=32)), ctypes.byref(need)) == 0
+    assert need.value == 0 and projection(desc(rows=32), ws=None, size=0) == bd.OK
+    fp32 = desc(rows=64, dtype=bd.DTYPE_F32)
+    assert bd.lib().bdlm_projection_workspace(ctypes.byref(fp32), ctypes.byref(need)) == 0 and need.value == 0
 
 
 def test_backward_arguments():

@@ -30,7 +30,7 @@ def near(got, want, what):
 
 # rows, in, out: one token to several tiles, odd sizes, both sides of every size rule
 SIZES = [(1, 64, 32), (1, 1, 1), (3, 129, 65), (16, 256, 96), (17, 100, 33), (33, 1024, 50), (64, 384, 130),
-         (65, 64, 64), (70, 7, 9), (128, 64, 128), (129, 200, 257), (300, 129, 515), (513, 448, 130)]
+         (65, 64, 64), (32, 2100, 16500), (2, 4100, 48), (70, 7, 9), (128, 64, 128), (129, 200, 257), (300, 129, 515), (513, 448, 130)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
