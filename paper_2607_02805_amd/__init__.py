@@ -869,8 +869,15 @@ def _vector(t, shape, dtype, device, what: str):
     return t
 
 
-def _dense_call(name: str, d, device, workspace, stream, args):
-    """One call of a dense operator on ``device``: its workspace and stream, then the C call."""
+def _on(stream, x):
+    """``stream`` made the current one: a call's outputs and workspace are allocated where they are used."""
+    if stream.device != x.device:
+        raise ValueError(f"stream must be one of {x.device}")
+    return _torch().cuda.stream(stream)
+
+
+def _dense_call(name: str, d, device, workspace, args):
+    """One call of a dense operator on ``device``'s current stream, with its workspace."""
     torch = _torch()
     if device.type != "cuda":
         raise ValueError("x must be a GPU tensor (no CPU path exists)")
@@ -882,12 +889,8 @@ def _dense_call(name: str, d, device, workspace, stream, args):
         elif workspace.device != device or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous tensor on {device}")
         size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-        s = torch.cuda.current_stream(device) if stream is None else stream
-        if s.device != device:
-            raise ValueError(f"stream must be one of {device}")
-        if stream is not None and workspace is not None:
-            workspace.record_stream(s)
-        rc = fn(ctypes.byref(d), *args, workspace.data_ptr() if size else None, size, s.cuda_stream)
+        rc = fn(ctypes.byref(d), *args, workspace.data_ptr() if size else None, size,
+                torch.cuda.current_stream(device).cuda_stream)
     if rc != OK:
         raise BdlmError(rc, "bdlm_" + name)
 
@@ -906,6 +909,9 @@ def projection(x, w, bias=None, act=None, residual=None, out=None, pre=None, str
     [..., out_features].  ``pre`` keeps x w^T + bias in x's dtype for the gradient: None (no),
     True (allocate) or a tensor.  Returns out, or (out, pre) if ``pre`` was asked for.
     """
+    if stream is not None:
+        with _on(stream, x):
+            return projection(x, w, bias, act, residual, out, pre, workspace=workspace)
     got = _native().projection(x, w, bias, act, residual, out, pre, stream, workspace)
     if got is not NotImplemented:
         return _answer(got, "bdlm_projection")
@@ -929,7 +935,7 @@ def projection(x, w, bias=None, act=None, residual=None, out=None, pre=None, str
     if pre is not None:
         pre = _place(pre, shape, x.dtype, x.device, "pre")
         _, ldp = _rows2d(pre, d.out_features, "pre", lead)
-    _dense_call("projection", d, x.device, workspace, stream,
+    _dense_call("projection", d, x.device, workspace,
                 (code, odt, _p(x), _p(w), _p(bias), _p(residual), ldr, _p(out), ldo, _p(pre), ldp))
     return out if pre is None else (out, pre)
 
@@ -943,6 +949,9 @@ def projection_backward(dy, x, w, pre=None, act=None, dx=True, dw=True, db=None,
     (allocate), None (not wanted) or a tensor; dx and dw have x's dtype, db is float32.
     The residual's gradient is dy.
     """
+    if stream is not None:
+        with _on(stream, x):
+            return projection_backward(dy, x, w, pre, act, dx, dw, db, workspace=workspace)
     got = _native().projection_backward(dy, x, w, pre, act, dx, dw, db, stream, workspace)
     if got is not NotImplemented:
         return _answer(got, "bdlm_projection_backward")
@@ -972,7 +981,7 @@ def projection_backward(dy, x, w, pre=None, act=None, dx=True, dw=True, db=None,
     if db is not None:
         db = _vector(_place(db, (d.out_features,), torch.float32, x.device, "db"), (d.out_features,),
                      torch.float32, x.device, "db")
-    _dense_call("projection_backward", d, x.device, workspace, stream,
+    _dense_call("projection_backward", d, x.device, workspace,
                 (code, ydt, _p(dy), ldy, _p(x), _p(w), _p(pre), ldp, _p(dx), ldx, _p(dw), ldw, _p(db)))
     return dx, dw, db
 
@@ -985,6 +994,9 @@ def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, worksp
     ``labels`` int64.  A row whose label is not a token that the softmax ranges over (negative, past
     the vocabulary, or ``exclude``) is left out: its loss and lse are 0.  The logits are never
     in memory."""
+    if stream is not None:
+        with _on(stream, x):
+            return head_loss(x, w, labels, exclude, loss, lse, workspace=workspace)
     got = _native().head_loss(x, w, labels, exclude, loss, lse, stream, workspace)
     if got is not NotImplemented:
         return _answer(got, "bdlm_head_loss")
@@ -993,7 +1005,7 @@ def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, worksp
     _vector(labels, lead, torch.int64, x.device, "labels")
     loss = _vector(_place(loss, lead, torch.float32, x.device, "loss"), lead, torch.float32, x.device, "loss")
     lse = _vector(_place(lse, lead, torch.float32, x.device, "lse"), lead, torch.float32, x.device, "lse")
-    _dense_call("head_loss", d, x.device, workspace, stream,
+    _dense_call("head_loss", d, x.device, workspace,
                 (_p(labels), int(exclude), _p(x), _p(w), _p(loss), _p(lse)))
     return loss, lse
 
@@ -1005,6 +1017,9 @@ def head_loss_backward(dloss, x, w, labels, loss, lse, exclude=-1, dx=True, dw=T
     ``dloss`` float32 is the gradient of the result by each row's loss (the weights of the block
     objective); ``loss`` and ``lse`` are what :func:`head_loss` returned for the same x, w,
     labels and exclude.  ``dx``, ``dw``: True (allocate), None (not wanted) or a tensor."""
+    if stream is not None:
+        with _on(stream, x):
+            return head_loss_backward(dloss, x, w, labels, loss, lse, exclude, dx, dw, workspace=workspace)
     got = _native().head_loss_backward(dloss, x, w, labels, loss, lse, exclude, dx, dw, stream,
                                        workspace)
     if got is not NotImplemented:
@@ -1021,7 +1036,7 @@ def head_loss_backward(dloss, x, w, labels, loss, lse, exclude=-1, dx=True, dw=T
     if dw is not None:
         dw = _place(dw, w.shape, w.dtype, x.device, "dw")
         _, ldw = _rows2d(dw, d.in_features, "dw")
-    _dense_call("head_loss_backward", d, x.device, workspace, stream,
+    _dense_call("head_loss_backward", d, x.device, workspace,
                 (_p(labels), int(exclude), _p(x), _p(w), _p(loss), _p(lse), _p(dloss), _p(dx), ldx, _p(dw), ldw))
     return dx, dw
 
@@ -1030,6 +1045,9 @@ def head_select(x, w, exclude=-1, token=None, logprob=None, stream=None, workspa
     """The head of a denoising step: (token, logprob) for hidden states x [..., in_features] and the
     vocabulary's weights w [tokens, in_features]: the most probable token (int64; the lowest of
     equals) but ``exclude``, and the log of its probability (float32)."""
+    if stream is not None:
+        with _on(stream, x):
+            return head_select(x, w, exclude, token, logprob, workspace=workspace)
     got = _native().head_select(x, w, exclude, token, logprob, stream, workspace)
     if got is not NotImplemented:
         return _answer(got, "bdlm_head_select")
@@ -1038,7 +1056,7 @@ def head_select(x, w, exclude=-1, token=None, logprob=None, stream=None, workspa
     token = _vector(_place(token, lead, torch.int64, x.device, "token"), lead, torch.int64, x.device, "token")
     logprob = _vector(_place(logprob, lead, torch.float32, x.device, "logprob"), lead, torch.float32, x.device,
                       "logprob")
-    _dense_call("head_select", d, x.device, workspace, stream,
+    _dense_call("head_select", d, x.device, workspace,
                 (int(exclude), _p(x), _p(w), _p(token), _p(logprob)))
     return token, logprob
 

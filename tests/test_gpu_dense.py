@@ -513,9 +513,16 @@ def test_given_stream_and_workspace():
     got = bd.projection(x, w, stream=s, workspace=ws)
     s.synchronize()
     assert torch.equal(got, want)
-    got = bd.projection(x, w, stream=s)          # a workspace of its own, kept until the stream is done
+    for _ in range(3):                           # outputs and workspace from the stream's own memory
+        got = bd.projection(x, w, stream=s)
+        torch.empty(got.numel(), dtype=got.dtype, device=DEV).fill_(9)
     s.synchronize()
     assert torch.equal(got, want)
+    one = bd.projection(x[0], w)                 # a single row without a leading dimension
+    token, logprob = bd.head_select(x[0], w)
+    loss, lse = bd.head_loss(x[0], w, token)
+    assert one.shape == (130,) and token.shape == loss.shape == () and torch.equal(loss, -logprob)
+    near(one, du.projection64(x[:1], w)[0], "one")
     with pytest.raises(bd.BdlmError) as e:
         bd.projection(x, w, workspace=ws[:256])
     assert e.value.code == bd.E_WORKSPACE
@@ -581,7 +588,7 @@ def test_native_and_python_marshalling_agree(monkeypatch):
         "loss": (lambda: bd.head_loss(x, w, labels, exclude=3), True),
         "grad": (lambda: bd.head_loss_backward(dloss, x, w, labels, loss, lse), True),
         "select": (lambda: bd.head_select(x, w, exclude=129), True),
-        "stream": (lambda: bd.projection(x, w, stream=torch.cuda.current_stream()), False),
+        "stream": (lambda: bd.projection(x, w, stream=torch.cuda.current_stream()), True),
         "rows": (lambda: bd.projection(x.view(7, 10, 72)[:, :4], w), False),
         "half": (lambda: bd.projection(x.half(), w.half()), False),
         "act": (lambda: bd.projection(x, w, act="tanh"), False),
