@@ -454,7 +454,8 @@ int bdlm_gated_rmsnorm(int64_t batch, int64_t len, int64_t nheads, int64_t ngrou
  *   overlap    no output or workspace overlaps another argument (BDLM_E_SHAPE, BDLM_E_WORKSPACE),
  *              except that a projection's out may be its residual.
  * Products accumulate in fp32; fp32 operands are multiplied as three bf16 terms each
- * (24 bits), so an infinity in one of them may come out as NaN.  Results do not depend on
+ * (24 bits), so an infinity in one of them, or in an operand of a gradient, may come out as NaN.
+ * Results do not depend on
  * timing: sums are taken in a fixed order.
  */
 typedef struct bdlm_dense_desc {
@@ -515,7 +516,8 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t
  *              a masked diffusion model sets to zero); negative or past the vocabulary: none.
  * labels       device int64 [rows].  A row whose label is not a token that the softmax
  *              ranges over (negative, past the vocabulary, or exclude) is left out: its loss,
- *              lse and gradients are 0, and its logits are not computed.
+ *              lse and gradients are 0, and its logits are not computed.  Neither such a
+ *              row of x nor w's row of `exclude` has a part in any result, NaN or not.
  * loss, lse    device fp32 [rows].
  * The backward takes dloss, the gradient of the result by each row's loss (the block
  * objective's weights), and the forward call's loss and lse:

@@ -72,6 +72,8 @@ struct TileArgs {
     const int32_t *nrow_dev, *k_dev;   // the count in device memory, at most nrow / k (null: nrow / k)
     int32_t npair;                     // pairs of planes: 1, 2 (two terms of row) or 6 (three of each)
     int32_t row_t, col_t;
+    int32_t skip;                      // a contraction index at which col is not read, below k - 1 (col_t;
+                                       // row holds zeros there), or -1
     int32_t big;                       // 1: 256 x 256 tiles, 0: 128 x 128
     int32_t splits;                    // > 1: kTilePartial only; 0: as many as fill the chip with
                                        // the rows that count (split_count)
@@ -121,8 +123,8 @@ inline int32_t skinny_rows(bool bf16) { return bf16 ? 32 : 64; }
 inline int32_t skinny_cols(int64_t ncol) { return ncol >= 32 * 512 ? 32 : 16; }
 int launch_skinny(const SkinnyArgs &a, void *stream);
 
-// Copies an operand to bf16 terms: dst[p][r][0 .. ld_dst) from src rows (row_of: gathered),
-// X
+// Copies an operand to bf16 terms: dst[p][r][0 .. ld_dst) from row r of src (row_of: row row_of[r]),
+// zeros past its columns, and rows of zeros up to a multiple of 64.
 struct PackArgs {
     const void *src;
     int64_t ld;

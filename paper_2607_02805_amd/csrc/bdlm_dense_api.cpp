@@ -164,6 +164,7 @@ TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, int64_t
     a.npair = npair;
     a.row_t = row_t;
     a.col_t = col_t;
+    a.skip = -1;
     a.big = s.big;
     a.splits = s.splits;
     return a;
@@ -645,7 +646,10 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
                           static_cast<int32_t>(v0), static_cast<int32_t>(up(n, 64))};
         TRY(launch_tile(a, stream));
         if (dx) {
-            TileArgs b = product(pm, false, w_at, true, rows, K, n, np, p.sx);
+            // w's row of the excluded token is not read: whatever it holds, it has no part in dx
+            const int64_t x = none >= v0 && none < v0 + n ? none - v0 : -1;
+            TileArgs b = product(pm, false, w_at, true, rows, K, x == n - 1 ? n - 1 : n, np, p.sx);
+            b.skip = static_cast<int32_t>(x == n - 1 ? -1 : x);
             b.nrow_dev = p.rows.count;
             b.out = kTilePartial;
             b.part = p.part_x;

@@ -2,7 +2,8 @@
 // matrix: out[row][col] = sum over k of x[row][k] * w[col][k], at most 64 rows.
 //
 // Bound by the weights' bytes: every weight is read once, straight into the registers that the
-// matrix instructions take it from.  A workgroup owns 16 or 32 columns; its waves share out the
+// matrix instructions take it from (one row over 50,257 x 1,024 in bf16: 22.6 us with the launch,
+// 4.56 TB/s; 4,384 x 1,024: 4.8 us, the launch).  A workgroup owns 16 or 32 columns; its waves share out the
 // contraction in runs of 128 indices, so that a wave has 4 or 8 loads of 16 bytes a lane in flight
 // and four lanes read 256 contiguous bytes of a weight row.  x is small and comes from the caches.
 // The waves' partial tiles meet in LDS, in a fixed order.
@@ -157,7 +158,7 @@ __global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const Sk
         if constexpr (OUT == kTileStore) {
             if (r < nrow) store4(a.store, v, load_bias(a.store, col0 + c, a.ncol), r, col0 + c, a.ncol);
         } else {
-            // eight consecutive lanes hold a row's 32 columns
+            // kQuads consecutive lanes hold a row's columns
             const BestArgs &b = a.best;
             const int label = b.label && r < nrow ? b.label[r] : -1;
             Best m{-INFINITY, 0.f, kNoColumn};

@@ -3,8 +3,19 @@
 // (bdlm_dense.h: the epilogue of a projection, partial sums, softmax records, loss gradients).
 //
 // One workgroup per tile (and split).  The operands go straight from memory to LDS in 16-byte
-// pieces, a stage of 64 contraction indices at a time into one of two buffers.  `col` is the
-// first MFMA operand, so a lane holds groups of four consecutive columns of one row.
+// pieces, a stage of 64 contraction indices at a time into one of two buffers (or four).  `col` is
+// the first MFMA operand, so a lane holds groups of four consecutive columns of one row.
+//
+// Bound by the matrix unit and the clock that it can hold: 8,192 x 8,192 x 8,192 in bf16 takes
+// 900 to 980 us by the card (1,225 to 1,120 TFLOP/s), with the matrix unit busy in 0.69 of the
+// cycles and the clock at 1.5 to 2.0 GHz under that load.  A tile of 256 x 256
+// reads a byte of its operands for 128 operations; tiles of 128 x 128 need twice the LDS reads and
+// copies and are for launches that large tiles would leave partly idle.  The epilogue of a large tile is not hidden, as its
+// buffers leave a CU one workgroup: GELU with the pre-activation kept costs 68 of the 218 us of
+// 16,384 x 1,024 x 4,096.
+// Built and measured slower at 8,192^3: four waves of 128 x 128 (900 to 1,080 us), operands
+// staged through registers, a ring of four stages of 32, a stage's copies all in one group,
+// nontemporal or streaming copies.
 //
 // An operand whose contraction index is contiguous lies in LDS as [row][64] (eight pieces a
 // row) and is read 16 bytes a lane; one whose contraction index is the slow one lies as
@@ -46,9 +57,9 @@ __device__ __forceinline__ s16x4 read_tr(const char *lds) {
 }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// c += a b, in place: written out so that the accumulators stay in their registers (256 of them are
-// all the accumulation registers there are; given the builtin, the compiler rotates them
-// through copies).  The wait states cover an operand that the compiler has just moved; the
+// c += a b, in place: written out so that the accumulators stay in their registers (given the
+// builtin, the compiler rotates them through copies).  The wait states cover an operand that the
+// compiler has just moved; the
 // matrix pipeline is busy for longer than that.  At every edge of the control flow, where the
 // compiler may move accumulators, settle() waits for the last products' results.
 // 32 x 32 outputs a product: a wave issues an instruction every four cycles or so, and products of
@@ -70,8 +81,8 @@ __device__ __forceinline__ void settle(f32x16 (&acc)[FC][FR]) {
 __device__ __forceinline__ int piece_of(int t) { return 4 * (t & 3) ^ 2 * ((t >> 3) & 1); }
 
 // One operand's share of a tile: R rows (or columns) from `first` on, a stage deep.  REPEAT (T
-// only): contraction indices past the operand's end read another row again, as the other
-// operand is zero there.
+// only): contraction indices past the operand's end, and the index `skip`, read another row again,
+// as the other operand is zero there.
 template <int R, bool T, int WAVES, bool REPEAT>
 struct Stage {
     static constexpr int kPieces = R * kDepth / 8;        // 16-byte pieces of a stage
@@ -107,10 +118,12 @@ struct Stage {
         return base + plane * 2 + kt * stride();
     }
     __device__ __forceinline__ int64_t stride() const { return T ? kDepth * ld2 : 2 * kDepth; }   // of a stage
-    // left: contraction indices from the stage's first to the operand's end
-    __device__ __forceinline__ void copy(int i, const char *from, uint4 *lds, int left, int wave) const {
+    // left, skip: contraction indices from the stage's first to the operand's end, and to the one that
+    // is not read (never the only one of a stage)
+    __device__ __forceinline__ void copy(int i, const char *from, uint4 *lds, int left, int skip, int wave) const {
         uint32_t o = off[i];
-        if constexpr (T && REPEAT) o = at[i] < left ? o : o - static_cast<uint32_t>(at[i] * ld2);
+        if constexpr (T && REPEAT)
+            o = at[i] < left && at[i] != skip ? o : o + static_cast<uint32_t>(((skip == 0) - at[i]) * ld2);
         copy16(from, o, lds + (i * WAVES + wave) * 64);
     }
 };
@@ -249,14 +262,14 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
     return m;
 }
 
-// Four waves of (E / 2) x (E / 2) outputs.  A stage is four groups of products, each from one of two
-// sets of registers while the other fills with the next group's operands from LDS.  With
-// the last group's operands read, and the next stage arrived in the other buffer, the waves
-// meet; then the stage after it is copied into this buffer, half of it during the last group
-// and half during the next stage's first.
+// WR x WC waves of (E / WR) x (E / WC) outputs: of 128 x 64 in a tile of 256, of 64 x 64 in one of
+// 128.  A stage is four groups of products, each from one of two sets of registers while the other
+// fills with the next group's operands from LDS.  With the last group's operands read, and the
+// next stage arrived in its buffer, the waves meet; then the stage that takes this buffer over is
+// copied into it, from the last group through the next stage's first two.
 //
-// E 256: one wave on each SIMD, 256 accumulators a lane.  E 128: two workgroups on a CU, so that
-// one's epilogue meets the other's products.
+// E 256: two waves on each SIMD, 128 accumulators a lane.  E 128 with two buffers: two workgroups on
+// a CU, so that one's epilogue meets the other's products.
 template <int E, int WR, int WC, int BUFS, bool ROWT, bool COLT, int OUT>
 __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_kernel(const TileArgs a) {
     constexpr int WAVES = WR * WC, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
@@ -332,26 +345,26 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     // where the next stage's contents come from, and the one's before it, half of which is copied later
     struct From {
         const char *c, *r;
-        int left;
+        int left, skip;
     };
     int pair = it0 / (nkt > 0 ? nkt : 1), kt = it0 - pair * nkt;
     From next{sc.at_step(col_term(a.npair, pair) * a.col.plane, kt),
-              sr.at_step(row_term(a.npair, pair) * a.row.plane, kt), K - kt * kDepth};
+              sr.at_step(row_term(a.npair, pair) * a.row.plane, kt), K - kt * kDepth, a.skip - kt * kDepth};
     From prev = next;
     auto advance = [&]() {
         prev = next;
-        next = From{next.c + sc.stride(), next.r + sr.stride(), next.left - kDepth};
+        next = From{next.c + sc.stride(), next.r + sr.stride(), next.left - kDepth, next.skip - kDepth};
         if (++kt == nkt) {   // (more than one pair of planes)
             kt = 0;
             ++pair;
             next = From{sc.at_step(col_term(a.npair, pair) * a.col.plane, 0),
-                        sr.at_step(row_term(a.npair, pair) * a.row.plane, 0), K};
+                        sr.at_step(row_term(a.npair, pair) * a.row.plane, 0), K, a.skip};
         }
     };
     constexpr int kLoads = Stage<E, COLT, WAVES, true>::kLoads;   // of either operand
     auto copy = [&](int i, int buf, const From &f) {
-        if (i < kLoads) sc.copy(i, f.c, sm[buf], f.left, wave);
-        else sr.copy(i - kLoads, f.r, sm[buf] + kBuf, f.left, wave);
+        if (i < kLoads) sc.copy(i, f.c, sm[buf], f.left, f.skip, wave);
+        else sr.copy(i - kLoads, f.r, sm[buf] + kBuf, 0, -1, wave);
     };
     bf16x8 fc[2][FC], fr[2][FR];
     // in the order that products use them: column 0, the rows, the other columns

@@ -322,6 +322,35 @@ def test_non_finite_values():
         assert bool((dx[2] == 0).all()) and bool(torch.isfinite(dx).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_excluded_token_has_no_part(dtype):
+    """The excluded token's row of w may hold anything: results are bitwise those with zeros there.
+    Excluded: the first, the last (also alone in a step of 64 contraction indices), the first, a
+    middle and the last of such a step; the ends of a piece of the vocabulary (66,000 rows)."""
+    import paper_2607_02805_amd as bd
+    r = gen(23)
+    cases = [(m, n, x) for m in (3, 70, 300) for n, x in ((577, 576), (577, 0), (577, 64), (640, 127), (640, 639), (578, 576))]
+    if dtype == BF:
+        cases += [(66000, 8200, 2815), (66000, 8200, 2816), (66000, 8200, 8199)]
+    for m, n, exclude in cases:
+        k = 64 if m < 1000 else 16
+        x, w = r(m, k).to(dtype).to(DEV), (r(n, k) / 8).to(dtype).to(DEV)
+        labels = (torch.arange(m, device=DEV) * 7) % n
+        labels[1] = -1
+        dloss = torch.ones(m, device=DEV)
+        w[exclude] = 0
+        got = []
+        for value in (0.0, float("nan")):
+            w[exclude] = value
+            token, logprob = bd.head_select(x, w, exclude=exclude)
+            loss, lse = bd.head_loss(x, w, labels, exclude=exclude)
+            dx, dw = bd.head_loss_backward(dloss, x, w, labels, loss, lse, exclude=exclude)
+            got.append((token, logprob, loss, lse, dx, dw))
+        for a, b in zip(*got):
+            assert torch.equal(a, b), (m, n, exclude)
+        assert bool(torch.isfinite(got[1][4]).all()) and bool((got[1][5][exclude] == 0).all())
+
+
 def test_activations_far_out():
     """Pre-activations of 1e4 and more, both ways, and infinities: values and slopes are the limits."""
     import paper_2607_02805_amd as bd
