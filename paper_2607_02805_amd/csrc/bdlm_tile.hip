@@ -366,33 +366,39 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         if (i < kLoads) sc.copy(i, f.c, sm[buf], f.left, f.skip, wave);
         else sr.copy(i - kLoads, f.r, sm[buf] + kBuf, 0, -1, wave);
     };
-    bf16x8 fc[2][FC], fr[2][FR];
+    constexpr int kAhead = E == 128 ? 2 : 1, kSets = 2 * kAhead;   // groups that operands are read ahead
+    bf16x8 fc[kSets][FC], fr[kSets][FR];
     // in the order that products use them: column 0, the rows, the other columns
     auto order = [](int k) { return k == 0 ? 0 : k <= FR ? FC + k - 1 : k - FR; };
     auto read = [&](int x, int buf, int g) {
-        if (x < FC) fc[g & 1][x] = rc.get(reinterpret_cast<const char *>(sm[buf]), x, g);
-        else fr[g & 1][x - FC] = rr.get(reinterpret_cast<const char *>(sm[buf] + kBuf), x - FC, g);
+        if (x < FC) fc[g % kSets][x] = rc.get(reinterpret_cast<const char *>(sm[buf]), x, g);
+        else fr[g % kSets][x - FC] = rr.get(reinterpret_cast<const char *>(sm[buf] + kBuf), x - FC, g);
     };
     constexpr int kProducts = FC * FR, kReads = FC + FR;   // of a group
-    // Copies of a stage, by the group that they are made in: the last of the stage before the one
-    // before it (where its buffer becomes free), then the next one's first two.  All at once they
+    // Copies of a stage, in parts by group: from the one in which its buffer becomes free, kMeetGroup,
+    // on, the second and third in the next stage where that one is the last.  All at once they
     // would come faster than they are served (64 bytes a cycle), and the products would wait.
-    constexpr int kCopies = 2 * kLoads, kC1 = kCopies * 7 / 16, kC0 = kCopies * 7 / 16, kC3 = kCopies - kC0 - kC1;
-    // Group g of the stage in buffer `buf`.  Between its products: the reads of the next group (of the
-    // last one: the next stage's first, or nothing's where there is none), and, if `copies`, a
-    // part of a stage's copies.  No product lies in a branch, so that no accumulator is moved.
-    auto group = [&](auto g_, int s, bool copies) {
+    constexpr int kMeetGroup = kGroups - kAhead;
+    constexpr int kCopies = 2 * kLoads, kPart2 = kCopies * 7 / 16, kPart1 = kPart2, kPart0 = kCopies - kPart1 - kPart2;
+    constexpr int kEarly = kAhead == 1 ? kPart0 : kPart0 + kPart1;   // in the stage whose buffer it is
+    // Group g of the stage in buffer `buf`.  Between its products: the reads of the group kAhead on (of
+    // the last ones: the next stage's first, or nothing's where there is none), and, if it has some,
+    // a part of a stage's copies.  No product lies in a branch, so that no accumulator is moved.
+    auto group = [&](auto g_, int s) {
         constexpr int g = decltype(g_)::value;
-        constexpr bool last = g == kGroups - 1;
+        constexpr bool meets = g == kMeetGroup, own = g >= kMeetGroup;   // own: copies over this stage's buffer
+        constexpr int part = (g - kMeetGroup + kGroups) % kGroups;
         const int buf = s % BUFS, after = (s + 1) % BUFS, before = (s + BUFS - 1) % BUFS;
-        constexpr int copies_from = g == 0 ? kC3 : kC3 + kC0, count = last ? kC3 : g == 0 ? kC0 : g == 1 ? kC1 : 0;
+        constexpr int copies_from = part == 0 ? 0 : part == 1 ? kPart0 : kPart0 + kPart1;
+        constexpr int count = part == 0 ? kPart0 : part == 1 ? kPart1 : part == 2 ? kPart2 : 0;
+        const bool copies = own ? s + BUFS < n : s + BUFS - 1 < n;
         __builtin_amdgcn_sched_barrier(0);
-        constexpr int kMeet = kProducts * 6 / 16;   // products before the waves meet, in the last group
+        constexpr int kMeet = kProducts * 6 / 16;   // products before the waves meet, in that group
 #pragma unroll
         for (int x = 0; x < kProducts; ++x) {
-            mma(fc[g & 1][x / FR], fr[g & 1][x % FR], acc[x / FR][x % FR]);
+            mma(fc[g % kSets][x / FR], fr[g % kSets][x % FR], acc[x / FR][x % FR]);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (last) {
+            if constexpr (meets) {
                 if (x + 1 == kMeet) {
                     // the next stage has arrived: only later ones' copies may be on their way
                     if (BUFS > 2 && s + BUFS <= n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies) : "memory");
@@ -401,16 +407,16 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
                     asm volatile("" ::: "memory");
                 }
             }
-            constexpr int from = last ? kMeet - 1 : 0, slots = kProducts - from;
+            constexpr int from = meets ? kMeet - 1 : 0, slots = kProducts - from;
             const int slot = x - from;
             if (slot >= 0) {
 #pragma unroll
                 for (int k = 0; k < kReads; ++k)
-                    if (k * slots / kReads == slot) read(order(k), last ? after : buf, (g + 1) % kGroups);
+                    if (k * slots / kReads == slot) read(order(k), own ? after : buf, (g + kAhead) % kGroups);
 #pragma unroll
                 for (int k = 0; k < count; ++k)
                     if (k * slots / count == slot && copies)
-                        copy(last ? k : copies_from + k, last ? buf : before, last ? next : prev);
+                        copy(copies_from + k, own ? buf : before, own ? next : prev);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -422,23 +428,25 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
             if (s >= n) break;
             if (s > 0) advance();
 #pragma unroll
-            for (int k = 0; k < (s + 1 < BUFS ? kCopies : kC3); ++k) copy(k, s, next);
+            for (int k = 0; k < (s + 1 < BUFS ? kCopies : kEarly); ++k) copy(k, s, next);
         }
-        if (n >= BUFS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies + kC3) : "memory");
+        if (n >= BUFS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies + kEarly) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
-        for (int x = 0; x < kReads; ++x) read(x, 0, 0);
+        for (int g = 0; g < kAhead; ++g)
+#pragma unroll
+            for (int x = 0; x < kReads; ++x) read(x, 0, g);
     }
     for (int s = 0; s < n; ++s) {
-        // stage s + BUFS is copied over stage s: from the last group on, through the next stage's first two
+        // stage s + BUFS is copied over stage s: from group kMeetGroup on, through the next stage's first
         prev = next;
         if (s + BUFS < n) advance();
-        group(Int<0>{}, s, s + BUFS - 1 < n);
-        group(Int<1>{}, s, s + BUFS - 1 < n);
-        group(Int<2>{}, s, false);
-        group(Int<3>{}, s, s + BUFS < n);
+        group(Int<0>{}, s);
+        group(Int<1>{}, s);
+        group(Int<2>{}, s);
+        group(Int<3>{}, s);
         settle(acc);
     }
     __syncthreads();   // every wave has read the last stage
