@@ -39,14 +39,15 @@ constexpr int kGroups = kDepth / 16;   // of products
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// 16 bytes a lane from base + off to LDS at `to`, lane by lane.  Written out because the compiler
-// makes every LDS transpose read wait for the copies it knows of; nothing is returned in
-// registers, and step() waits for the copies before the barrier that hands a buffer over.
-__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint4 *to) {
-    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void *)to));
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+// 16 bytes a lane from base + off + AT to LDS at `to` + AT, lane by lane (the instruction adds its
+// offset to both).  Written out because the compiler makes every LDS transpose read wait for the
+// copies it knows of; nothing is returned in registers, and group() waits for the copies before
+// the barrier that hands a buffer over.
+template <int AT>
+__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%3"
                  :
-                 : "v"(off), "s"(base), "s"(lds)
+                 : "v"(off), "s"(base), "s"(to), "n"(AT)
                  : "memory", "m0");
 }
 __device__ __forceinline__ bf16x8 frag(const char *lds) {
@@ -88,29 +89,31 @@ struct Stage {
     static constexpr int kPieces = R * kDepth / 8;        // 16-byte pieces of a stage
     static constexpr int kLoads = kPieces / (64 * WAVES);   // per lane
     static_assert(kLoads * 64 * WAVES == kPieces, "whole loads");
-    const char *base;      // the operand at (first, 0) of its first plane
+    static constexpr int kLast = (kLoads - 1) * 1024;   // a wave's pieces lie together: its last 64 from its first
+    static_assert(kLast < 4096, "the instruction's offset");
+    const char *base;      // the operand at (first, 0) of its first plane, less kLast
     int64_t ld2;           // bytes of a row
-    uint32_t off[kLoads];    // this lane's bytes from base
+    uint32_t off[kLoads];    // this lane's bytes from base, less the instruction's offset
     int32_t at[T ? kLoads : 1];   // T: contraction index of the piece within the stage
 
     // rows past the operand's end repeat its last row, columns past it its first piece
     __device__ __forceinline__ void init(const Mat &m, int64_t first, int64_t size, int wave, int lane) {
         ld2 = m.ld * 2;
-        base = reinterpret_cast<const char *>(m.p) + (T ? first * 2 : first * ld2);
+        base = reinterpret_cast<const char *>(m.p) + (T ? first * 2 : first * ld2) - kLast;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int piece = (i * WAVES + wave) * 64 + lane;
+            const int piece = (wave * kLoads + i) * 64 + lane, more = kLast - i * 1024;
             if constexpr (T) {
                 constexpr int kRow = R / 8;
                 const int t = piece / kRow, pos = piece % kRow;
                 int c = pos ^ piece_of(t);
                 if (first + 8 * c >= size) c = 0;
                 at[i] = t;
-                off[i] = static_cast<uint32_t>(t * ld2 + c * 16);
+                off[i] = static_cast<uint32_t>(t * ld2 + c * 16) + more;
             } else {
                 const int r = piece >> 3, c = (piece & 7) ^ ((r >> 1) & 7);
                 const int64_t rr = first + r < size ? r : size - 1 - first;
-                off[i] = static_cast<uint32_t>(rr * ld2 + c * 16);
+                off[i] = static_cast<uint32_t>(rr * ld2 + c * 16) + more;
             }
         }
     }
@@ -120,11 +123,14 @@ struct Stage {
     __device__ __forceinline__ int64_t stride() const { return T ? kDepth * ld2 : 2 * kDepth; }   // of a stage
     // left, skip: contraction indices from the stage's first to the operand's end, and to the one that
     // is not read (never the only one of a stage)
-    __device__ __forceinline__ void copy(int i, const char *from, uint4 *lds, int left, int skip, int wave) const {
+    // lds: the wave's pieces of the stage
+    template <int I>
+    __device__ __forceinline__ void copy(const char *from, uint32_t lds, int left, int skip) const {
+        constexpr int i = I;
         uint32_t o = off[i];
         if constexpr (T && REPEAT)
             o = at[i] < left && at[i] != skip ? o : o + static_cast<uint32_t>(((skip == 0) - at[i]) * ld2);
-        copy16(from, o, lds + (i * WAVES + wave) * 64);
+        copy16<I * 1024>(from, o, lds);
     }
 };
 
@@ -160,13 +166,21 @@ struct Reader {
 
 // Pair i of planes multiplies term row_term(i) of `row` and col_term(i) of `col`: of two fp32
 // operands the six of weight 2^-16 or more, of a `row` in two terms and a bf16 `col` both.
-__device__ __forceinline__ int row_term(int npair, int i) { return npair == 6 ? (0x010210 >> (4 * i)) & 15 : i; }
-__device__ __forceinline__ int col_term(int npair, int i) { return npair == 6 ? (0x102010 >> (4 * i)) & 15 : 0; }
+__device__ __forceinline__ int row_term(int npair, int i) { return npair == 6 ? static_cast<int>(0x010210ll >> (4 * i)) & 15 : i; }
+__device__ __forceinline__ int col_term(int npair, int i) { return npair == 6 ? static_cast<int>(0x102010ll >> (4 * i)) & 15 : 0; }
 
 template <int V>
 struct Int {
     static constexpr int value = V;
 };
+// f(Int<0>) .. f(Int<N - 1>)
+template <int N, class F>
+__device__ __forceinline__ void repeat(F f) {
+    if constexpr (N > 0) {
+        repeat<N - 1>(f);
+        f(Int<N - 1>{});
+    }
+}
 
 // What the epilogue needs of a row, kept in LDS from the start of the kernel.
 struct RowData {
@@ -342,7 +356,7 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    // where the next stage's contents come from, and the one's before it, half of which is copied later
+    // where the next stage's contents come from
     struct From {
         const char *c, *r;
         int left, skip;
@@ -350,9 +364,7 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     int pair = it0 / (nkt > 0 ? nkt : 1), kt = it0 - pair * nkt;
     From next{sc.at_step(col_term(a.npair, pair) * a.col.plane, kt),
               sr.at_step(row_term(a.npair, pair) * a.row.plane, kt), K - kt * kDepth, a.skip - kt * kDepth};
-    From prev = next;
-    auto advance = [&]() {
-        prev = next;
+    auto advance = [&]() {   // (past the last stage: to addresses that are not read)
         next = From{next.c + sc.stride(), next.r + sr.stride(), next.left - kDepth, next.skip - kDepth};
         if (++kt == nkt) {   // (more than one pair of planes)
             kt = 0;
@@ -362,9 +374,12 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         }
     };
     constexpr int kLoads = Stage<E, COLT, WAVES, true>::kLoads;   // of either operand
-    auto copy = [&](int i, int buf, const From &f) {
-        if (i < kLoads) sc.copy(i, f.c, sm[buf], f.left, f.skip, wave);
-        else sr.copy(i - kLoads, f.r, sm[buf] + kBuf, 0, -1, wave);
+    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_void *)sm)) + wave * kLoads * 1024;
+    auto copy = [&](auto i_, int buf) {
+        constexpr int i = decltype(i_)::value;
+        const uint32_t to = lds + buf * int(sizeof(sm[0]));
+        if constexpr (i < kLoads) sc.template copy<i>(next.c, to, next.left, next.skip);
+        else sr.template copy<i - kLoads>(next.r, to + kBuf * 16, 0, -1);
     };
     constexpr int kAhead = E == 128 ? 2 : 1, kSets = 2 * kAhead;   // groups that operands are read ahead
     bf16x8 fc[kSets][FC], fr[kSets][FR];
@@ -392,6 +407,7 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         constexpr int copies_from = part == 0 ? 0 : part == 1 ? kPart0 : kPart0 + kPart1;
         constexpr int count = part == 0 ? kPart0 : part == 1 ? kPart1 : part == 2 ? kPart2 : 0;
         const bool copies = own ? s + BUFS < n : s + BUFS - 1 < n;
+        constexpr int kStep = kProducts / 2;   // in the group before that one: on to the next stage
         __builtin_amdgcn_sched_barrier(0);
         constexpr int kMeet = kProducts * 6 / 16;   // products before the waves meet, in that group
 #pragma unroll
@@ -401,8 +417,8 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
             if constexpr (meets) {
                 if (x + 1 == kMeet) {
                     // the next stage has arrived: only later ones' copies may be on their way
-                    if (BUFS > 2 && s + BUFS <= n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies) : "memory");
-                    else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies) : "memory");
+                    if (BUFS > 2 && s + BUFS > n) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
                 }
@@ -413,11 +429,13 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
 #pragma unroll
                 for (int k = 0; k < kReads; ++k)
                     if (k * slots / kReads == slot) read(order(k), own ? after : buf, (g + kAhead) % kGroups);
-#pragma unroll
-                for (int k = 0; k < count; ++k)
-                    if (k * slots / count == slot && copies)
-                        copy(copies_from + k, own ? buf : before, own ? next : prev);
+                if (copies)
+                    repeat<count>([&](auto k) {
+                        constexpr int v = decltype(k)::value;
+                        if (v * slots / count == slot) copy(Int<copies_from + v>{}, own ? buf : before);
+                    });
             }
+            if (g == kMeetGroup - 1 && x == kStep) advance();
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -427,8 +445,8 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         for (int s = 0; s < BUFS; ++s) {
             if (s >= n) break;
             if (s > 0) advance();
-#pragma unroll
-            for (int k = 0; k < (s + 1 < BUFS ? kCopies : kEarly); ++k) copy(k, s, next);
+            repeat<kEarly>([&](auto k) { copy(k, s); });
+            if (s + 1 < BUFS) repeat<kCopies - kEarly>([&](auto k) { copy(Int<kEarly + decltype(k)::value>{}, s); });
         }
         if (n >= BUFS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies + kEarly) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -441,8 +459,6 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     }
     for (int s = 0; s < n; ++s) {
         // stage s + BUFS is copied over stage s: from group kMeetGroup on, through the next stage's first
-        prev = next;
-        if (s + BUFS < n) advance();
         group(Int<0>{}, s);
         group(Int<1>{}, s);
         group(Int<2>{}, s);
