@@ -134,23 +134,23 @@ struct Stage {
     }
 };
 
-// Operand reads: fragment i, 32 rows from `row0` + 32 i, of group g of the stage (16 indices).
-// Lane: row lane & 31, indices 8 (lane >> 5) .. + 7.
-template <int R, bool T, int F>
+// Operand reads: fragment i, 32 rows from `row0` + 32 i, of group `first` + g of the stage (16
+// indices; G groups).  Lane: row lane & 31, indices 8 (lane >> 5) .. + 7.
+template <int R, bool T, int F, int G>
 struct Reader {
-    int off[T ? F : kGroups];
-    __device__ __forceinline__ void init(int row0, int lane) {
+    int off[T ? F : G];
+    __device__ __forceinline__ void init(int row0, int first, int lane) {
         if constexpr (T) {
             const int s = lane & 15, t = 8 * (lane >> 5) + (s >> 2);
 #pragma unroll
             for (int i = 0; i < F; ++i) {
                 const int c = (row0 + 32 * i + (lane & 16)) / 8 + ((s & 3) >> 1);
-                off[i] = (t * (R / 8) + (c ^ piece_of(t))) * 16 + (s & 1) * 8;
+                off[i] = (t * (R / 8) + (c ^ piece_of(t))) * 16 + (s & 1) * 8 + first * (16 * 2 * R);
             }
         } else {
             const int r = row0 + (lane & 31);
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) off[g] = r * 128 + (((2 * g + (lane >> 5)) ^ ((r >> 1) & 7)) * 16);
+            for (int g = 0; g < G; ++g) off[g] = r * 128 + (((2 * (first + g) + (lane >> 5)) ^ ((r >> 1) & 7)) * 16);
         }
     }
     __device__ __forceinline__ bf16x8 get(const char *lds, int i, int g) const {
@@ -277,16 +277,20 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
 }
 
 // WR x WC waves of (E / WR) x (E / WC) outputs: of 128 x 64 in a tile of 256, of 64 x 64 in one of
-// 128.  A stage is four groups of products, each from one of two sets of registers while the other
+// 128, where KS = 2 such sets of waves take half of a stage's contraction each and add up at the
+// end.  (With one set a SIMD has a wave too few: instructions come at most every four cycles from a
+// wave, some ten a product, and a product takes 32.  512 x 1,024 x 4,384 takes 14.8 us instead of
+// 17.1, 1,500 x 832 x 16,001 in fp32 276 instead of 286.  Large tiles have two waves a SIMD, and no
+// registers for more.)  A stage is groups of products, four or a wave's two, each from one of two sets of registers while the other
 // fills with the next group's operands from LDS.  With the last group's operands read, and the
 // next stage arrived in its buffer, the waves meet; then the stage that takes this buffer over is
 // copied into it, from the last group through the next stage's first two.
 //
 // E 256: two waves on each SIMD, 128 accumulators a lane.  E 128 with two buffers: two workgroups on
 // a CU, so that one's epilogue meets the other's products.
-template <int E, int WR, int WC, int BUFS, bool ROWT, bool COLT, int OUT>
-__global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_kernel(const TileArgs a) {
-    constexpr int WAVES = WR * WC, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
+template <int E, int WR, int WC, int KS, int BUFS, bool ROWT, bool COLT, int OUT>
+__global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) bdlm_tile_kernel(const TileArgs a) {
+    constexpr int WAVES = WR * WC * KS, kWaveGroups = kGroups / KS, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
     constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's stage
     constexpr int kRec = OUT == kTileBest ? E : 1;
     __shared__ uint4 sm[BUFS][2 * kBuf];                 // [buffer][col, then row]
@@ -324,11 +328,11 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     Stage<E, ROWT, WAVES, false> sr;
     sc.init(a.col, col0, a.ncol, wave, lane);
     sr.init(a.row, row0, nrow, wave, lane);
-    const int wr = wave % WR, wc = wave / WR;
-    Reader<E, COLT, FC> rc;
-    Reader<E, ROWT, FR> rr;
-    rc.init(wc * (E / WC), lane);
-    rr.init(wr * (E / WR), lane);
+    const int wr = wave % WR, wc = wave / WR % WC, half = wave / (WR * WC);
+    Reader<E, COLT, FC, kWaveGroups> rc;
+    Reader<E, ROWT, FR, kWaveGroups> rr;
+    rc.init(wc * (E / WC), half * kWaveGroups, lane);
+    rr.init(wr * (E / WR), half * kWaveGroups, lane);
 
     if constexpr (OUT == kTileProb) {
         const ProbArgs &b = a.prob;
@@ -381,40 +385,39 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         if constexpr (i < kLoads) sc.template copy<i>(next.c, to, next.left, next.skip);
         else sr.template copy<i - kLoads>(next.r, to + kBuf * 16, 0, -1);
     };
-    constexpr int kAhead = E == 128 ? 2 : 1, kSets = 2 * kAhead;   // groups that operands are read ahead
-    bf16x8 fc[kSets][FC], fr[kSets][FR];
+    bf16x8 fc[2][FC], fr[2][FR];
     // in the order that products use them: column 0, the rows, the other columns
     auto order = [](int k) { return k == 0 ? 0 : k <= FR ? FC + k - 1 : k - FR; };
     auto read = [&](int x, int buf, int g) {
-        if (x < FC) fc[g % kSets][x] = rc.get(reinterpret_cast<const char *>(sm[buf]), x, g);
-        else fr[g % kSets][x - FC] = rr.get(reinterpret_cast<const char *>(sm[buf] + kBuf), x - FC, g);
+        if (x < FC) fc[g & 1][x] = rc.get(reinterpret_cast<const char *>(sm[buf]), x, g);
+        else fr[g & 1][x - FC] = rr.get(reinterpret_cast<const char *>(sm[buf] + kBuf), x - FC, g);
     };
     constexpr int kProducts = FC * FR, kReads = FC + FR;   // of a group
-    // Copies of a stage, in parts by group: from the one in which its buffer becomes free, kMeetGroup,
-    // on, the second and third in the next stage where that one is the last.  All at once they
-    // would come faster than they are served (64 bytes a cycle), and the products would wait.
-    constexpr int kMeetGroup = kGroups - kAhead;
-    constexpr int kCopies = 2 * kLoads, kPart2 = kCopies * 7 / 16, kPart1 = kPart2, kPart0 = kCopies - kPart1 - kPart2;
-    constexpr int kEarly = kAhead == 1 ? kPart0 : kPart0 + kPart1;   // in the stage whose buffer it is
-    // Group g of the stage in buffer `buf`.  Between its products: the reads of the group kAhead on (of
-    // the last ones: the next stage's first, or nothing's where there is none), and, if it has some,
+    // Copies of a stage, in parts: in the last group of the stage whose buffer it takes, where that
+    // becomes free, and in the next stage's first group, or two of four.  All at once they would
+    // come faster than they are served (64 bytes a cycle), and the products would wait.
+    constexpr int kCopies = 2 * kLoads, kPart1 = kCopies * (KS == 1 ? 7 : 8) / 16, kPart2 = KS == 1 ? kPart1 : 0;
+    constexpr int kPart0 = kCopies - kPart1 - kPart2;
+    // Group g of the stage in buffer `buf`.  Between its products: the reads of the next group (of the
+    // last one: the next stage's first, or nothing's where there is none), and, if it has some,
     // a part of a stage's copies.  No product lies in a branch, so that no accumulator is moved.
     auto group = [&](auto g_, int s) {
         constexpr int g = decltype(g_)::value;
-        constexpr bool meets = g == kMeetGroup, own = g >= kMeetGroup;   // own: copies over this stage's buffer
-        constexpr int part = (g - kMeetGroup + kGroups) % kGroups;
+        constexpr bool last = g == kWaveGroups - 1;
+        constexpr int part = (g + 1) % kWaveGroups;
         const int buf = s % BUFS, after = (s + 1) % BUFS, before = (s + BUFS - 1) % BUFS;
         constexpr int copies_from = part == 0 ? 0 : part == 1 ? kPart0 : kPart0 + kPart1;
         constexpr int count = part == 0 ? kPart0 : part == 1 ? kPart1 : part == 2 ? kPart2 : 0;
-        const bool copies = own ? s + BUFS < n : s + BUFS - 1 < n;
-        constexpr int kStep = kProducts / 2;   // in the group before that one: on to the next stage
+        const bool copies = last ? s + BUFS < n : s + BUFS - 1 < n;
+        // in the group before the last, after its copies: on to the next stage
+        constexpr int kStep = KS == 1 ? kProducts / 2 : kProducts - 1;
         __builtin_amdgcn_sched_barrier(0);
         constexpr int kMeet = kProducts * 6 / 16;   // products before the waves meet, in that group
 #pragma unroll
         for (int x = 0; x < kProducts; ++x) {
-            mma(fc[g % kSets][x / FR], fr[g % kSets][x % FR], acc[x / FR][x % FR]);
+            mma(fc[g & 1][x / FR], fr[g & 1][x % FR], acc[x / FR][x % FR]);
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (meets) {
+            if constexpr (last) {
                 if (x + 1 == kMeet) {
                     // the next stage has arrived: only later ones' copies may be on their way
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies) : "memory");
@@ -423,19 +426,19 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
                     asm volatile("" ::: "memory");
                 }
             }
-            constexpr int from = meets ? kMeet - 1 : 0, slots = kProducts - from;
+            constexpr int from = last ? kMeet - 1 : 0, slots = kProducts - from;
             const int slot = x - from;
             if (slot >= 0) {
 #pragma unroll
                 for (int k = 0; k < kReads; ++k)
-                    if (k * slots / kReads == slot) read(order(k), own ? after : buf, (g + kAhead) % kGroups);
+                    if (k * slots / kReads == slot) read(order(k), last ? after : buf, (g + 1) % kWaveGroups);
                 if (copies)
                     repeat<count>([&](auto k) {
                         constexpr int v = decltype(k)::value;
-                        if (v * slots / count == slot) copy(Int<copies_from + v>{}, own ? buf : before);
+                        if (v * slots / count == slot) copy(Int<copies_from + v>{}, last ? buf : before);
                     });
             }
-            if (g == kMeetGroup - 1 && x == kStep) advance();
+            if (g == kWaveGroups - 2 && x == kStep) advance();
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -445,24 +448,24 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         for (int s = 0; s < BUFS; ++s) {
             if (s >= n) break;
             if (s > 0) advance();
-            repeat<kEarly>([&](auto k) { copy(k, s); });
-            if (s + 1 < BUFS) repeat<kCopies - kEarly>([&](auto k) { copy(Int<kEarly + decltype(k)::value>{}, s); });
+            repeat<kPart0>([&](auto k) { copy(k, s); });
+            if (s + 1 < BUFS) repeat<kCopies - kPart0>([&](auto k) { copy(Int<kPart0 + decltype(k)::value>{}, s); });
         }
-        if (n >= BUFS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies + kEarly) : "memory");
+        if (n >= BUFS) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((BUFS - 2) * kCopies + kPart0) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
-        for (int g = 0; g < kAhead; ++g)
-#pragma unroll
-            for (int x = 0; x < kReads; ++x) read(x, 0, g);
+        for (int x = 0; x < kReads; ++x) read(x, 0, 0);
     }
     for (int s = 0; s < n; ++s) {
-        // stage s + BUFS is copied over stage s: from group kMeetGroup on, through the next stage's first
+        // stage s + BUFS is copied over stage s: from the last group on, through the next stage's first
         group(Int<0>{}, s);
         group(Int<1>{}, s);
-        group(Int<2>{}, s);
-        group(Int<3>{}, s);
+        if constexpr (KS == 1) {
+            group(Int<2>{}, s);
+            group(Int<3>{}, s);
+        }
         settle(acc);
     }
     __syncthreads();   // every wave has read the last stage
@@ -471,8 +474,8 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     // consecutive columns, or a lane has a whole row; quads are permuted by the row against bank
     // conflicts.
     constexpr int kCols = E / WC, kQuads = kCols / 4, kRows = 64 / kQuads;   // rows of one pass of the wave
-    static_assert(WAVES * 64 * kCols * 4 <= int(sizeof(sm)), "the waves' regions fit");
-    f32x4 *mine = reinterpret_cast<f32x4 *>(sm) + wave * 64 * kQuads;
+    static_assert(WR * WC * 64 * kCols * 4 <= int(sizeof(sm)), "the waves' regions fit");
+    f32x4 *mine = reinterpret_cast<f32x4 *>(sm) + (wave % (WR * WC)) * 64 * kQuads;   // (both halves')
     const int rows_out = OUT == kTileProb ? (nrow + 63) / 64 * 64 : nrow;
     const int col1 = static_cast<int>(col0) + wc * kCols;   // the wave's first column
     const int quad = lane % kQuads, sub = lane / kQuads;
@@ -481,19 +484,33 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     auto part = [&](auto j0_) {
         constexpr int j0 = decltype(j0_)::value;
         const int r1 = wr * (E / WR) + 32 * j0;   // the part's first row in the tile
-        if (row0 + r1 >= rows_out) return;
+        auto put = [&](bool add) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int i = 0; i < FC; ++i)
+                for (int i = 0; i < FC; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const f32x16 &v = acc[i][j0 + j];
-                    mine[(32 * j + (lane & 31)) * kQuads + ((8 * i + 2 * e + (lane >> 5)) ^ (lane & 15))] =
-                        f32x4{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
-                }
-        __builtin_amdgcn_wave_barrier();
+                    for (int e = 0; e < 4; ++e) {
+                        const f32x16 &v = acc[i][j0 + j];
+                        f32x4 *to = mine + (32 * j + (lane & 31)) * kQuads + ((8 * i + 2 * e + (lane >> 5)) ^ (lane & 15));
+                        const f32x4 u = {v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+                        *to = add ? u + *to : u;
+                    }
+        };
+        if constexpr (KS == 1) {
+            if (row0 + r1 >= rows_out) return;
+            put(false);
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            // the second half's sums, then the first half's added onto them
+            if (half == 1) put(false);
+            __syncthreads();
+            if (half == 0) put(true);
+            __syncthreads();
+            if (row0 + r1 >= rows_out) return;
+        }
         if constexpr (OUT == kTileBest) {
+            if (half != 0) return;
             const Best m = row_best(a, mine + lane * kQuads, lane & 15, kCols, col1);
             top[wc][r1 + lane] = m.top;
             others[wc][r1 + lane] = m.others;
@@ -509,7 +526,7 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
         } else {
             const int most = static_cast<int>(rows_out - row0) - r1;
 #pragma unroll 4
-            for (int x = sub; x < 64; x += kRows) {
+            for (int x = sub + half * (64 / KS); x < (half + 1) * (64 / KS); x += kRows) {
                 const f32x4 v = mine[x * kQuads + (quad ^ (x & 15))];
                 RowData d{};
                 if constexpr (OUT == kTileProb) d = rows[r1 + x];
@@ -520,7 +537,7 @@ __global__ void __launch_bounds__(64 * WR * WC, BUFS == 2 ? 2 : 1) bdlm_tile_ker
     };
     part(Int<0>{});
     if constexpr (FR > 2) part(Int<2>{});
-    static_assert(FR == 2 || FR == 4, "parts of 64 rows");
+    static_assert(FR == 2 || (FR == 4 && KS == 1), "parts of 64 rows, one where the halves meet");
     if constexpr (OUT == kTileBest) {
         __syncthreads();
         for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
@@ -540,10 +557,10 @@ template <bool ROWT, bool COLT, int OUT>
 hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
     // Small tiles that leave a CU one workgroup take four buffers, so that copies have three stages to
     // arrive (a stage of theirs is 512 cycles of products).
-    if (a.big) hipLaunchKernelGGL((bdlm_tile_kernel<256, 2, 4, 2, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
+    if (a.big) hipLaunchKernelGGL((bdlm_tile_kernel<256, 2, 4, 1, 2, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
     else if (g.x <= static_cast<unsigned>(kChip))
-        hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 4, ROWT, COLT, OUT>), g, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, ROWT, COLT, OUT>), g, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, 4, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, 2, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
     return hipGetLastError();
 }
 

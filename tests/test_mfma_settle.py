@@ -3,7 +3,7 @@
 The products of bdlm_tile.hip are written as inline assembly, so the compiler does not add the
 wait states that a product's result needs before another instruction reads or writes it (at
 most 19; another product on the same registers needs none).  This test follows
-the generated code in program order: no instruction but a product may touch an accumulator of a
+the generated code along every path: no instruction but a product may touch an accumulator of a
 product issued fewer than 19 wait states before.
 """
 import os
@@ -28,32 +28,60 @@ def _acc(text):
     return got
 
 
+def _blocks(lines):
+    """Basic blocks [(instructions, successors)] of a function's lines, in order."""
+    blocks, names = [[[], None]], {}
+    for line in lines:
+        line = line.split(";")[0].strip()
+        label = re.match(r"(\.L\w+):$", line)
+        if label:
+            names[label.group(1)] = len(blocks)
+            blocks.append([[], None])
+        elif line and not line.startswith(".") and not line.endswith(":"):
+            blocks[-1][0].append(line)
+            if re.match(r"s_c?branch|s_endpgm", line):
+                blocks[-1][1] = line
+                blocks.append([[], None])
+    out = []
+    for n, (code, end) in enumerate(blocks):
+        after = [n + 1] if n + 1 < len(blocks) and not (end or "").startswith(("s_branch", "s_endpgm")) else []
+        target = re.search(r"\.L\w+", end or "")
+        out.append((code, after + ([names[target.group(0)]] if target else [])))
+    return out
+
+
 def early_touches(asm: str):
-    """(function, product, instruction) for each accumulator touched too early."""
-    found = []
+    """(function, product, instruction) for each accumulator touched too early on any path."""
+    found = set()
     for block in re.split(r"\n(?=_Z\w+:)", asm):
         m = re.match(r"(_Z\w+):", block)
         if not m or "v_mfma" not in block:
             continue
-        age, by = {}, {}           # register: wait states since its product, the product
-        for line in block.splitlines()[1:]:
-            line = line.split(";")[0].strip()
-            if not line or line.startswith(".") or line.endswith(":"):
-                continue
-            op = line.split()[0]
-            if op.startswith("v_mfma"):
-                for r in age:
-                    age[r] += 1
-                for r in _acc(line.split(",")[0]):
-                    age[r], by[r] = 0, line
-                continue
-            for r in _acc(line):
-                if age.get(r, WAIT) < WAIT:
-                    found.append((m.group(1)[:70], by[r], line))
-            states = int(line.split()[1]) + 1 if op == "s_nop" else 1
-            for r in age:
-                age[r] += states
-    return found
+        blocks = _blocks(block.split(".Lfunc_end")[0].splitlines()[1:])
+        entry = {0: {}}            # block: {register: (wait states since its product, the product)}
+        todo = [0]
+        while todo:
+            n = todo.pop()
+            age = dict(entry[n])
+            for line in blocks[n][0]:
+                op = line.split()[0]
+                if op.startswith("v_mfma"):
+                    age = {r: (a + 1, by) for r, (a, by) in age.items()}
+                    age.update({r: (0, line) for r in _acc(line.split(",")[0])})
+                    continue
+                found |= {(m.group(1)[:70], age[r][1], line) + (r,) for r in _acc(line) if r in age}
+                states = int(line.split()[1]) + 1 if op == "s_nop" else 1
+                age = {r: (a + states, by) for r, (a, by) in age.items() if a + states < WAIT}
+            for to in blocks[n][1]:
+                known = entry.get(to)
+                merged = dict(known or {})
+                for r, v in age.items():
+                    if r not in merged or v[0] < merged[r][0]:
+                        merged[r] = v
+                if known is None or {r: a for r, (a, _) in merged.items()} != {r: a for r, (a, _) in known.items()}:
+                    entry[to] = merged
+                    todo.append(to)
+    return sorted(found)
 
 
 @pytest.fixture(scope="module")
@@ -92,3 +120,17 @@ def test_the_scan_finds_a_planted_touch():
     assert early_touches(head + product + "\ts_nop 15\n\ts_nop 3\n\tv_accvgpr_read_b32 v2, a5\n") == []
     assert early_touches(head + product + "\tv_accvgpr_read_b32 v2, a8\n") == []
     assert early_touches(head + product + product) == []
+
+
+def test_the_scan_follows_branches():
+    head = "_ZN4bdlm1fEv:\n"
+    product = "\tv_mfma_f32_16x16x32_bf16 a[4:7], v[8:11], v[12:15], a[4:7]\n"
+    settle, touch = "\ts_nop 15\n\ts_nop 3\n", "\tv_accvgpr_read_b32 v2, a5\n"
+    # what follows an unconditional branch in the text does not follow the product
+    away = head + product + "\ts_branch .LBB0_2\n.LBB0_1:\n" + touch + "\ts_endpgm\n.LBB0_2:\n"
+    assert early_touches(away + settle + touch + "\ts_endpgm\n") == []
+    assert len(early_touches(away + touch + "\ts_endpgm\n")) == 1
+    # a loop's first instruction follows its last, and a conditional branch goes both ways
+    loop = head + ".LBB0_1:\n" + touch + settle + product + "\ts_cbranch_scc1 .LBB0_1\n" + settle + "\ts_endpgm\n"
+    assert len(early_touches(loop)) == 1
+    assert early_touches(loop.replace(touch, settle + touch)) == []
