@@ -89,21 +89,29 @@ struct Shape {
     bool fits = true;   // in one launch (fewer than 2^32 threads)
 };
 bool launch_fits(bool big, int64_t tiles) { return tiles < (big ? int64_t(1) << 23 : int64_t(1) << 24); }
-// The tiles and splits of the least time, as measured: a step of a large tile takes 1.85 us (one
-// workgroup on a CU), of a small one 1.15 (two), or 0.75 alone on its CU, and a tile five or four
-// steps more to begin and to end.  16,384 x 4,096 over 1,024 takes 148 us in large tiles and 200 in
-// small ones, 4,096 x 832 over 1,664 takes 45 and 22.  Partial sums are written and read again
-// at 4 TB/s, by a launch of their own.
-Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split) {
+// The tiles and splits of the least time, as measured: a step of a large tile takes 1.75 us where
+// every CU has one and 1.1 where few have (the clock), two of small tiles on a CU 0.92, one alone
+// 0.38 to 0.52 (a third more where both operands' contraction index is the slow one: twice as many
+// reads from LDS), and a tile 5 to 7 steps more to begin and to end.  16,384 x 4,096 over 1,024 takes
+// 158 us in large tiles and 188 in small ones, 4,096 x 832 over 1,664 takes 43 and 20.  Partial
+// sums are written and read again at 4 TB/s, by a launch of their own: 448 x 1,934 over 16,384
+// takes 110 us whole and 50 in four splits, 512 x 4,384 over 1,024 takes 14 and 24 in two.
+Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split, bool both_slow = false) {
+    const double small = both_slow ? 1.35 : 1.0;
     Shape best{true, 1, false};
     double least = 1e300;
     for (int big = 0; big < 2; ++big) {
-        const int64_t e = tile_edge(big), per = big ? 256 : 512;
+        const int64_t e = tile_edge(big);
         const int64_t tiles = ((nrow + e - 1) / e) * ((ncol + e - 1) / e);
         for (int s = 1; s <= (may_split ? kMostSplits : 1); ++s) {
             if ((s > 1 && steps / s < 4) || !launch_fits(big, tiles * s)) break;
-            const double rounds = double((tiles * s + per - 1) / per);
-            double us = rounds * ((double((steps + s - 1) / s) + (big ? 5.0 : 4.0)) * (big ? 1.85 : tiles * s <= kChip ? 0.75 : 1.15));
+            const double deep = double((steps + s - 1) / s);
+            // whole rounds of the chip, and what is left
+            const int64_t per = big ? kChip : 2 * kChip, left = tiles * s % per;
+            const double share = double(left) / kChip;
+            double us = double(tiles * s / per) * (big ? (deep + 5.0) * 1.75 : (deep + 6.0) * 0.92 * small);
+            if (left) us += big ? (deep + 5.0) * (1.1 + 0.65 * share)
+                                : (share > 1.0 ? (deep + 6.0) * 0.92 : (deep + 7.0) * (0.38 + 0.14 * share)) * small;
             if (s > 1) us += 3.0 + double(s + 1) * nrow * ncol * 4.0 / 4.0e6;
             if (us < least) {
                 least = us;
@@ -231,7 +239,7 @@ struct BackwardPlan {
           w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
         const int32_t np = grad_pairs(grad_terms(d));
         sx = shape_of(d.rows, d.in_features, steps_of(d.out_features, np), true);
-        sw = shape_of(d.out_features, d.in_features, steps_of(d.rows, np), true);
+        sw = shape_of(d.out_features, d.in_features, steps_of(d.rows, np), true, true);
         ld_dz = up(d.out_features, 64);
         dz = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * ld_dz);
         sums = ws.take<float>(int64_t(pack_row_blocks(static_cast<int32_t>(d.rows))) * d.out_features);
@@ -344,7 +352,7 @@ struct LossBackwardPlan {
         const bool big = d.rows > tile_edge(false);
         const int64_t e = tile_edge(big), cols = (d.in_features + e - 1) / e;
         sx = Shape{big, 0, launch_fits(big, (d.rows + e - 1) / e * cols)};
-        sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true);
+        sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true, true);
         p = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * piece);
         // summed over the pieces: what the splits of any number of rows take
         part_x = ws.take<float>(std::max(d.rows, std::min(d.rows * kMostSplits, kChip / std::min<int64_t>(cols, kChip) * e)) * d.in_features);

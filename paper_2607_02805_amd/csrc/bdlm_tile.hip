@@ -279,12 +279,13 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
 // WR x WC waves of (E / WR) x (E / WC) outputs: of 128 x 64 in a tile of 256, of 64 x 64 in one of
 // 128, where KS = 2 such sets of waves take half of a stage's contraction each and add up at the
 // end.  (With one set a SIMD has a wave too few: instructions come at most every four cycles from a
-// wave, some ten a product, and a product takes 32.  512 x 1,024 x 4,384 takes 14.8 us instead of
+// wave, some ten a product, and a product takes 32.  512 x 1,024 x 4,384 takes 14.5 us instead of
 // 17.1, 1,500 x 832 x 16,001 in fp32 276 instead of 286.  Large tiles have two waves a SIMD, and no
-// registers for more.)  A stage is groups of products, four or a wave's two, each from one of two sets of registers while the other
-// fills with the next group's operands from LDS.  With the last group's operands read, and the
-// next stage arrived in its buffer, the waves meet; then the stage that takes this buffer over is
-// copied into it, from the last group through the next stage's first two.
+// registers for more.)  A stage is four groups of products, or a wave's two of them, each from one
+// of two sets of registers while the other fills with the next group's operands from LDS.  With
+// the last group's operands read, and the next stage arrived in its buffer, the waves meet; then the
+// stage that takes this buffer over is copied into it, from the last group on and through the next
+// stage's first.
 //
 // E 256: two waves on each SIMD, 128 accumulators a lane.  E 128 with two buffers: two workgroups on
 // a CU, so that one's epilogue meets the other's products.
@@ -564,7 +565,8 @@ hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
     return hipGetLastError();
 }
 
-// out = epilogue(sum of the slices), four columns per thread
+// out = epilogue(sum of the slices), four columns per thread; four slices are asked for at a time
+// (one after the other, 128 x 1,024 in 16 slices took 4 us more)
 __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int splits, int edge, int nrow, int ncol,
                                                         const int32_t *nrow_dev, const StoreArgs s) {
     const int quads = (ncol + 3) / 4;
@@ -577,7 +579,15 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
         const float *p = part + r * ncol + c;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
         if (ncol % 4 == 0) {
-            for (int k = 0; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(p + k * slice);
+            int k = 0;
+            for (; k + 4 <= splits; k += 4) {
+                f32x4 u[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const f32x4 *>(p + (k + j) * slice);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v += u[j];
+            }
+            for (; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(p + k * slice);
         } else {
             for (int k = 0; k < splits; ++k)
                 for (int e = 0; e < 4; ++e)
