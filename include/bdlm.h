@@ -522,8 +522,9 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t
  * The backward takes dloss, the gradient of the result by each row's loss (the block
  * objective's weights), and the forward call's loss and lse:
  *     dx = P w,  dw = P^T x,  P = dloss * (softmax - onehot(label)),
- * forming the logits again in pieces of the vocabulary.  With bf16 inputs P is rounded as dz
- * is there.  dx, dw in_dtype, shaped as x and w, or NULL (not wanted).  rows == 0 zeroes dw.
+ * forming the logits again in pieces of the vocabulary.  With bf16 inputs and more than 64 rows P
+ * is rounded to bf16, each row as a multiple of its label's entry, and for dw so is that entry times
+ * the row of x (of fewer rows two bf16 terms of P are kept).  dx, dw in_dtype, shaped as x and w, or NULL (not wanted).  rows == 0 zeroes dw.
  * Errors: as bdlm_projection; BDLM_E_SHAPE where exclude is the vocabulary's only token.
  */
 int bdlm_head_loss_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);

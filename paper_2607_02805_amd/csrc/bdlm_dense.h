@@ -50,6 +50,11 @@ struct BestArgs {
     int32_t ntile, exclude;
 };
 
+// Of one bf16 term, a row of the logits' gradients is divided by its label's entry: that one, which
+// outweighs the others, is 1 and loses nothing.  The divisor (RowsArgs' scale) multiplies dx's row in
+// fp32, and x's row, rounded to bf16 element by element, in dw's product.  (Rounded as it
+// was, the label's entry put one error on a whole row of dx: 0.0028 over a few rows with
+// large weights, where the rounding of dx itself is 0.0017.)
 struct ProbArgs {
     uint16_t *p;               // [terms][nrow][ld]
     int64_t ld, plane;
@@ -100,8 +105,9 @@ inline int32_t tile_edge(bool big) { return big ? 256 : 128; }
 
 // out = epilogue(sum of the partial slices); splits 0: as many as a tiled product of these sizes
 // made (big: its tiles)
+// scale: a factor of every row, or null
 int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
-                const StoreArgs &s, void *stream);
+                const float *scale, const StoreArgs &s, void *stream);
 
 // Few rows (skinny_rows): the weights stream through once.  x [nrow][k], w [ncol][k], both bf16
 // or both fp32, any stride; out kTileStore or kTileBest (one record per skinny_cols columns).
@@ -130,6 +136,7 @@ struct PackArgs {
     int64_t ld;
     int32_t rows, cols, src_bf16;
     const int32_t *rows_dev, *row_of;
+    const float *scale;        // factors of the rows laid out (a bf16 copy of one term), or null
     uint16_t *dst;
     int64_t ld_dst, plane;
     int32_t terms;
@@ -157,7 +164,7 @@ struct RowsArgs {
     int64_t exclude;
     int32_t *count, *row_of, *label;
     const float *dloss, *loss, *lse;     // null in the forward call
-    float *weight_c, *loss_c, *lse_c;
+    float *weight_c, *loss_c, *lse_c, *scale_c;   // scale: the gradient by the label's logit
 };
 int launch_rows(const RowsArgs &a, void *stream);
 

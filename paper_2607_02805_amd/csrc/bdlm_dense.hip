@@ -1,7 +1,9 @@
 // bdlm_dense.hip -- gfx950 kernels around the products of the dense operators: operands laid out as
 // bf16 terms, the gradient of a projection's activation with the bias gradient's column sums, the
 // rows that count of a masked loss, and the merge of softmax records.  All are bound by the
-// bytes they move, and small beside the products they serve.
+// bytes they move or, of few bytes, by their launch: the gradient of a GELU over 16,384 x 4,096 in
+// bf16 (402 MB) takes 80 to 95 us, 4.2 to 5.0 TB/s; the rows of 8,192 labels 7 to 12 us (one
+// workgroup); 8,192 rows of 197 records 12 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -67,7 +69,7 @@ __device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, const 
 }
 
 // Thread: eight columns of kPackBatch rows at a time, all asked for before any is used (with one row
-// at a time, 1,003 x 1,934 fp32 took 33 us instead of 8); a workgroup takes kPackRows rows of 64 x 8
+// at a time, 1,003 x 1,934 fp32 took 33 us instead of 12); a workgroup takes kPackRows rows of 64 x 8
 // columns with its four waves (row r of every four).  The column sums are of the fp32 values,
 // before they are rounded.
 constexpr int kPackBatch = 4;
@@ -102,6 +104,11 @@ __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
                     float f[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] = v[k].value(e);
+                    if constexpr (!GRAD && BF16 && TERMS == 1) {
+                        const float scale = a.scale && r < rows ? a.scale[r] : 1.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] *= scale;
+                    }
                     if constexpr (GRAD) {
                         if (slope) {
 #pragma unroll
@@ -181,6 +188,8 @@ __global__ void __launch_bounds__(1024) bdlm_rows_kernel(const RowsArgs a) {
                 a.weight_c[to] = a.dloss[r];
                 a.loss_c[to] = a.loss[r];
                 a.lse_c[to] = a.lse[r];
+                // the label's probability less one is exp(-loss) - 1, without cancellation
+                a.scale_c[to] = a.dloss[r] * expm1f(-a.loss[r]);
             }
         }
         base += all;

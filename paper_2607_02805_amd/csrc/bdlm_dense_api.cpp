@@ -143,7 +143,8 @@ struct Operand {
             mat = Mat{copy, w, up(r, 64) * w};
         }
     }
-    int lay(void *stream, const int32_t *row_of = nullptr, const int32_t *rows_dev = nullptr) const {
+    int lay(void *stream, const int32_t *row_of = nullptr, const int32_t *rows_dev = nullptr,
+            const float *scale = nullptr) const {
         if (direct) return BDLM_OK;
         PackArgs a{};
         a.src = src;
@@ -153,6 +154,7 @@ struct Operand {
         a.src_bf16 = dtype == BDLM_DTYPE_BF16;
         a.rows_dev = rows_dev;
         a.row_of = row_of;
+        a.scale = scale;
         a.dst = copy;
         a.ld_dst = mat.ld;
         a.plane = mat.plane;
@@ -197,7 +199,7 @@ int store_product(TileArgs a, const StoreArgs &s, float *part, void *stream) {
     a.out = kTilePartial;
     a.part = part;
     const int rc = launch_tile(a, stream);
-    return rc != BDLM_OK ? rc : launch_join(part, a.splits, a.big, a.nrow, a.ncol, a.nrow_dev, s, stream);
+    return rc != BDLM_OK ? rc : launch_join(part, a.splits, a.big, a.nrow, a.ncol, a.nrow_dev, nullptr, s, stream);
 }
 int64_t part_size(const Shape &s, int64_t nrow, int64_t ncol) { return s.splits > 1 ? s.splits * nrow * ncol : 0; }
 
@@ -252,16 +254,17 @@ struct BackwardPlan {
 // The rows that count of a masked loss.
 struct Rows {
     int32_t *count, *row_of, *label;
-    float *weight, *loss, *lse;
+    float *weight, *loss, *lse, *scale;
     Rows(int64_t n, bool backward, Space &ws) {
         count = ws.take<int32_t>(1);
         row_of = ws.take<int32_t>(n);
         label = ws.take<int32_t>(n);
-        weight = loss = lse = nullptr;
+        weight = loss = lse = scale = nullptr;
         if (!backward) return;
         weight = ws.take<float>(n);
         loss = ws.take<float>(n);
         lse = ws.take<float>(n);
+        scale = ws.take<float>(n);
     }
 };
 
@@ -332,14 +335,17 @@ struct LossPlan {
 struct LossBackwardPlan {
     Space ws;
     Rows rows;
-    Operand x, w;
+    bool scaled;               // the rows of P are divided by their labels' entries
+    Operand x, w, xs;          // xs: x times what they were divided by
     int64_t piece;
     Shape sp, sx, sw;
     uint16_t *p;
     float *part_x, *part_w;
     LossBackwardPlan(const bdlm_dense_desc_t &d, const void *px, const void *pw, void *mem)
-        : ws(mem), rows(d.rows, true, ws), x(px, d.rows, d.in_features, d.x_stride, d.in_dtype, true, ws),
-          w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
+        : ws(mem), rows(d.rows, true, ws), scaled(grad_terms(d) == 1),
+          x(px, d.rows, d.in_features, d.x_stride, d.in_dtype, true, ws),
+          w(pw, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
+          xs(px, scaled ? d.rows : 0, d.in_features, d.x_stride, d.in_dtype, true, ws) {
         const int32_t np = grad_pairs(grad_terms(d));
         const int64_t per = std::max<int64_t>(d.rows, 1) * 2 * grad_terms(d);
         piece = std::max<int64_t>((int64_t(512) << 20) / per / 256 * 256, 4096);
@@ -584,7 +590,7 @@ int bdlm_head_loss(const bdlm_dense_desc_t *d, const int64_t *labels, int64_t ex
     const int32_t rows = static_cast<int32_t>(d->rows), vocab = static_cast<int32_t>(d->out_features);
     const int32_t none = token_or_none(d, exclude);
     TRY(launch_rows(RowsArgs{labels, rows, vocab, exclude, p.rows.count, p.rows.row_of, p.rows.label, nullptr,
-                             nullptr, nullptr, nullptr, nullptr, nullptr},
+                             nullptr, nullptr, nullptr, nullptr, nullptr, nullptr},
                     stream));
     const BestArgs best{p.rec.top, p.rec.others, p.rec.at, p.label_logit, p.rows.label, p.rec.ntile, none};
     if (p.skinny) {
@@ -639,10 +645,11 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
     const int32_t none = token_or_none(d, exclude), terms = grad_terms(*d), np = grad_pairs(terms);
     const int64_t K = d->in_features;
     TRY(launch_rows(RowsArgs{labels, rows, vocab, exclude, p.rows.count, p.rows.row_of, p.rows.label, dloss, loss,
-                             lse, p.rows.weight, p.rows.loss, p.rows.lse},
+                             lse, p.rows.weight, p.rows.loss, p.rows.lse, p.rows.scale},
                     stream));
     TRY(p.x.lay(stream, p.rows.row_of, p.rows.count));
     TRY(p.w.lay(stream));
+    if (dw) TRY(p.xs.lay(stream, p.rows.row_of, p.rows.count, p.rows.scale));   // (of no rows: nothing)
     const Mat pm{p.p, p.piece, up(rows, 64) * p.piece};
     for (int64_t v0 = 0; v0 < vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, vocab - v0);
@@ -665,7 +672,7 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
             TRY(launch_tile(b, stream));
         }
         if (dw) {
-            TileArgs c = product(pm, true, p.x.mat, true, n, K, rows, np, p.sw);
+            TileArgs c = product(pm, true, p.scaled ? p.xs.mat : p.x.mat, true, n, K, rows, np, p.sw);
             c.k_dev = p.rows.count;
             TRY(store_product(c, plain_store(static_cast<char *>(dw) + v0 * dw_stride * elem_size(d->in_dtype),
                                              dw_stride, d->in_dtype),
@@ -675,7 +682,8 @@ int bdlm_head_loss_backward(const bdlm_dense_desc_t *d, const int64_t *labels, i
     if (dx) {
         StoreArgs s = plain_store(dx, dx_stride, d->in_dtype);
         s.row_of = p.rows.row_of;
-        TRY(launch_join(p.part_x, 0, p.sx.big, rows, static_cast<int32_t>(K), p.rows.count, s, stream));
+        TRY(launch_join(p.part_x, 0, p.sx.big, rows, static_cast<int32_t>(K), p.rows.count,
+                        p.scaled ? p.rows.scale : nullptr, s, stream));
         TRY(launch_zero_rows(labels, exclude, vocab, rows, dx, dx_stride, static_cast<int32_t>(K),
                              d->in_dtype == BDLM_DTYPE_BF16, stream));
     }

@@ -342,9 +342,10 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             const int64_t r = row0 + x;
             RowData d{INFINITY, 0.f, 0.f, -1};
             if (r < nrow) {
-                const float g = b.weight[r];
-                // the label's probability less one is exp(-loss) - 1, without cancellation
-                d = RowData{b.lse[r], g, g * expm1f(-b.loss[r]), b.label[r] - b.col0};
+                const float g = b.weight[r], rest = expm1f(-b.loss[r]);   // the label's probability less one
+                d = RowData{b.lse[r], g, g * rest, b.label[r] - b.col0};
+                // one term: divided by the label's entry (where that is 0, the row's factor is as well)
+                if (b.terms == 1) d = RowData{rest == 0.f ? INFINITY : d.lse + logf(-rest), -1.f, 1.f, d.label};
             }
             rows[x] = d;
         }
@@ -568,7 +569,7 @@ hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
 // out = epilogue(sum of the slices), four columns per thread; four slices are asked for at a time
 // (one after the other, 128 x 1,024 in 16 slices took 4 us more)
 __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int splits, int edge, int nrow, int ncol,
-                                                        const int32_t *nrow_dev, const StoreArgs s) {
+                                                        const int32_t *nrow_dev, const float *scale, const StoreArgs s) {
     const int quads = (ncol + 3) / 4;
     const int64_t rows = nrow_dev ? *nrow_dev : nrow;
     const int64_t slice = (splits ? int64_t(nrow) : rows) * ncol;
@@ -593,6 +594,7 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
                 for (int e = 0; e < 4; ++e)
                     if (c + e < ncol) v[e] += p[k * slice + e];
         }
+        if (scale) v *= scale[r];
         store4(s, v, load_bias(s, c, ncol), r, c, ncol);
     }
 }
@@ -625,12 +627,12 @@ int launch_tile(const TileArgs &a, void *stream) {
 }
 
 int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
-                const StoreArgs &s, void *stream) {
+                const float *scale, const StoreArgs &s, void *stream) {
     if (nrow <= 0 || ncol <= 0) return BDLM_OK;
     const int64_t blocks = (int64_t(nrow) * ((ncol + 3) / 4) + 255) / 256;
     const dim3 g(static_cast<unsigned>(blocks < 8192 ? blocks : 8192));
     hipLaunchKernelGGL(bdlm_join_kernel, g, dim3(256), 0, static_cast<hipStream_t>(stream), part, splits,
-                       tile_edge(big), nrow, ncol, nrow_dev, s);
+                       tile_edge(big), nrow, ncol, nrow_dev, scale, s);
     return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }
 

@@ -129,9 +129,14 @@ def head_loss_backward64(dloss, x, w, labels, exclude=-1):
         dp = dp + U[ty] * (P.abs() + dp)
     x, w = rows2(d64(x)), d64(w)
     m, n = P.shape
+    dpw = dp
+    if ty == torch.bfloat16 and m > 64:
+        # dw's product is of P / h and h x, h the label's entry, each rounded to half a step u: together
+        # (1 + u)^2 - 1 = 2 u + u^2 of a product (the label's own, of 1 and h x, less), u of it is in dp
+        dpw = dp + (U[ty] + U[ty] ** 2) * (P.abs() + dp)
     dx, dw = P @ w, P.t() @ x
     ex = (dp + (n + 8) * F * P.abs()) @ w.abs()
-    ew = (dp + (m + 8) * F * P.abs()).t() @ x.abs()
+    ew = (dpw + (m + 8) * F * P.abs()).t() @ x.abs()
     return (dx, ex + U[ty] * (dx.abs() + ex) + 1e-37), (dw, ew + U[ty] * (dw.abs() + ew) + 1e-37)
 
 

@@ -351,6 +351,32 @@ def test_excluded_token_has_no_part(dtype):
         assert bool(torch.isfinite(got[1][4]).all()) and bool((got[1][5][exclude] == 0).all())
 
 
+@pytest.mark.parametrize("m,counted", [(100, [7]), (100, [0, 99]), (1000, [500])])
+def test_few_counted_rows_keep_their_labels_entry(m, counted):
+    """One or two rows that count among many, bf16: the label's entry h of the logits' gradients is just
+    off a bf16 value by 0.98 of half a step.  Rounded, it would shift all of a row of dx and of dw
+    by 2^-8 of it.  Compared with the 64-bit values rounded to bf16, as h x of bf16 x for h near 1
+    is itself rounded with a mean (towards 0 up to a mantissa of 1 / 0.98, away from there on, 0.0016
+    in all): what is left is an element in some that rounds the other way, by a step of 2^-7 at most,
+    at random.  Were it all of the K = 512, their mean would be 2^-7 / sqrt(3 K) = 2^-7 / 39,
+    a fifth of the bound."""
+    import paper_2607_02805_amd as bd
+    r = gen(29)
+    n, k = 3000, 512
+    x, w = r(m, k).to(BF).to(DEV), (r(n, k) / 40).to(BF).to(DEV)
+    labels = torch.full((m,), -100, device=DEV)
+    for i, row in enumerate(counted):
+        labels[row] = 11 + i
+    loss, lse = bd.head_loss(x, w, labels)
+    dloss = (1 + 0.98 * 2.0 ** -8) / torch.where(labels >= 0, -torch.expm1(-loss), 1.0)
+    dx, dw = bd.head_loss_backward(dloss, x, w, labels, loss, lse)
+    (rx, _), (rw, _) = du.head_loss_backward64(dloss, x, w, labels)
+    for i, row in enumerate(counted):
+        for got, ref in ((dx[row], rx[row]), (dw[11 + i], rw[11 + i])):
+            got, ref = got.double().cpu(), ref.to(BF).double()
+            assert abs(float(got @ ref / (ref @ ref)) - 1) < 2.0 ** -10
+
+
 def test_activations_far_out():
     """Pre-activations of 1e4 and more, both ways, and infinities: values and slopes are the limits."""
     import paper_2607_02805_amd as bd
