@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
                     if constexpr (GRAD) {
                         if (slope) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] = r < rows && e < n ? f[e] * act_slope(z[k].value(e), a.act) : 0.f;
+                            for (int e = 0; e < 8; ++e) f[e] = r < rows && e < n ? f[e] * act_slope<!PRE16>(z[k].value(e), a.act) : 0.f;
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) sum[e] += f[e];

@@ -23,19 +23,49 @@ __device__ __forceinline__ void split_terms(float v, uint16_t (&t)[3]) {
     t[2] = static_cast<uint16_t>(bf16_bits(r1 - bf16_to_f32(static_cast<short>(t[1]))));
 }
 
-// The normal distribution's Phi(z), off by at most 3e-7, and e = exp(-z^2 / 2): with x = |z| / sqrt 2,
-// erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x) (Abramowitz and Stegun 7.1.26), on
-// the hardware's reciprocal and exponential.  The library's erfc costs three times as much, which
-// shows where a tile's epilogue is not hidden behind products.
+// The normal distribution's Phi(z) and e = exp(-z^2 / 2) on the hardware's reciprocal and exponential.
+// Phi(-a) = e R(t), t = 1 / (1 + p a), where R(t) = t (c0 + c1 t + ..) stands for erfcx(a / sqrt 2) / 2, which is
+// smooth in t over 0 <= a <= 14; the polynomials are minimax fits made for this file.
+// FINE, for what is kept in fp32: R's relative error stays below 4e-8, t is improved by a Newton step and e by
+// the part of -z^2 / 2 that fp32 drops, so that Phi(z) is off by at most 4e-7 of itself, the tail included (emulated
+// over 50,001 points; GELU of normal z by 3.7e-8, as with a correctly rounded erf near 0).
+// Otherwise, for values that are rounded to bf16 (half a step is 3.9e-3) and slopes at a z that was (which moves
+// Phi(z) by up to z^2 2^-8 of itself in the tail): a polynomial of degree 5, off by 1e-7 and in the tail by 2.9e-4 of
+// itself; GELU is off by 2.5e-7 |z| at most, also where a residual cancels it.
+template <bool FINE>
 __device__ __forceinline__ float normal_cdf(float z, float &e) {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-    e = __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2e));
-    // half of erfc
-    const float h = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f),
-                                     0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
+    const float a = FINE ? fminf(fabsf(z), 14.5f) : fabsf(z);   // (finite, as q is subtracted from itself)
+    const float d = fmaf(FINE ? 0.42426407f : 0.28284271f, a, 1.f);
+    float t = __builtin_amdgcn_rcpf(d), r;
+    const float q = a * a, y = q * (-0.5f * kLog2e);
+    e = __builtin_amdgcn_exp2f(y);
+    if constexpr (FINE) {
+        t = fmaf(t, fmaf(-d, t, 1.f), t);
+        // what y lacks of -z^2 log2(e) / 2: the roundings of q and y, and the constant's
+        constexpr float rest = static_cast<float>(-0.5 * 1.4426950408889634 - double(-0.5f * kLog2e));
+        const float lack = fmaf(fmaf(a, a, -q), -0.5f * kLog2e, fmaf(q, rest, fmaf(q, -0.5f * kLog2e, -y)));
+        e = fmaf(e, lack * 0.69314718f, e);
+        r = fmaf(t, 0.03233261f, -0.15625919f);
+        r = fmaf(t, r, 0.27504578f);
+        r = fmaf(t, r, -0.16007753f);
+        r = fmaf(t, r, -0.068789035f);
+        r = fmaf(t, r, 0.032218184f);
+        r = fmaf(t, r, 0.066111073f);
+        r = fmaf(t, r, 0.14113246f);
+        r = fmaf(t, r, 0.16901903f);
+        r = fmaf(t, r, 0.16926664f);
+    } else {
+        r = fmaf(t, -0.096094035f, 0.338998735f);
+        r = fmaf(t, r, -0.161798224f);
+        r = fmaf(t, r, 0.216511309f);
+        r = fmaf(t, r, 0.087330155f);
+        r = fmaf(t, r, 0.115052164f);
+    }
+    const float h = t * r * e;
     return z > 0.f ? 1.f - h : h;
 }
 // Values and slopes at infinities are the limits; a NaN stays one.
+template <bool FINE>
 __device__ __forceinline__ float act_value(float z, int act) {
     if (act == BDLM_ACT_SILU) {
         const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
@@ -43,12 +73,13 @@ __device__ __forceinline__ float act_value(float z, int act) {
     }
     if (act == BDLM_ACT_GELU) {
         float e;
-        const float p = normal_cdf(z, e);
+        const float p = normal_cdf<FINE>(z, e);
         return z < -14.f ? 0.f : z * p;
     }
     return z;
 }
 // d act / dz
+template <bool FINE>
 __device__ __forceinline__ float act_slope(float z, int act) {
     if (act == BDLM_ACT_SILU) {
         const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
@@ -56,7 +87,7 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     }
     if (act == BDLM_ACT_GELU) {
         float e;
-        const float p = normal_cdf(z, e);
+        const float p = normal_cdf<FINE>(z, e);
         return z < -14.f ? 0.f : z > 14.f ? 1.f : fmaf(z * 0.39894228f, e, p);
     }
     return 1.f;
