@@ -100,6 +100,7 @@ inline int32_t split_count(int64_t tiles) {
     const int64_t s = tiles > 0 ? kChip / tiles : 1;
     return static_cast<int32_t>(s < 1 ? 1 : s > kMostSplits ? kMostSplits : s);
 }
+constexpr int32_t kTileThreads = 512;   // of a workgroup, whatever its tile
 // Columns of a tile (what kTileBest's ntile counts).
 inline int32_t tile_edge(bool big) { return big ? 256 : 128; }
 

@@ -88,7 +88,7 @@ struct Shape {
     int32_t splits;
     bool fits = true;   // in one launch (fewer than 2^32 threads)
 };
-bool launch_fits(bool big, int64_t tiles) { return tiles < (big ? int64_t(1) << 23 : int64_t(1) << 24); }
+bool launch_fits(int64_t tiles) { return tiles * kTileThreads < int64_t(1) << 32; }
 // The tiles and splits of the least time, as measured: a step of a large tile takes 1.75 us where
 // every CU has one and 1.1 where few have (the clock), two of small tiles on a CU 0.92, one alone
 // 0.38 to 0.52 (a third more where both operands' contraction index is the slow one: twice as many
@@ -104,7 +104,7 @@ Shape shape_of(int64_t nrow, int64_t ncol, int64_t steps, bool may_split, bool b
         const int64_t e = tile_edge(big);
         const int64_t tiles = ((nrow + e - 1) / e) * ((ncol + e - 1) / e);
         for (int s = 1; s <= (may_split ? kMostSplits : 1); ++s) {
-            if ((s > 1 && steps / s < 4) || !launch_fits(big, tiles * s)) break;
+            if ((s > 1 && steps / s < 4) || !launch_fits(tiles * s)) break;
             const double deep = double((steps + s - 1) / s);
             // whole rounds of the chip, and what is left
             const int64_t per = big ? kChip : 2 * kChip, left = tiles * s % per;
@@ -357,7 +357,7 @@ struct LossBackwardPlan {
         // (few rows: the small tile, half of which they would leave empty in the large one)
         const bool big = d.rows > tile_edge(false);
         const int64_t e = tile_edge(big), cols = (d.in_features + e - 1) / e;
-        sx = Shape{big, 0, launch_fits(big, (d.rows + e - 1) / e * cols)};
+        sx = Shape{big, 0, launch_fits((d.rows + e - 1) / e * cols)};
         sw = shape_of(piece, d.in_features, steps_of(d.rows, np), true, true);
         p = ws.take<uint16_t>(grad_terms(d) * up(d.rows, 64) * piece);
         // summed over the pieces: what the splits of any number of rows take

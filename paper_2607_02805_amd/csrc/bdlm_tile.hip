@@ -291,6 +291,7 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
 // a CU, so that one's epilogue meets the other's products.
 template <int E, int WR, int WC, int KS, int BUFS, bool ROWT, bool COLT, int OUT>
 __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) bdlm_tile_kernel(const TileArgs a) {
+    static_assert(64 * WR * WC * KS == kTileThreads, "what the launch has, and the host's check counts on");
     constexpr int WAVES = WR * WC * KS, kWaveGroups = kGroups / KS, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
     constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's stage
     constexpr int kRec = OUT == kTileBest ? E : 1;
@@ -559,10 +560,10 @@ template <bool ROWT, bool COLT, int OUT>
 hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
     // Small tiles that leave a CU one workgroup take four buffers, so that copies have three stages to
     // arrive (a stage of theirs is 512 cycles of products).
-    if (a.big) hipLaunchKernelGGL((bdlm_tile_kernel<256, 2, 4, 1, 2, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
+    if (a.big) hipLaunchKernelGGL((bdlm_tile_kernel<256, 2, 4, 1, 2, ROWT, COLT, OUT>), g, dim3(kTileThreads), 0, s, a);
     else if (g.x <= static_cast<unsigned>(kChip))
-        hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, 4, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, 2, ROWT, COLT, OUT>), g, dim3(512), 0, s, a);
+        hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, 4, ROWT, COLT, OUT>), g, dim3(kTileThreads), 0, s, a);
+    else hipLaunchKernelGGL((bdlm_tile_kernel<128, 2, 2, 2, 2, ROWT, COLT, OUT>), g, dim3(kTileThreads), 0, s, a);
     return hipGetLastError();
 }
 
