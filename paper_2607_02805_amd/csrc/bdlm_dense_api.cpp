@@ -22,15 +22,19 @@ int64_t elem_size(int32_t dt) { return dt == BDLM_DTYPE_BF16 ? 2 : 4; }
 bool known(int32_t dt) { return dt == BDLM_DTYPE_F32 || dt == BDLM_DTYPE_BF16; }
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// The memory of rows x cols elements with a row stride: `row` bytes every `ld`, `bytes` in all.
+// The memory of rows x cols elements with a row stride: `row` bytes every `ld`, `bytes` in all (unsigned: the largest
+// rows and strides come to a little less than 2^64).
 struct Span {
     uintptr_t p, bytes, row, ld;
     Span(const void *q, int64_t rows, int64_t cols, int64_t stride, int64_t es)
         : p(reinterpret_cast<uintptr_t>(q)),
-          bytes(q && rows > 0 && cols > 0 ? static_cast<uintptr_t>(((rows - 1) * stride + cols) * es) : 0),
+          bytes(q && rows > 0 && cols > 0
+                    ? (static_cast<uintptr_t>(rows - 1) * static_cast<uintptr_t>(stride) + static_cast<uintptr_t>(cols)) *
+                          static_cast<uintptr_t>(es)
+                    : 0),
           row(static_cast<uintptr_t>(cols * es)), ld(static_cast<uintptr_t>(stride * es)) {}
     bool meets(const Span &o) const {
-        if (!bytes || !o.bytes || p >= o.p + o.bytes || o.p >= p + bytes) return false;
+        if (!bytes || !o.bytes || (o.p >= p ? o.p - p >= bytes : p - o.p >= o.bytes)) return false;
         if (ld != o.ld || ld == 0) return true;
         // column slices of one matrix: apart if the other's columns lie between this one's rows
         const uintptr_t at = o.p >= p ? (o.p - p) % ld : (ld - (p - o.p) % ld) % ld;

@@ -200,3 +200,16 @@ def test_python_refusals():
                         (lambda: bd.head_select(x, w, token=torch.zeros(3)), "token")):
         with pytest.raises(ValueError, match=match):
             call()
+
+
+def test_overlaps_of_the_widest_matrices():
+    """2^22 rows 2^40 elements apart reach past 2^63 bytes: what lies between them is still seen."""
+    far = desc(rows=1 << 22, k=64, n=130, dtype=bd.DTYPE_F32, x_stride=1 << 40)
+    assert projection(far, x=X) == bd.E_SHAPE                             # out, pre: above x's first row
+    assert projection(far, x=DY) == bd.OK                                 # all below it
+    assert projection(far, x=DY, out=DY + A) == bd.E_SHAPE
+    assert select(far, x=X) == bd.E_SHAPE and select(far, x=DY) == bd.OK
+    assert select(far, x=DY, token=DY + A) == bd.E_SHAPE and select(far, x=DY, ws=DY + A) == bd.E_WORKSPACE
+    d = desc(rows=1 << 22, k=64, n=130, dtype=bd.DTYPE_F32)
+    assert projection(d, res=DY, ldr=1 << 40) == bd.OK
+    assert projection(d, res=DY, ldr=1 << 40, out=DY + A) == bd.E_SHAPE
