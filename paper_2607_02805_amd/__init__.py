@@ -895,6 +895,12 @@ def _dense_call(name: str, d, device, workspace, args):
         raise BdlmError(rc, "bdlm_" + name)
 
 
+def _token(exclude, d) -> int:
+    """``exclude`` for the C call: -1 for any number that is no token (it may not fit 64 bits)."""
+    token = int(exclude)
+    return token if 0 <= token < d.out_features else -1
+
+
 def _p(t):
     return None if t is None or t.numel() == 0 else t.data_ptr()
 
@@ -1006,7 +1012,7 @@ def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, worksp
     loss = _vector(_place(loss, lead, torch.float32, x.device, "loss"), lead, torch.float32, x.device, "loss")
     lse = _vector(_place(lse, lead, torch.float32, x.device, "lse"), lead, torch.float32, x.device, "lse")
     _dense_call("head_loss", d, x.device, workspace,
-                (_p(labels), int(exclude), _p(x), _p(w), _p(loss), _p(lse)))
+                (_p(labels), _token(exclude, d), _p(x), _p(w), _p(loss), _p(lse)))
     return loss, lse
 
 
@@ -1037,7 +1043,7 @@ def head_loss_backward(dloss, x, w, labels, loss, lse, exclude=-1, dx=True, dw=T
         dw = _place(dw, w.shape, w.dtype, x.device, "dw")
         _, ldw = _rows2d(dw, d.in_features, "dw")
     _dense_call("head_loss_backward", d, x.device, workspace,
-                (_p(labels), int(exclude), _p(x), _p(w), _p(loss), _p(lse), _p(dloss), _p(dx), ldx, _p(dw), ldw))
+                (_p(labels), _token(exclude, d), _p(x), _p(w), _p(loss), _p(lse), _p(dloss), _p(dx), ldx, _p(dw), ldw))
     return dx, dw
 
 
@@ -1057,7 +1063,7 @@ def head_select(x, w, exclude=-1, token=None, logprob=None, stream=None, workspa
     logprob = _vector(_place(logprob, lead, torch.float32, x.device, "logprob"), lead, torch.float32, x.device,
                       "logprob")
     _dense_call("head_select", d, x.device, workspace,
-                (int(exclude), _p(x), _p(w), _p(token), _p(logprob)))
+                (_token(exclude, d), _p(x), _p(w), _p(token), _p(logprob)))
     return token, logprob
 
 

@@ -213,3 +213,18 @@ def test_overlaps_of_the_widest_matrices():
     d = desc(rows=1 << 22, k=64, n=130, dtype=bd.DTYPE_F32)
     assert projection(d, res=DY, ldr=1 << 40) == bd.OK
     assert projection(d, res=DY, ldr=1 << 40, out=DY + A) == bd.E_SHAPE
+
+
+@pytest.mark.parametrize("exclude", [-1, 5, 4, 0, 2 ** 64, 2 ** 64 + 3, -2 ** 64 + 3, 2 ** 63, -2 ** 63 - 1, 2 ** 40])
+def test_any_integer_may_be_excluded(monkeypatch, exclude):
+    """A token past the vocabulary is none of it, however large: it does not come out as another one."""
+    seen = []
+    monkeypatch.setattr(bd, "_dense_call", lambda name, d, device, workspace, args: seen.append(args))
+    x, w, v = torch.zeros(3, 8), torch.zeros(5, 8), torch.zeros(3)
+    labels = torch.zeros(3, dtype=torch.int64)
+    bd.head_select(x, w, exclude=exclude)
+    bd.head_loss(x, w, labels, exclude=exclude)
+    bd.head_loss_backward(v, x, w, labels, v, v, exclude=exclude)
+    for args, at in zip(seen, (0, 1, 1)):
+        got = ctypes.c_int64(args[at]).value
+        assert got == exclude if 0 <= exclude < 5 else not 0 <= got < 5, (args, got)
