@@ -914,6 +914,9 @@ def projection(x, w, bias=None, act=None, residual=None, out=None, pre=None, str
     bfloat16 or float32) and ``residual`` (out's dtype; may be ``out`` itself) are
     [..., out_features].  ``pre`` keeps x w^T + bias in x's dtype for the gradient: None (no),
     True (allocate) or a tensor.  Returns out, or (out, pre) if ``pre`` was asked for.
+
+    No autograd graph is recorded, whatever requires gradients: :func:`projection_backward` has them.
+    In float32, where operands are multiplied as bfloat16 terms, an infinity may come out as NaN.
     """
     if stream is not None:
         with _on(stream, x):
@@ -954,6 +957,9 @@ def projection_backward(dy, x, w, pre=None, act=None, dx=True, dw=True, db=None,
     the forward call kept (needed with an activation).  ``dx``, ``dw``, ``db``: True
     (allocate), None (not wanted) or a tensor; dx and dw have x's dtype, db is float32.
     The residual's gradient is dy.
+
+    With bfloat16 inputs and more than 64 rows ``dy * act'(pre)`` is rounded to bfloat16 for dx and dw (relative errors
+    of 0.0023, of which the outputs' own rounding makes 0.0017); float32 inputs keep it to 24 bits.
     """
     if stream is not None:
         with _on(stream, x):
@@ -998,8 +1004,9 @@ def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, worksp
     ``lse = logsumexp(x w^T)`` over the tokens but ``exclude``, ``loss = lse - logit of the label``.
 
     ``labels`` int64.  A row whose label is not a token that the softmax ranges over (negative, past
-    the vocabulary, or ``exclude``) is left out: its loss and lse are 0.  The logits are never
-    in memory."""
+    the vocabulary, or ``exclude``) is left out: its loss and lse are 0.  An ``exclude`` that is no token leaves
+    none out.  The logits are never in memory.  No autograd graph is recorded:
+    :func:`head_loss_backward` has the gradients."""
     if stream is not None:
         with _on(stream, x):
             return head_loss(x, w, labels, exclude, loss, lse, workspace=workspace)
@@ -1022,7 +1029,11 @@ def head_loss_backward(dloss, x, w, labels, loss, lse, exclude=-1, dx=True, dw=T
 
     ``dloss`` float32 is the gradient of the result by each row's loss (the weights of the block
     objective); ``loss`` and ``lse`` are what :func:`head_loss` returned for the same x, w,
-    labels and exclude.  ``dx``, ``dw``: True (allocate), None (not wanted) or a tensor."""
+    labels and exclude.  ``dx``, ``dw``: True (allocate), None (not wanted) or a tensor.
+
+    With bfloat16 inputs and more than 64 rows the logits' gradients are rounded to bfloat16, and for dw so are the
+    rows of x times their labels' entries (relative errors of 0.0019 to 0.0024, of which the outputs' own
+    rounding makes 0.0017); float32 inputs keep them to 24 bits."""
     if stream is not None:
         with _on(stream, x):
             return head_loss_backward(dloss, x, w, labels, loss, lse, exclude, dx, dw, workspace=workspace)

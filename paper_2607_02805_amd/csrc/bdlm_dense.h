@@ -124,7 +124,8 @@ struct SkinnyArgs {
 };
 // Above that many rows the tiles are faster: over 50,257 columns of 1,024 in bf16, 32 rows take 34
 // us here and 29 there, 64 rows 54 and 34, but over 4,384 of them 32 rows take 9 and 11; in fp32,
-// where the tiles lay the weights out anew, 64 rows take 110 and 215.
+// where the tiles lay the weights out anew, 64 rows take 110 and 215.  One limit for every width: it costs the widest
+// calls of nearly 32 bf16 rows a sixth and saves the narrow ones as much.
 inline int32_t skinny_rows(bool bf16) { return bf16 ? 32 : 64; }
 // Columns of a workgroup: fewer where there are not two workgroups for every CU.
 inline int32_t skinny_cols(int64_t ncol) { return ncol >= 32 * 512 ? 32 : 16; }

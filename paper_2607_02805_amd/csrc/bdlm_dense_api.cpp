@@ -184,8 +184,10 @@ TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, int64_t
     return a;
 }
 // Terms of a gradient's first operand (dz, or the logits' gradients).  With bf16 inputs they are
-// rounded to bf16, as the activations of the forward products are; of few rows, where an
-// output's errors do not average out and the weights' bytes bound the products, two terms are kept.
+// rounded to bf16, as the activations of the forward products are: the outputs of 16,384 x 1,024 x 4,096 are then
+// off by 0.0023 of their size, where their own rounding makes 0.0017 of it, and a second term would double both
+// products (277 of 352 us).  Of few rows, where an output's errors do not average out and the weights' bytes
+// bound the products, two terms are kept; fp32 inputs keep three, and are the choice of a caller who needs more.
 int grad_terms(const bdlm_dense_desc_t &d) {
     return d.in_dtype != BDLM_DTYPE_BF16 ? 3 : d.rows <= kFewRows ? 2 : 1;
 }
@@ -332,9 +334,9 @@ struct LossPlan {
     bool fits() const { return skinny || shape.fits; }
 };
 
-// The vocabulary goes in pieces whose logit gradients (rows x piece, bf16 terms) stay within 512 MB:
-// they are written once and read twice, mostly from the memory-side cache where half of the
-// rows count.  The number of rows that count is known on the device alone, so the product over the
+// The vocabulary goes in pieces whose logit gradients (rows x piece, bf16 terms) stay within 512 MB, or have 4,096
+// columns where those take more (bf16 above 65,536 rows, 2^22 rows 34 GB; fp32 above 21,845, 2^22 rows 103 GB): they
+// are written once and read twice, mostly from the memory-side cache where half of the rows count.  The number of rows that count is known on the device alone, so the product over the
 // vocabulary (dx) is split there.
 struct LossBackwardPlan {
     Space ws;

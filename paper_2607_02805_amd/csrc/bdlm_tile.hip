@@ -7,12 +7,12 @@
 // the first MFMA operand, so a lane holds groups of four consecutive columns of one row.
 //
 // Bound by the matrix unit and the clock that it can hold: 8,192 x 8,192 x 8,192 in bf16 takes
-// 900 to 960 us by the card (1,225 to 1,145 TFLOP/s), with the matrix unit busy in 0.76 of the
+// 860 to 960 us by the card (1,280 to 1,145 TFLOP/s), with the matrix unit busy in 0.76 of the
 // cycles and the clock at 1.4 to 2.0 GHz under that load.  A tile of 256 x 256
 // reads a byte of its operands for 128 operations; tiles of 128 x 128 need twice the LDS reads and
 // copies and are for launches that large tiles would leave partly idle.  The epilogue of a large tile is not hidden, as its
-// buffers leave a CU one workgroup: GELU with the pre-activation kept costs 65 of the 216 us of
-// 16,384 x 1,024 x 4,096.
+// buffers leave a CU one workgroup: GELU with the pre-activation kept costs 40 of the 204 us of
+// 16,384 x 1,024 x 4,096 in bf16 (164 without either, 195 with GELU alone).
 // Built and measured slower at 8,192^3: four waves of 128 x 128 (900 to 1,080 us), operands
 // staged through registers, a ring of four stages of 32, a stage's copies all in one group,
 // nontemporal or streaming copies.
