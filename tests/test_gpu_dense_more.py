@@ -266,3 +266,30 @@ def test_activations_keep_their_digits_in_the_tail(act, m):
         off = (db.cpu().double() - slope).abs() / (share * size + 1e-37)
         say(act, m, dtype, "slope: error / bound %.3g" % float(off.max()))
         assert float(off.max()) <= 1.0
+
+
+@pytest.mark.parametrize("m", [1, 70])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_activations_far_out_in_bf16(act, m):
+    """Where squares overflow, and at infinities: values and slopes are the limits, a NaN stays one."""
+    import paper_2607_02805_amd as bd
+    z = torch.tensor([-3e38, -1e30, -1e19, -200.0, -90.0, 0.0, -0.0, 90.0, 200.0, 1e19, 1e30, 3e38,
+                      float("inf"), float("-inf"), float("nan")]).to(BF)
+    n = len(z)
+    x, w = torch.zeros(m, 8, dtype=BF, device=DEV), torch.zeros(n, 8, dtype=BF, device=DEV)
+    right = torch.where(z > 0, z, torch.where(z.isnan(), z, torch.zeros_like(z)))
+    for out_dtype in (BF, F32):
+        out = torch.empty(m, n, dtype=out_dtype, device=DEV)
+        bd.projection(x, w, z.float().to(DEV), act=act, out=out)
+        got = out.cpu()
+        assert torch.equal(got[:, :-1], right[:-1].to(out_dtype).expand(m, n - 1)), (out_dtype, got[0])
+        assert bool(got[:, -1].isnan().all())
+    dy = torch.zeros(m, n, dtype=BF, device=DEV)
+    dy[0] = 1.0
+    _, _, db = bd.projection_backward(dy, x, w, pre=z.expand(m, n).contiguous().to(DEV), act=act, dx=None, dw=None, db=True)
+    slope = torch.where(z > 0, 1.0, torch.where(z == 0, 0.5, 0.0))
+    got = db.cpu()
+    # (at 0: Phi's fit, off by 1e-7)
+    assert bool(((got - slope)[:-1].abs() <= 2.0 ** -22).all()), got
+    # (the other rows' products of 0 with a NaN's slope, too)
+    assert bool(got[-1].isnan())
