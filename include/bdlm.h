@@ -75,7 +75,8 @@ enum bdlm_status {
     BDLM_E_WORKSPACE = -8 /* sequence entry points: workspace missing or too small */
 };
 
-enum bdlm_dtype { BDLM_DTYPE_F32 = 0, BDLM_DTYPE_BF16 = 1 };
+/* BDLM_DTYPE_E4M3 (8 bits, 4 of exponent, largest 448): outputs of bdlm_add_rmsnorm only. */
+enum bdlm_dtype { BDLM_DTYPE_F32 = 0, BDLM_DTYPE_BF16 = 1, BDLM_DTYPE_E4M3 = 2 };
 
 /*
  * Shape and activation layout of one call.  Strides are in elements.
@@ -433,6 +434,47 @@ int bdlm_gated_rmsnorm(int64_t batch, int64_t len, int64_t nheads, int64_t ngrou
                        void *stream);
 
 /*
+ * Norm at a sublayer's entry: the sublayer before, x, is added onto the residual stream, and the sum is normalised by
+ * its root mean square, per row of `width` columns:
+ *     s = x + residual,   out = norm_w * s / sqrt(mean s^2 + eps).
+ * s is formed in fp32 and normalised unrounded (squares may leave fp32's range, s itself may not: an infinity or NaN
+ * makes its row's norm 0 or NaN, as the formula says).
+ * x            device [rows][width], x_dtype; residual residual_dtype, or NULL (s = x); row strides in elements, which
+ *              may be 0 or overlap.
+ * sum          s in residual_dtype (what the gradient takes), or NULL; may be residual (same stride).
+ * norm_w       device fp32 [width].  eps finite, >= 0.
+ * out          out_dtype: BDLM_DTYPE_F32, BDLM_DTYPE_BF16, or BDLM_DTYPE_E4M3; may be x (same type and stride).
+ * scale        BDLM_DTYPE_E4M3 only, else not used: device fp32, contiguous, what an 8-bit value is to be multiplied with: the largest
+ *              |out| of those that share it divided by 448 (1 where they are all 0; NaN in a row that holds a NaN or infinity).
+ *              scale_block 0: one a row, [rows]; 128: one for each 128 columns, [rows][(width + 127) / 128].
+ * Matrices and norm_w 16-byte aligned; rows 0 .. 2^22, width 1 .. 2^22; otherwise no argument overlaps an output.
+ * Errors: BDLM_E_NULL, BDLM_E_SHAPE, BDLM_E_DTYPE, BDLM_E_ALIGN, BDLM_E_LAUNCH.  rows == 0 enqueues nothing.
+ */
+int bdlm_add_rmsnorm(int64_t rows, int64_t width, int32_t x_dtype, const void *x, int64_t x_stride,
+                     int32_t residual_dtype, const void *residual, int64_t residual_stride,
+                     void *sum, int64_t sum_stride, const float *norm_w, float eps,
+                     int32_t out_dtype, void *out, int64_t out_stride, float *scale,
+                     int64_t scale_block, void *stream);
+
+/*
+ * Its gradient, at the sum s (of a call without residual: x).  With rstd = 1 / sqrt(mean s^2 + eps) and n = s rstd:
+ *     ds = rstd (norm_w dy - n mean(n norm_w dy)) + dsum,   dw = sum over the rows of dy n;
+ * ds is the gradient of x and of residual alike.
+ * dy           device [rows][width], dy_dtype; s s_dtype.
+ * dsum         the gradient that arrives at sum from behind, ds_dtype, or NULL.
+ * ds           ds_dtype, or NULL (not wanted); may be dsum (same stride).
+ * dw           device fp32 [width], or NULL.  Summed in a fixed order.  rows == 0 zeroes it.
+ * workspace    for dw alone: 256-byte aligned, of at least the size that the query returns.
+ * Errors: as bdlm_add_rmsnorm, and BDLM_E_WORKSPACE.
+ */
+int bdlm_add_rmsnorm_backward_workspace(int64_t rows, int64_t width, int64_t *bytes);
+int bdlm_add_rmsnorm_backward(int64_t rows, int64_t width, int32_t dy_dtype, const void *dy,
+                              int64_t dy_stride, int32_t s_dtype, const void *s, int64_t s_stride,
+                              const float *norm_w, float eps, int32_t ds_dtype, const void *dsum,
+                              int64_t dsum_stride, void *ds, int64_t ds_stride, float *dw,
+                              void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Dense operators around the scan: the projections of a Mamba-H layer (the mixer's input and
  * output projections, the MLP's products), and the language-model head, whose logits never exist
  * in memory: the most probable token of every position of a denoising step, and the masked
@@ -614,6 +656,17 @@ int bdlm_check_prefill(const bdlm_desc_t *desc, const void *x, const void *dt, c
                        const int64_t *n_blocks, int64_t expected_block_index,
                        int64_t blocks_in_prefix, const float *y_fwd, const void *workspace,
                        int64_t workspace_bytes);
+int bdlm_check_add_rmsnorm(int64_t rows, int64_t width, int32_t x_dtype, const void *x,
+                           int64_t x_stride, int32_t residual_dtype, const void *residual,
+                           int64_t residual_stride, const void *sum, int64_t sum_stride,
+                           const float *norm_w, float eps, int32_t out_dtype, const void *out,
+                           int64_t out_stride, const float *scale, int64_t scale_block);
+int bdlm_check_add_rmsnorm_backward(int64_t rows, int64_t width, int32_t dy_dtype, const void *dy,
+                                    int64_t dy_stride, int32_t s_dtype, const void *s,
+                                    int64_t s_stride, const float *norm_w, float eps,
+                                    int32_t ds_dtype, const void *dsum, int64_t dsum_stride,
+                                    const void *ds, int64_t ds_stride, const float *dw,
+                                    const void *workspace, int64_t workspace_bytes);
 int bdlm_check_projection(const bdlm_dense_desc_t *desc, int32_t act, int32_t out_dtype,
                           const void *x, const void *w, const float *bias, const void *residual,
                           int64_t residual_stride, const void *out, int64_t out_stride,

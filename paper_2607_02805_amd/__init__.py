@@ -16,6 +16,8 @@ Entry points (same names as the C ABI):
   (the DiffuMamba-style contrast).
 * :func:`prefill` -- summarise a long clean prefix into the cached states in one call.
 * :func:`cache_reset` -- empty the given cache slots.
+* :func:`add_rmsnorm`, :func:`add_rmsnorm_backward` -- the norm at a sublayer's entry, with the
+  residual's addition and an output in 8 bits with scales if asked, and its gradient.
 * :func:`projection`, :func:`projection_backward` -- the layer's dense products with bias,
   activation and residual, and their gradients.
 * :func:`head_select`, :func:`head_loss`, :func:`head_loss_backward` -- the language-model head
@@ -43,6 +45,8 @@ MAX_SLOT_ROWS = 256
 SCRATCH_BYTES = 64 << 20     # BDLM_SCRATCH_BYTES: the no-allocation prefill's device scratch
 DTYPE_F32 = 0
 DTYPE_BF16 = 1
+DTYPE_E4M3 = 2
+SCALE_BLOCK = 128            # columns that can share a scale of an 8-bit output
 
 OK, E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_OFFSET, E_SLOT, E_LAUNCH, E_WORKSPACE = \
     0, -1, -2, -3, -4, -5, -6, -7, -8
@@ -163,6 +167,14 @@ def lib() -> ctypes.CDLL:
             getattr(L, "bdlm_check_" + name).argtypes = args
             getattr(L, f"bdlm_{name}_workspace").argtypes = [ddp, i64p]
             dense += ["bdlm_" + name, "bdlm_check_" + name, f"bdlm_{name}_workspace"]
+        norm = [i64, i64, i32, vp, i64, i32, vp, i64, vp, i64, fp, f32, i32, vp, i64, fp, i64]
+        norm_back = [i64, i64, i32, vp, i64, i32, vp, i64, fp, f32, i32, vp, i64, vp, i64, fp, vp, i64]
+        for name, args in (("add_rmsnorm", norm), ("add_rmsnorm_backward", norm_back)):
+            getattr(L, "bdlm_" + name).argtypes = args + [vp]
+            getattr(L, "bdlm_check_" + name).argtypes = args
+            dense += ["bdlm_" + name, "bdlm_check_" + name]
+        L.bdlm_add_rmsnorm_backward_workspace.argtypes = [i64, i64, i64p]
+        dense.append("bdlm_add_rmsnorm_backward_workspace")
         for name in dense:
             getattr(L, name).restype = ctypes.c_int
         for name in ("bdlm_desc_init", "bdlm_check_block_step", "bdlm_check_commit",
@@ -903,6 +915,127 @@ def _token(exclude, d) -> int:
 
 def _p(t):
     return None if t is None or t.numel() == 0 else t.data_ptr()
+
+
+def _out_code(dtype, what: str) -> int:
+    torch = _torch()
+    if dtype == torch.float8_e4m3fn:
+        return DTYPE_E4M3
+    if dtype in (torch.bfloat16, torch.float32):
+        return DTYPE_BF16 if dtype == torch.bfloat16 else DTYPE_F32
+    raise ValueError(f"{what} must be bfloat16, float32 or float8_e4m3fn, got {dtype}")
+
+
+def _norm_rows(t, x, what: str):
+    """Row stride of a matrix of x's shape and device, bfloat16 or float32, and its type."""
+    if t.device != x.device:
+        raise ValueError(f"{what} must be on {x.device}")
+    _, ld = _rows2d(t, x.shape[-1], what, x.shape[:-1])
+    return ld, _dtype_code(t, what)
+
+
+def add_rmsnorm(x, w, residual=None, eps=1e-5, out_dtype=None, out=None, sum=None, scale=None, scale_block=0,
+                stream=None):
+    """The norm at a sublayer's entry: ``s = x + residual``, ``out = w * s / sqrt(mean(s^2) + eps)`` over
+    the last dimension of x [..., width] (bfloat16 or float32).  Returns (out, sum, scale).
+
+    ``w`` float32 [width].  ``residual`` (bfloat16 or float32, x's shape) is the stream; ``sum``
+    is s in its type, allocated if None, False if not wanted, or a tensor, ``residual`` itself among them; without a
+    residual it is None.  ``out`` has ``out_dtype`` (x's if None): bfloat16, float32, or float8_e4m3fn, whose
+    values are to be multiplied with ``scale``, float32 [..., 1] (``scale_block`` 0) or one for every
+    128 columns (``scale_block`` 128): the largest magnitude among them over 448.
+
+    No autograd graph is recorded: :func:`add_rmsnorm_backward` has the gradients."""
+    torch = _torch()
+    if stream is not None:
+        with _on(stream, x):
+            return add_rmsnorm(x, w, residual, eps, out_dtype, out, sum, scale, scale_block)
+    if x.dim() < 1 or x.shape[-1] == 0:
+        raise ValueError("x [..., width] expected")
+    if x.device.type != "cuda":
+        raise ValueError("x must be a GPU tensor (no CPU path exists)")
+    width = x.shape[-1]
+    rows, ldx = _rows2d(x, width, "x")
+    xdt = _dtype_code(x, "x")
+    _vector(w, (width,), torch.float32, x.device, "w")
+    ldr = rdt = lds = 0
+    if residual is not None:
+        ldr, rdt = _norm_rows(residual, x, "residual")
+        if sum is not False:
+            sum = _place(sum, x.shape, residual.dtype, x.device, "sum")
+            _, lds = _rows2d(sum, width, "sum")
+    elif sum is not None and sum is not False:
+        raise ValueError("sum needs a residual")
+    sum = None if sum is False else sum
+    if out_dtype is None:
+        out_dtype = x.dtype if out is None else out.dtype
+    odt = _out_code(out_dtype, "out_dtype")
+    out = _place(out, x.shape, out_dtype, x.device, "out")
+    _, ldo = _rows2d(out, width, "out")
+    if odt == DTYPE_E4M3:
+        if scale_block not in (0, SCALE_BLOCK):
+            raise ValueError(f"scale_block must be 0 (a scale for each row) or {SCALE_BLOCK}, got {scale_block!r}")
+        shape = (*x.shape[:-1], (width + SCALE_BLOCK - 1) // SCALE_BLOCK if scale_block else 1)
+        scale = _vector(_place(scale, shape, torch.float32, x.device, "scale"), shape, torch.float32, x.device, "scale")
+    elif scale is not None or scale_block != 0:
+        raise ValueError("scale and scale_block are for float8_e4m3fn outputs")
+    with torch.cuda.device(x.device):
+        rc = lib().bdlm_add_rmsnorm(rows, width, xdt, _p(x), ldx, rdt, _p(residual), ldr, _p(sum), lds, _p(w), float(eps),
+                                    odt, _p(out), ldo, _p(scale), scale_block, _stream_handle(None))
+    if rc != OK:
+        raise BdlmError(rc, "bdlm_add_rmsnorm")
+    return out, sum, scale
+
+
+def add_rmsnorm_backward(dy, s, w, dsum=None, eps=1e-5, ds=True, dw=True, stream=None, workspace=None):
+    """Gradients of :func:`add_rmsnorm` by the stream and by ``w``: (ds, dw), each None if not wanted.
+
+    ``dy`` [..., width] is the gradient of the norm's output, ``s`` the sum that the forward call returned
+    (without a residual: its x), ``dsum`` the gradient that arrives at the sum from behind, or None.
+    ``ds`` is the gradient of x and of the residual alike, in dsum's type (s's without one; a given tensor may be
+    ``dsum`` itself).  dw is float32.  ``ds``, ``dw``: True (allocate), None (not wanted) or a tensor."""
+    torch = _torch()
+    if stream is not None:
+        with _on(stream, s):
+            return add_rmsnorm_backward(dy, s, w, dsum, eps, ds, dw, workspace=workspace)
+    if s.dim() < 1 or s.shape[-1] == 0:
+        raise ValueError("s [..., width] expected")
+    if s.device.type != "cuda":
+        raise ValueError("s must be a GPU tensor (no CPU path exists)")
+    width = s.shape[-1]
+    rows, lds = _rows2d(s, width, "s")
+    sdt = _dtype_code(s, "s")
+    ldy, ydt = _norm_rows(dy, s, "dy")
+    _vector(w, (width,), torch.float32, s.device, "w")
+    ldt = ldd = 0
+    dtype = s.dtype
+    if dsum is not None:
+        ldt, _ = _norm_rows(dsum, s, "dsum")
+        dtype = dsum.dtype
+    elif torch.is_tensor(ds):
+        dtype = ds.dtype
+    if ds is not None:
+        ds = _place(ds, s.shape, dtype, s.device, "ds")
+        ldd, _ = _norm_rows(ds, s, "ds")
+    if dw is not None:
+        dw = _vector(_place(dw, (width,), torch.float32, s.device, "dw"), (width,), torch.float32, s.device, "dw")
+    need = ctypes.c_int64(0)
+    if dw is not None:
+        rc = lib().bdlm_add_rmsnorm_backward_workspace(rows, width, ctypes.byref(need))
+        if rc != OK:
+            raise BdlmError(rc, "bdlm_add_rmsnorm_backward")
+    with torch.cuda.device(s.device):
+        if workspace is None:
+            workspace = torch.empty(need.value, dtype=torch.uint8, device=s.device) if need.value else None
+        elif workspace.device != s.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous tensor on {s.device}")
+        size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        rc = lib().bdlm_add_rmsnorm_backward(
+            rows, width, ydt, _p(dy), ldy, sdt, _p(s), lds, _p(w), float(eps), DTYPE_BF16 if dtype == torch.bfloat16 else DTYPE_F32,
+            _p(dsum), ldt, _p(ds), ldd, _p(dw), workspace.data_ptr() if size else None, size, _stream_handle(None))
+    if rc != OK:
+        raise BdlmError(rc, "bdlm_add_rmsnorm_backward")
+    return ds, dw
 
 
 def projection(x, w, bias=None, act=None, residual=None, out=None, pre=None, stream=None,

@@ -15,41 +15,6 @@
 namespace bdlm {
 namespace {
 
-typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
-typedef u32x4 __attribute__((aligned(4))) u32x4_a4;
-
-// Eight consecutive elements of a row as they lie, zeros past the n that there are.
-template <bool BF16>
-struct Eight {
-    u32x4 u[BF16 ? 1 : 2];
-    __device__ __forceinline__ void load(const void *src, int64_t at, int n) {
-        if constexpr (BF16) {
-            const uint16_t *p = static_cast<const uint16_t *>(src) + at;
-            if (n >= 8) {
-                u[0] = *reinterpret_cast<const u32x4_a2 *>(p);
-            } else {
-                uint32_t h[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = e < n ? p[e] : 0u;
-                u[0] = u32x4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
-            }
-        } else {
-            const float *p = static_cast<const float *>(src) + at;
-            if (n >= 8) {
-                u[0] = *reinterpret_cast<const u32x4_a4 *>(p);
-                u[1] = *reinterpret_cast<const u32x4_a4 *>(p + 4);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e >> 2][e & 3] = e < n ? __float_as_uint(p[e]) : 0u;
-            }
-        }
-    }
-    __device__ __forceinline__ float value(int e) const {
-        if constexpr (BF16) return e & 1 ? __uint_as_float(u[0][e >> 1] & 0xffff0000u) : __uint_as_float(u[0][e >> 1] << 16);
-        else return __uint_as_float(u[e >> 2][e & 3]);
-    }
-};
-
 template <int TERMS>
 __device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, const float (&v)[8]) {
     if constexpr (TERMS == 1) {

@@ -1,4 +1,4 @@
-// bdlm_dense_device.h -- device helpers of the dense operators: activations and their
+// bdlm_dense_device.h -- device helpers of the dense operators: unaligned row pieces, activations and their
 // derivatives, bf16 terms of fp32 values, and the merge of softmax records.  Internal.
 #pragma once
 
@@ -9,6 +9,41 @@ namespace bdlm {
 namespace {
 
 constexpr int kNoColumn = 0x7fffffff;
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_a4;
+
+// Eight consecutive elements of a row as they lie, zeros past the n that there are.
+template <bool BF16>
+struct Eight {
+    u32x4 u[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void *src, int64_t at, int n) {
+        if constexpr (BF16) {
+            const uint16_t *p = static_cast<const uint16_t *>(src) + at;
+            if (n >= 8) {
+                u[0] = *reinterpret_cast<const u32x4_a2 *>(p);
+            } else {
+                uint32_t h[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[e] = e < n ? p[e] : 0u;
+                u[0] = u32x4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+            }
+        } else {
+            const float *p = static_cast<const float *>(src) + at;
+            if (n >= 8) {
+                u[0] = *reinterpret_cast<const u32x4_a4 *>(p);
+                u[1] = *reinterpret_cast<const u32x4_a4 *>(p + 4);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e >> 2][e & 3] = e < n ? __float_as_uint(p[e]) : 0u;
+            }
+        }
+    }
+    __device__ __forceinline__ float value(int e) const {
+        if constexpr (BF16) return e & 1 ? __uint_as_float(u[0][e >> 1] & 0xffff0000u) : __uint_as_float(u[0][e >> 1] << 16);
+        else return __uint_as_float(u[e >> 2][e & 3]);
+    }
+};
 
 // v = t[0] + t[1] + t[2]: each term the rounded remainder of the ones before it, 24 bits together.
 // A value whose rounding to bf16 would overflow keeps the largest finite first term, and an

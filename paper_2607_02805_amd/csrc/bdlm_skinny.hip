@@ -24,9 +24,6 @@ namespace {
 constexpr int kRun = 128;    // contraction indices of a wave's turn
 constexpr int kSteps = kRun / 32;
 
-typedef u32x4 __attribute__((aligned(2))) u32x4_a2;
-typedef u32x4 __attribute__((aligned(4))) u32x4_a4;
-
 // Eight consecutive elements from index k of a row of length K, as bf16 terms; zeros past K.
 template <bool BF16>
 struct Piece;
