@@ -556,6 +556,43 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t
                              int64_t workspace_bytes, void *stream);
 
 /*
+ * Gated product of an MLP: gate = x w_gate^T + bias_gate, up = x w_up^T + bias_up, out = act(gate) * up,
+ * in one pass over x (with act BDLM_ACT_NONE the product of the two).
+ * desc         w_stride is that of both weights, [out_features][in_features] each (they may be slices of one matrix).
+ * bias_gate, bias_up  device fp32 [out_features], each or NULL.
+ * out          device [rows][out_features], out_dtype; formed from the unrounded gate and up.
+ * pre_gate, pre_up    gate and up, device [rows][out_features], in_dtype, at one stride, both or neither: kept for the gradient.
+ * Up to 32 rows (fp32: 64) need no workspace.
+ * Errors: as bdlm_projection.  rows == 0 enqueues nothing.
+ */
+int bdlm_gated_projection_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_gated_projection(const bdlm_dense_desc_t *desc, int32_t act, int32_t out_dtype,
+                          const void *x, const void *w_gate, const void *w_up,
+                          const float *bias_gate, const float *bias_up, void *out,
+                          int64_t out_stride, void *pre_gate, void *pre_up, int64_t pre_stride,
+                          void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient: d_gate = dh * up * act'(gate), d_up = dh * act(gate), at gate and up as kept;
+ *     dx = d_gate w_gate + d_up w_up,  dw_gate = d_gate^T x,  dw_up = d_up^T x,  db = sums over the rows.
+ * dh           device [rows][out_features], dh_dtype.
+ * dx, dw_gate, dw_up  device, in_dtype, shaped as x and the weights (dw_stride is that of both), each or NULL (not
+ *              wanted: the weights are read for dx alone, x for dw alone).  db_gate, db_up fp32 [out_features], each or NULL.
+ *              rows == 0 zeroes the weights' and biases' gradients.
+ * With bf16 inputs and more than 64 rows d_gate and d_up are rounded to bf16 for the products (of fewer rows two bf16
+ * terms are kept; db sums them unrounded).
+ * Errors: as bdlm_projection.
+ */
+int bdlm_gated_projection_backward_workspace(const bdlm_dense_desc_t *desc, int64_t *bytes);
+int bdlm_gated_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t dh_dtype,
+                                   const void *dh, int64_t dh_stride, const void *x,
+                                   const void *w_gate, const void *w_up, const void *pre_gate,
+                                   const void *pre_up, int64_t pre_stride, void *dx,
+                                   int64_t dx_stride, void *dw_gate, void *dw_up,
+                                   int64_t dw_stride, float *db_gate, float *db_up,
+                                   void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * Masked loss of a head: per row, with logits l = x w^T over the vocabulary,
  *     lse = log sum exp l,   loss = lse - l[label].
  * exclude      a token the softmax does not range over (the mask token, whose probability
@@ -678,6 +715,21 @@ int bdlm_check_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, i
                                    const void *dx, int64_t dx_stride, const void *dw,
                                    int64_t dw_stride, const float *db, const void *workspace,
                                    int64_t workspace_bytes);
+int bdlm_check_gated_projection(const bdlm_dense_desc_t *desc, int32_t act, int32_t out_dtype,
+                                const void *x, const void *w_gate, const void *w_up,
+                                const float *bias_gate, const float *bias_up, const void *out,
+                                int64_t out_stride, const void *pre_gate, const void *pre_up,
+                                int64_t pre_stride, const void *workspace,
+                                int64_t workspace_bytes);
+int bdlm_check_gated_projection_backward(const bdlm_dense_desc_t *desc, int32_t act,
+                                         int32_t dh_dtype, const void *dh, int64_t dh_stride,
+                                         const void *x, const void *w_gate, const void *w_up,
+                                         const void *pre_gate, const void *pre_up,
+                                         int64_t pre_stride, const void *dx, int64_t dx_stride,
+                                         const void *dw_gate, const void *dw_up,
+                                         int64_t dw_stride, const float *db_gate,
+                                         const float *db_up, const void *workspace,
+                                         int64_t workspace_bytes);
 int bdlm_check_head_loss(const bdlm_dense_desc_t *desc, const int64_t *labels, int64_t exclude,
                          const void *x, const void *w, const float *loss, const float *lse,
                          const void *workspace, int64_t workspace_bytes);

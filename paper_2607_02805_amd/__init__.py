@@ -20,6 +20,8 @@ Entry points (same names as the C ABI):
   residual's addition and an output in 8 bits with scales if asked, and its gradient.
 * :func:`projection`, :func:`projection_backward` -- the layer's dense products with bias,
   activation and residual, and their gradients.
+* :func:`gated_projection`, :func:`gated_projection_backward` -- the gated product of an MLP,
+  act(gate) * up, and its gradients.
 * :func:`head_select`, :func:`head_loss`, :func:`head_loss_backward` -- the language-model head
   without its logits: the most probable tokens of a denoising step, and the masked training
   loss with its gradient.
@@ -161,8 +163,11 @@ def lib() -> ctypes.CDLL:
         grad = [ddp, vp, i64, vp, vp, fp, fp, fp, vp, i64, vp, i64, vp, i64]
         pick = [ddp, i64, vp, vp, vp, fp, vp, i64]
         dense = ["bdlm_dense_desc_init"]
+        gate = [ddp, i32, i32, vp, vp, vp, fp, fp, vp, i64, vp, vp, i64, vp, i64]
+        gate_back = [ddp, i32, i32, vp, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, vp, i64, fp, fp, vp, i64]
         for name, args in (("projection", proj), ("projection_backward", back), ("head_loss", loss),
-                           ("head_loss_backward", grad), ("head_select", pick)):
+                           ("head_loss_backward", grad), ("head_select", pick), ("gated_projection", gate),
+                           ("gated_projection_backward", gate_back)):
             getattr(L, "bdlm_" + name).argtypes = args + [vp]
             getattr(L, "bdlm_check_" + name).argtypes = args
             getattr(L, f"bdlm_{name}_workspace").argtypes = [ddp, i64p]
@@ -1129,6 +1134,110 @@ def projection_backward(dy, x, w, pre=None, act=None, dx=True, dw=True, db=None,
     _dense_call("projection_backward", d, x.device, workspace,
                 (code, ydt, _p(dy), ldy, _p(x), _p(w), _p(pre), ldp, _p(dx), ldx, _p(dw), ldw, _p(db)))
     return dx, dw, db
+
+
+def _two_weights(x, w_gate, w_up):
+    d, lead = _dense(x, w_gate)
+    if w_up.shape != w_gate.shape or w_up.dtype != w_gate.dtype or w_up.device != w_gate.device:
+        raise ValueError("w_gate and w_up must share shape, dtype and device")
+    if _rows2d(w_up, d.in_features, "w_up")[1] != d.w_stride:
+        raise ValueError("w_gate and w_up must share one row stride")
+    return d, lead
+
+
+def _pair(t, d, lead, x, what: str):
+    """Two tensors [..., out_features] in x's type at one row stride, new ones for True; and the stride."""
+    shape = (*lead, d.out_features)
+    if t is True:
+        t = tuple(_torch().empty(shape, dtype=x.dtype, device=x.device) for _ in range(2))
+    if not isinstance(t, (tuple, list)) or len(t) != 2:
+        raise ValueError(f"{what} must be two tensors")
+    for v in t:
+        if not _torch().is_tensor(v):
+            raise ValueError(f"{what} must be two tensors")
+    strides = [_rows2d(_place(v, shape, x.dtype, x.device, what), d.out_features, what, lead)[1] for v in t]
+    if strides[0] != strides[1]:
+        raise ValueError(f"both tensors of {what} must share one row stride")
+    return (t[0], t[1]), strides[0]
+
+
+def gated_projection(x, w_gate, w_up, bias_gate=None, bias_up=None, act="silu", out=None, pre=None, stream=None,
+                     workspace=None):
+    """``act(x w_gate^T + bias_gate) * (x w_up^T + bias_up)``, the gated product of an MLP, for x [..., in_features] and
+    weights [out_features, in_features] (bfloat16 or float32, both weights at one row stride); ``act`` None, "silu" or "gelu".
+
+    The biases are float32 [out_features] or None.  ``out`` (x's dtype if None; a given tensor may be bfloat16 or
+    float32) is [..., out_features].  ``pre`` keeps both products with their biases in x's dtype for the gradient: None
+    (no), True (allocate) or two tensors at one row stride.  Returns out, or (out, (gate, up)) if ``pre`` was asked for.
+
+    No autograd graph is recorded: :func:`gated_projection_backward` has the gradients."""
+    if stream is not None:
+        with _on(stream, x):
+            return gated_projection(x, w_gate, w_up, bias_gate, bias_up, act, out, pre, workspace=workspace)
+    torch = _torch()
+    code = _act_code(act)
+    d, lead = _two_weights(x, w_gate, w_up)
+    out = _place(out, (*lead, d.out_features), x.dtype if out is None else out.dtype, x.device, "out")
+    odt = _dtype_code(out, "out")
+    _, ldo = _rows2d(out, d.out_features, "out", lead)
+    for t, what in ((bias_gate, "bias_gate"), (bias_up, "bias_up")):
+        if t is not None:
+            _vector(t, (d.out_features,), torch.float32, x.device, what)
+    ldp = 0
+    gate = up = None
+    if pre is not None:
+        (gate, up), ldp = _pair(pre, d, lead, x, "pre")
+    _dense_call("gated_projection", d, x.device, workspace,
+                (code, odt, _p(x), _p(w_gate), _p(w_up), _p(bias_gate), _p(bias_up), _p(out), ldo, _p(gate), _p(up), ldp))
+    return out if pre is None else (out, (gate, up))
+
+
+def gated_projection_backward(dh, x, w_gate, w_up, pre, act="silu", dx=True, dw_gate=True, dw_up=True, dbg=None, dbu=None,
+                              stream=None, workspace=None):
+    """Gradients of :func:`gated_projection` by x, the weights and the biases: (dx, dw_gate, dw_up, dbg, dbu), each None if
+    not wanted.
+
+    ``dh`` [..., out_features] (bfloat16 or float32) is the gradient of the output, ``pre`` the two tensors that the forward
+    call kept.  ``dx``, ``dw_gate``, ``dw_up``, ``dbg``, ``dbu``: True (allocate), None (not wanted) or a tensor; dx and the
+    weights' gradients (at one row stride) have x's dtype, the biases' are float32.
+
+    With bfloat16 inputs and more than 64 rows the gradients by both factors are rounded to bfloat16 for dx and the weights;
+    float32 inputs keep them to 24 bits."""
+    if stream is not None:
+        with _on(stream, x):
+            return gated_projection_backward(dh, x, w_gate, w_up, pre, act, dx, dw_gate, dw_up, dbg, dbu, workspace=workspace)
+    torch = _torch()
+    code = _act_code(act)
+    d, lead = _two_weights(x, w_gate, w_up)
+    if dh.device != x.device:
+        raise ValueError("dh must be on x's device")
+    hdt = _dtype_code(dh, "dh")
+    _, ldh = _rows2d(dh, d.out_features, "dh", lead)
+    if pre is None or pre is True:
+        raise ValueError("pre is needed for the gradient")
+    (gate, up), ldp = _pair(pre, d, lead, x, "pre")
+    ldx = 0
+    if dx is not None:
+        dx = _place(dx, x.shape, x.dtype, x.device, "dx")
+        _, ldx = _rows2d(dx, d.in_features, "dx", lead)
+    grads, strides = [], []
+    for t, what in ((dw_gate, "dw_gate"), (dw_up, "dw_up")):
+        if t is not None:
+            t = _place(t, w_gate.shape, x.dtype, x.device, what)
+            strides.append(_rows2d(t, d.in_features, what)[1])
+        grads.append(t)
+    if len(set(strides)) > 1:
+        raise ValueError("dw_gate and dw_up must share one row stride")
+    sums = []
+    for t, what in ((dbg, "dbg"), (dbu, "dbu")):
+        if t is not None:
+            t = _vector(_place(t, (d.out_features,), torch.float32, x.device, what), (d.out_features,), torch.float32,
+                        x.device, what)
+        sums.append(t)
+    _dense_call("gated_projection_backward", d, x.device, workspace,
+                (code, hdt, _p(dh), ldh, _p(x), _p(w_gate), _p(w_up), _p(gate), _p(up), ldp, _p(dx), ldx, _p(grads[0]),
+                 _p(grads[1]), strides[0] if strides else 0, _p(sums[0]), _p(sums[1])))
+    return dx, grads[0], grads[1], sums[0], sums[1]
 
 
 def head_loss(x, w, labels, exclude=-1, loss=None, lse=None, stream=None, workspace=None):

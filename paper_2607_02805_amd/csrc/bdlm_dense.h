@@ -26,7 +26,10 @@ enum TileOut {
     kTileStore = 0,    // v = act(acc + bias) + residual -> out
     kTilePartial = 1,  // fp32 partial sums, one slice per split (added onto what is there, if asked)
     kTileBest = 2,     // per row: the tile's largest value, its column, the others' sum of exps
-    kTileProb = 3      // gradient of the loss by the logits, in bf16 terms
+    kTileProb = 3,     // gradient of the loss by the logits, in bf16 terms
+    kTileGated = 4,    // act(gate) * up -> out, of products with two weight matrices
+    kTileGatedPart = 5,   // their fp32 partial sums
+    kTileTwo = 6       // kTileStore whose rows go to two matrices
 };
 
 // Store: the epilogue of a projection (also applied by the join of partial sums).
@@ -40,6 +43,18 @@ struct StoreArgs {
     int32_t act;
     const int32_t *row_of;     // row r goes to row row_of[r] of out (null: r)
 };
+
+// Gated: of two weight matrices of n rows each, groups of 32 rows in turn (gate, up) make the columns of a product, so that a lane
+// has both of an output in its registers: column c of either is column 64 (c / 32) + c % 32 of the product, up's 32 more.
+struct GatedArgs {
+    void *out;
+    const float *bias_gate, *bias_up;   // [n] or null
+    void *pre_gate, *pre_up;            // the products with their biases, or null
+    int64_t ld_out, ld_pre;
+    int32_t out_bf16, pre_bf16;
+    int32_t act, n;
+};
+inline int64_t gated_columns(int64_t n) { return (n + 31) / 32 * 64; }
 
 // One record per (row, column tile): largest value, sum over the others of exp(v - largest).
 struct BestArgs {
@@ -88,6 +103,14 @@ struct TileArgs {
     StoreArgs store;
     BestArgs best;
     ProbArgs prob;
+    // Pairs from `half` on are of the operands' second parts, that many elements further: dz of up beside dz of gate, times
+    // w_up after w_gate (half = npair: there are none).  kTileGated: col_duo from w_gate to w_up.
+    int32_t half;
+    int64_t row_duo, col_duo;
+    GatedArgs gated;
+    // kTileTwo: rows below two_rows are store's, those from two_at on go to two_out from its row 0 on (same stride).
+    void *two_out;
+    int32_t two_rows, two_at;
 };
 int launch_tile(const TileArgs &a, void *stream);
 constexpr int32_t kChip = 256;   // workgroups of large tiles that run at once
@@ -110,6 +133,12 @@ inline int32_t tile_edge(bool big) { return big ? 256 : 128; }
 int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, int32_t ncol, const int32_t *nrow_dev,
                 const float *scale, const StoreArgs &s, void *stream);
 
+// The same with its rows in two matrices, as kTileTwo has them.
+int launch_join_two(const float *part, int32_t splits, int32_t nrow, int32_t ncol, void *two_out, int32_t two_rows,
+                    int32_t two_at, const StoreArgs &s, void *stream);
+// Of the columns of gated products, their activation and product.
+int launch_join_gated(const float *part, int32_t splits, int32_t nrow, const GatedArgs &g, void *stream);
+
 // Few rows (skinny_rows): the weights stream through once.  x [nrow][k], w [ncol][k], both bf16
 // or both fp32, any stride; out kTileStore or kTileBest (one record per skinny_cols columns).
 struct SkinnyArgs {
@@ -121,6 +150,8 @@ struct SkinnyArgs {
     int32_t out;
     StoreArgs store;
     BestArgs best;
+    const void *w2;                    // kTileGated: w_up, w being w_gate (ncol columns each)
+    GatedArgs gated;
 };
 // Above that many rows the tiles are faster: over 50,257 columns of 1,024 in bf16, 32 rows take 34
 // us here and 29 there, 64 rows 54 and 34, but over 4,384 of them 32 rows take 9 and 11; in fp32,
@@ -155,6 +186,16 @@ constexpr int32_t kPackRows = 16;   // rows per workgroup
 __host__ __device__
 #endif
 inline int32_t pack_row_blocks(int32_t rows) { return (rows + 63) / 64 * (64 / kPackRows); }
+// The gradients of a gated product by its two factors, in bf16 terms: columns 0 .. n of dst's rows are dh up act'(gate), columns
+// ldz .. ldz + n dh act(gate), zeros up to the next part, and rows of zeros up to a multiple of 64.
+struct GatedPackArgs {
+    const void *dh, *gate, *up;
+    int64_t ld_dh, ld_pre, ldz, plane;
+    int32_t rows, n, dh_bf16, pre_bf16, terms, act;
+    uint16_t *dst;             // [terms][rows][2 ldz], or null
+    float *sum_gate, *sum_up;  // [pack_row_blocks(rows)][n] partial column sums, or null
+};
+int launch_gated_pack(const GatedPackArgs &a, void *stream);
 // out[c] = sum over the blocks of part[b][c]
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream);
 

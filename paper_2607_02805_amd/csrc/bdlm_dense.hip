@@ -100,6 +100,69 @@ __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
     }
 }
 
+// The gradients of a gated product by its factors, as bdlm_pack_kernel lays out the one of a projection: a workgroup takes
+// kPackRows rows of 64 x 8 columns, a thread eight columns of two rows at a time, and writes both parts.
+template <bool DH16, bool PRE16, int TERMS>
+__global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArgs a) {
+    __shared__ float sums[2][4][64 * 8];
+    constexpr int kBatch = 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t rows_up = (int64_t(a.rows) + 63) / 64 * 64;
+    const int64_t across = (a.ldz + 511) / 512, blocks = across * pack_row_blocks(a.rows);
+    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const int64_t down = block / across;
+        const int c0 = static_cast<int>(block - down * across) * 512, c = c0 + lane * 8;
+        const int64_t r0 = down * kPackRows;
+        const int n = a.n - c;
+        float sum[2][8] = {};
+        if (c < a.ldz) {
+            for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += 4 * kBatch) {
+                Eight<DH16> dh[kBatch];
+                Eight<PRE16> gate[kBatch], up[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int64_t r = q + 4 * k, from = r < a.rows ? r : 0;
+                    const int there = r < a.rows ? n : 0;
+                    dh[k].load(a.dh, from * a.ld_dh + c, there);
+                    gate[k].load(a.gate, from * a.ld_pre + c, there);
+                    up[k].load(a.up, from * a.ld_pre + c, there);
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int64_t r = q + 4 * k;
+                    float f[2][8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float value, slope;
+                        act_both<!PRE16>(gate[k].value(e), a.act, value, slope);
+                        const bool here = r < a.rows && e < n;   // (a slope of no column is not 0)
+                        f[0][e] = here ? dh[k].value(e) * up[k].value(e) * slope : 0.f;
+                        f[1][e] = here ? dh[k].value(e) * value : 0.f;
+                        sum[0][e] += f[0][e];
+                        sum[1][e] += f[1][e];
+                    }
+                    if (a.dst && r < rows_up) {
+                        store_terms<TERMS>(a.dst + r * 2 * a.ldz + c, a.plane, f[0]);
+                        store_terms<TERMS>(a.dst + r * 2 * a.ldz + a.ldz + c, a.plane, f[1]);
+                    }
+                }
+            }
+        }
+        if (!a.sum_gate && !a.sum_up) continue;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sums[p][wave][lane * 8 + e] = sum[p][e];
+        __syncthreads();
+        for (int x = threadIdx.x; x < 1024; x += 256) {
+            const int p = x >> 9, y = x & 511;
+            float *to = p ? a.sum_up : a.sum_gate;
+            if (to && c0 + y < a.n) to[down * a.n + c0 + y] = (sums[p][0][y] + sums[p][1][y]) + (sums[p][2][y] + sums[p][3][y]);
+        }
+        __syncthreads();
+    }
+}
+
 // Column sums of the blocks' partial sums: 64 columns a workgroup, sixteen waves over the blocks,
 // eight loads in flight in each.
 __global__ void __launch_bounds__(1024) bdlm_colsum_kernel(const float *part, int blocks, int cols, float *out) {
@@ -246,6 +309,25 @@ int launch_pack(const PackArgs &a, void *stream) {
         case 8: hipLaunchKernelGGL((bdlm_pack_kernel<false, false, false, 3>), g, b, 0, s, a); break;
         case 10: hipLaunchKernelGGL((bdlm_pack_kernel<false, true, false, 3>), g, b, 0, s, a); break;
         default: return BDLM_E_LAUNCH;
+    }
+    return done();
+}
+
+int launch_gated_pack(const GatedPackArgs &a, void *stream) {
+    if (a.rows <= 0) return BDLM_OK;
+    const int64_t blocks = (a.ldz + 511) / 512 * pack_row_blocks(a.rows);
+    const dim3 g(static_cast<unsigned>(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22)), b(256);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    // (bf16 inputs: one or two terms; fp32: three)
+    if (a.terms == 1) {
+        if (a.dh_bf16) hipLaunchKernelGGL((bdlm_gated_pack_kernel<true, true, 1>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((bdlm_gated_pack_kernel<false, true, 1>), g, b, 0, s, a);
+    } else if (a.terms == 2) {
+        if (a.dh_bf16) hipLaunchKernelGGL((bdlm_gated_pack_kernel<true, true, 2>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((bdlm_gated_pack_kernel<false, true, 2>), g, b, 0, s, a);
+    } else {
+        if (a.dh_bf16) hipLaunchKernelGGL((bdlm_gated_pack_kernel<true, false, 3>), g, b, 0, s, a);
+        else hipLaunchKernelGGL((bdlm_gated_pack_kernel<false, false, 3>), g, b, 0, s, a);
     }
     return done();
 }

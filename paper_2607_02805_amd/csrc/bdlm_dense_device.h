@@ -128,6 +128,24 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     return 1.f;
 }
 
+// act(z) and d act / dz together
+template <bool FINE>
+__device__ __forceinline__ void act_both(float z, int act, float &value, float &slope) {
+    if (act == BDLM_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z));
+        value = z < -87.f ? 0.f : z * s;
+        slope = z < -87.f ? 0.f : z > 87.f ? 1.f : s * fmaf(z, 1.f - s, 1.f);
+    } else if (act == BDLM_ACT_GELU) {
+        float e;
+        const float p = normal_cdf<FINE>(z, e);
+        value = z < -14.f ? 0.f : z * p;
+        slope = z < -14.f ? 0.f : z > 14.f ? 1.f : fmaf(z * 0.39894228f, e, p);
+    } else {
+        value = z;
+        slope = 1.f;
+    }
+}
+
 // A softmax record: the largest value, its column (the lowest of equals), and the sum over the
 // other columns of exp(value - largest).  The largest one's own 1 stays out of the sum, so that a
 // log-probability near 0, -log(1 + others), keeps its digits.

@@ -177,6 +177,7 @@ inline TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, 
     a.ncol = static_cast<int32_t>(ncol);
     a.k = static_cast<int32_t>(k);
     a.npair = npair;
+    a.half = npair;
     a.row_t = row_t;
     a.col_t = col_t;
     a.skip = -1;

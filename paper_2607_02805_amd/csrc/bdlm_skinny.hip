@@ -87,15 +87,18 @@ __global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const Sk
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
     const int s = lane & 15, kg = lane >> 4;
-    const int col0 = blockIdx.x * kCols;
+    // gated: group 0 is 16 columns of the gate's weights, group 1 the same of the other's
+    constexpr bool kGated = OUT == kTileGated;
+    static_assert(!kGated || G == 2, "a group of either matrix");
+    const int col0 = blockIdx.x * (kGated ? 16 : kCols);
     const int esz = BF16 ? 2 : 4;
     const int nrow = a.nrow_dev ? *a.nrow_dev : a.nrow;
     if (nrow <= 0) return;
     const char *wrow[G], *xrow[MT];
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        const int c = col0 + 16 * g + s;
-        wrow[g] = static_cast<const char *>(a.w) + int64_t(c < a.ncol ? c : a.ncol - 1) * a.ldw * esz;
+        const int c = col0 + (kGated ? 0 : 16 * g) + s;
+        wrow[g] = static_cast<const char *>(kGated && g == 1 ? a.w2 : a.w) + int64_t(c < a.ncol ? c : a.ncol - 1) * a.ldw * esz;
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -147,6 +150,19 @@ __global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const Sk
         for (int m = 0; m < MT; ++m)
             *reinterpret_cast<f32x4 *>(part + (wave * 16 * MT + 16 * m + s) * kPitch + 16 * g + 4 * kg) = acc[g][m];
     __syncthreads();
+    if constexpr (kGated) {
+        for (int x = threadIdx.x; x < 16 * MT * 4; x += blockDim.x) {
+            const int r = x >> 2, c = (x & 3) * 4;
+            f32x4 gate = gated_bias(a.gated.bias_gate, col0 + c, a.gated.n), up = gated_bias(a.gated.bias_up, col0 + c, a.gated.n);
+            for (int w = 0; w < waves; ++w) {
+                const float *p = part + (w * 16 * MT + r) * kPitch + c;
+                gate += *reinterpret_cast<const f32x4 *>(p);
+                up += *reinterpret_cast<const f32x4 *>(p + 16);
+            }
+            if (r < nrow) gated4(a.gated, gate, up, r, col0 + c);
+        }
+        return;
+    }
     constexpr int kQuads = kCols / 4;
     for (int x = threadIdx.x; x < 16 * MT * kQuads; x += blockDim.x) {
         const int r = x / kQuads, c = x % kQuads * 4;
@@ -195,15 +211,17 @@ hipError_t launch_cols_of(const SkinnyArgs &a, hipStream_t s) {
     constexpr int kMost = BF16 ? 16 : 8, kRoom = 32 / (MT * G);   // registers; LDS
     constexpr int most = kMost < kRoom ? kMost : kRoom;
     waves = waves < 1 ? 1 : waves > most ? most : waves;
-    const dim3 g((a.ncol + 16 * G - 1) / (16 * G)), blk(64 * waves);
+    const int across = a.out == kTileGated ? 16 : 16 * G;
+    const dim3 g((a.ncol + across - 1) / across), blk(64 * waves);
     const size_t lds = size_t(waves) * 16 * MT * (16 * G + 4) * 4;   // at most 40 KB
     if (a.out == kTileStore) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileStore>), g, blk, lds, s, a);
+    else if (a.out == kTileGated) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, 2, BF16, kTileGated>), g, blk, lds, s, a);
     else hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileBest>), g, blk, lds, s, a);
     return hipGetLastError();
 }
 template <int MT, bool BF16>
 hipError_t launch_rows_of(const SkinnyArgs &a, hipStream_t s) {
-    return skinny_cols(a.ncol) == 32 ? launch_cols_of<MT, 2, BF16>(a, s) : launch_cols_of<MT, 1, BF16>(a, s);
+    return a.out == kTileGated || skinny_cols(a.ncol) == 32 ? launch_cols_of<MT, 2, BF16>(a, s) : launch_cols_of<MT, 1, BF16>(a, s);
 }
 
 }  // namespace

@@ -1,4 +1,4 @@
-// bdlm_store.h -- the epilogue of a projection, four consecutive columns of a row at a time, shared by
+// bdlm_store.h -- the epilogues of a projection and of a gated one, four consecutive columns of a row at a time, shared by
 // the kernels that end one (bdlm_tile.hip, bdlm_skinny.hip).  Internal.
 #pragma once
 
@@ -78,6 +78,49 @@ __device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, f32x4 bias, 
         else
             for (int e = 0; e < n; ++e) p[e] = v[e];
     }
+}
+
+// Four consecutive values to a row of bf16 or fp32, n of which there are.
+__device__ __forceinline__ void put4(void *dst, int64_t o, int n, bool whole, bool bf16, f32x4 v) {
+    if (bf16) {
+        uint16_t *p = static_cast<uint16_t *>(dst) + o;
+        if (whole) *reinterpret_cast<uint2 *>(p) = uint2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+        else
+            for (int e = 0; e < n; ++e) p[e] = static_cast<uint16_t>(bf16_bits(v[e]));
+    } else {
+        float *p = static_cast<float *>(dst) + o;
+        if (whole) *reinterpret_cast<f32x4 *>(p) = v;
+        else
+            for (int e = 0; e < n; ++e) p[e] = v[e];
+    }
+}
+__device__ __forceinline__ f32x4 gated_bias(const float *bias, int col, int n) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (bias) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < n) v[e] = bias[col + e];
+    }
+    return v;
+}
+// Four consecutive columns of one row of a gated product, biases added already: act(gate) * up, of the unrounded ones.
+__device__ __forceinline__ void gated4(const GatedArgs &a, f32x4 gate, f32x4 up, int64_t row, int col) {
+    const int n = a.n - col < 4 ? a.n - col : 4;
+    if (n <= 0) return;
+    if (a.pre_gate) {
+        const int64_t o = row * a.ld_pre + col;
+        const bool whole = n == 4 && a.ld_pre % 4 == 0;
+        put4(a.pre_gate, o, n, whole, a.pre_bf16, gate);
+        put4(a.pre_up, o, n, whole, a.pre_bf16, up);
+    }
+    if (a.act == BDLM_ACT_GELU && !a.out_bf16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) gate[e] = act_value<true>(gate[e], BDLM_ACT_GELU);
+    } else if (a.act != BDLM_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) gate[e] = act_value<false>(gate[e], a.act);
+    }
+    put4(a.out, row * a.ld_out + col, n, n == 4 && a.ld_out % 4 == 0, a.out_bf16, gate * up);
 }
 
 }  // namespace

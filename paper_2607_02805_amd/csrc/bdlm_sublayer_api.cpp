@@ -1,5 +1,6 @@
 // bdlm_sublayer_api.cpp -- the C ABI of the operators of a sublayer (include/bdlm.h): the norm at its entry, with
-// the residual's addition, and its gradient.  Argument checks, workspaces and launches.
+// the residual's addition, the gated product of an MLP, and their gradients.  Argument checks, the plan of a call
+// and its launches; a plan depends on the descriptor alone.
 #include <stdint.h>
 
 #include <algorithm>
@@ -30,6 +31,75 @@ int64_t scales_of(int64_t width, int64_t block) { return block ? (width + block 
 int64_t norm_space(int64_t rows, int64_t width) {
     return up(int64_t(bdlm::add_norm_grad_blocks(rows, width)) * width * 4, 256);
 }
+
+// From one operand to the other, in elements.
+int64_t between(const Mat &a, const Mat &b) {
+    return static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) / 2;
+}
+
+struct GatedPlan {
+    bool skinny;
+    Space ws;
+    Operand x, wg, wu;         // (laid out anew, the weights lie one behind the other)
+    Shape shape;
+    float *part;
+    GatedPlan(const bdlm_dense_desc_t &d, const void *px, const void *pg, const void *pu, void *p)
+        : skinny(few(d)), ws(p),
+          x(px, skinny ? 0 : d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
+          wg(pg, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
+          wu(pu, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
+        const int64_t cols = gated_columns(d.out_features);
+        shape = skinny ? Shape{false, 1, true}
+                       : shape_of(d.rows, cols, steps_of(d.in_features, pairs_of(d.in_dtype)), true);
+        part = ws.take<float>(part_size(shape, d.rows, cols));
+    }
+    bool fits() const { return shape.fits; }
+};
+
+// The gradients by both factors lie side by side, [terms][rows][2 ldz]: one product over both for dx, and one whose rows
+// are those of both weights.
+struct GatedBackwardPlan {
+    Space ws;
+    Operand x, wg, wu;
+    int64_t ldz, plane;
+    Shape sx, sw;
+    uint16_t *dz;
+    float *part, *sum_gate, *sum_up;
+    GatedBackwardPlan(const bdlm_dense_desc_t &d, const void *px, const void *pg, const void *pu, void *p)
+        : ws(p), x(px, d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
+          wg(pg, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
+          wu(pu, d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws) {
+        const int32_t np = grad_pairs(grad_terms(d));
+        ldz = up(d.out_features, 64);
+        plane = up(d.rows, 64) * 2 * ldz;
+        const int64_t both = ldz + d.out_features;
+        sx = shape_of(d.rows, d.in_features, steps_of(d.out_features, 2 * np), true);
+        sw = shape_of(both, d.in_features, steps_of(d.rows, np), true, true);
+        dz = ws.take<uint16_t>(grad_terms(d) * plane);
+        const int64_t sums = int64_t(pack_row_blocks(static_cast<int32_t>(d.rows))) * d.out_features;
+        sum_gate = ws.take<float>(sums);
+        sum_up = ws.take<float>(sums);
+        part = ws.take<float>(std::max(part_size(sx, d.rows, d.in_features), part_size(sw, both, d.in_features)));
+    }
+    bool fits() const { return sx.fits && sw.fits; }
+};
+
+template <class P>
+int gated_query(const bdlm_dense_desc_t *d, int64_t *bytes) {
+    TRY(check_desc(d));
+    if (!bytes) return BDLM_E_NULL;
+    *bytes = P(*d, nullptr, nullptr, nullptr, nullptr).ws.used;
+    return BDLM_OK;
+}
+template <class P>
+int gated_space(const bdlm_dense_desc_t *d, const void *ws, int64_t bytes) {
+    const P plan(*d, nullptr, nullptr, nullptr, nullptr);
+    if (!plan.fits()) return BDLM_E_SHAPE;
+    if (plan.ws.used == 0) return BDLM_OK;
+    if (!ws || bytes < plan.ws.used) return BDLM_E_WORKSPACE;
+    return aligned(ws, 256) ? BDLM_OK : BDLM_E_ALIGN;
+}
+int check_act(int32_t act) { return act < BDLM_ACT_NONE || act > BDLM_ACT_GELU ? BDLM_E_SHAPE : BDLM_OK; }
 
 }  // namespace
 
@@ -148,6 +218,162 @@ int bdlm_add_rmsnorm_backward(int64_t rows, int64_t width, int32_t dy_dtype, con
     a.eps = eps;
     TRY(launch_add_norm_grad(a, stream));
     return dw ? launch_colsum(a.part, add_norm_grad_blocks(rows, width), a.width, dw, stream) : BDLM_OK;
+}
+
+int bdlm_gated_projection_workspace(const bdlm_dense_desc_t *d, int64_t *bytes) { return gated_query<GatedPlan>(d, bytes); }
+int bdlm_gated_projection_backward_workspace(const bdlm_dense_desc_t *d, int64_t *bytes) {
+    return gated_query<GatedBackwardPlan>(d, bytes);
+}
+
+int bdlm_check_gated_projection(const bdlm_dense_desc_t *d, int32_t act, int32_t out_dtype, const void *x,
+                                const void *w_gate, const void *w_up, const float *bias_gate, const float *bias_up,
+                                const void *out, int64_t out_stride, const void *pre_gate, const void *pre_up,
+                                int64_t pre_stride, const void *ws, int64_t ws_bytes) {
+    TRY(check_desc(d));
+    if (!known(out_dtype)) return BDLM_E_DTYPE;
+    TRY(check_act(act));
+    TRY(check_inputs(d, x, w_gate));
+    TRY(check_in(w_up, d->out_features));
+    if (!aligned(bias_gate, 4) || !aligned(bias_up, 4)) return BDLM_E_ALIGN;
+    TRY(check_out(out, d->rows, d->out_features, out_stride));
+    if (!pre_gate != !pre_up) return BDLM_E_NULL;
+    if (pre_gate) {
+        TRY(check_out(pre_gate, d->rows, d->out_features, pre_stride));
+        TRY(check_out(pre_up, d->rows, d->out_features, pre_stride));
+    }
+    const int64_t es = elem_size(d->in_dtype);
+    const Span so(out, d->rows, d->out_features, out_stride, elem_size(out_dtype)),
+        pg(pre_gate, d->rows, d->out_features, pre_stride, es), pu(pre_up, d->rows, d->out_features, pre_stride, es),
+        bg(bias_gate, 1, d->out_features, 0, 4), bu(bias_up, 1, d->out_features, 0, 4), sx = span_x(d, x),
+        wg = span_w(d, w_gate), wu = span_w(d, w_up);
+    TRY(gated_space<GatedPlan>(d, ws, ws_bytes));
+    const Span ss(ws, 1, ws_bytes, 0, 1);
+    if (!apart(so, sx, wg, wu, bg, bu, pg, pu) || !apart(pg, sx, wg, wu, bg, bu, pu) || !apart(pu, sx, wg, wu, bg, bu))
+        return BDLM_E_SHAPE;
+    return apart(ss, so, pg, pu, sx, wg, wu, bg, bu) ? BDLM_OK : BDLM_E_WORKSPACE;
+}
+
+int bdlm_gated_projection(const bdlm_dense_desc_t *d, int32_t act, int32_t out_dtype, const void *x, const void *w_gate,
+                          const void *w_up, const float *bias_gate, const float *bias_up, void *out, int64_t out_stride,
+                          void *pre_gate, void *pre_up, int64_t pre_stride, void *ws, int64_t ws_bytes, void *stream) {
+    TRY(bdlm_check_gated_projection(d, act, out_dtype, x, w_gate, w_up, bias_gate, bias_up, out, out_stride, pre_gate,
+                                    pre_up, pre_stride, ws, ws_bytes));
+    if (d->rows == 0) return BDLM_OK;
+    GatedPlan p(*d, x, w_gate, w_up, ws);
+    const GatedArgs g{out, bias_gate, bias_up, pre_gate, pre_up, out_stride, pre_stride, out_dtype == BDLM_DTYPE_BF16,
+                      d->in_dtype == BDLM_DTYPE_BF16, act, static_cast<int32_t>(d->out_features)};
+    if (p.skinny) {
+        SkinnyArgs a = few_rows(*d, x, w_gate, kTileGated);
+        a.w2 = w_up;
+        a.gated = g;
+        return launch_skinny(a, stream);
+    }
+    TRY(p.x.lay(stream));
+    TRY(p.wg.lay(stream));
+    TRY(p.wu.lay(stream));
+    TileArgs a = product(p.x.mat, false, p.wg.mat, false, d->rows, gated_columns(d->out_features), d->in_features,
+                         pairs_of(d->in_dtype), p.shape);
+    a.col_duo = between(p.wg.mat, p.wu.mat);
+    a.gated = g;
+    a.out = p.shape.splits > 1 ? kTileGatedPart : kTileGated;
+    a.part = p.part;
+    TRY(launch_tile(a, stream));
+    return p.shape.splits > 1 ? launch_join_gated(p.part, p.shape.splits, a.nrow, g, stream) : BDLM_OK;
+}
+
+int bdlm_check_gated_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int32_t dh_dtype, const void *dh,
+                                         int64_t dh_stride, const void *x, const void *w_gate, const void *w_up,
+                                         const void *pre_gate, const void *pre_up, int64_t pre_stride, const void *dx,
+                                         int64_t dx_stride, const void *dw_gate, const void *dw_up, int64_t dw_stride,
+                                         const float *db_gate, const float *db_up, const void *ws, int64_t ws_bytes) {
+    TRY(check_desc(d));
+    if (!known(dh_dtype)) return BDLM_E_DTYPE;
+    TRY(check_act(act));
+    // x is read for the weights' gradients alone, the weights for dx alone
+    TRY(check_in(x, dw_gate || dw_up ? d->rows : 0));
+    TRY(check_in(w_gate, dx ? d->out_features : 0));
+    TRY(check_in(w_up, dx ? d->out_features : 0));
+    TRY(check_rows(dh, d->rows, dh_stride));
+    TRY(check_rows(pre_gate, d->rows, pre_stride));
+    TRY(check_rows(pre_up, d->rows, pre_stride));
+    if (dx) TRY(check_out(dx, d->rows, d->in_features, dx_stride));
+    if (dw_gate) TRY(check_out(dw_gate, d->out_features, d->in_features, dw_stride));
+    if (dw_up) TRY(check_out(dw_up, d->out_features, d->in_features, dw_stride));
+    if (!aligned(db_gate, 4) || !aligned(db_up, 4)) return BDLM_E_ALIGN;
+    const int64_t es = elem_size(d->in_dtype), n = d->out_features, k = d->in_features;
+    const Span sx = span_x(d, x), wg = span_w(d, w_gate), wu = span_w(d, w_up),
+               sh(dh, d->rows, n, dh_stride, elem_size(dh_dtype)), pg(pre_gate, d->rows, n, pre_stride, es),
+               pu(pre_up, d->rows, n, pre_stride, es), gx(dx, d->rows, k, dx_stride, es),
+               gg(dw_gate, n, k, dw_stride, es), gu(dw_up, n, k, dw_stride, es), bg(db_gate, 1, n, 0, 4),
+               bu(db_up, 1, n, 0, 4);
+    TRY(gated_space<GatedBackwardPlan>(d, ws, ws_bytes));
+    const Span ss(ws, 1, ws_bytes, 0, 1);
+    if (!apart(gx, sx, wg, wu, sh, pg, pu, gg, gu, bg, bu) || !apart(gg, sx, wg, wu, sh, pg, pu, gu, bg, bu) ||
+        !apart(gu, sx, wg, wu, sh, pg, pu, bg, bu) || !apart(bg, sx, wg, wu, sh, pg, pu, bu) ||
+        !apart(bu, sx, wg, wu, sh, pg, pu))
+        return BDLM_E_SHAPE;
+    return apart(ss, sx, wg, wu, sh, pg, pu, gx, gg, gu, bg, bu) ? BDLM_OK : BDLM_E_WORKSPACE;
+}
+
+int bdlm_gated_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int32_t dh_dtype, const void *dh,
+                                   int64_t dh_stride, const void *x, const void *w_gate, const void *w_up,
+                                   const void *pre_gate, const void *pre_up, int64_t pre_stride, void *dx,
+                                   int64_t dx_stride, void *dw_gate, void *dw_up, int64_t dw_stride, float *db_gate,
+                                   float *db_up, void *ws, int64_t ws_bytes, void *stream) {
+    TRY(bdlm_check_gated_projection_backward(d, act, dh_dtype, dh, dh_stride, x, w_gate, w_up, pre_gate, pre_up,
+                                             pre_stride, dx, dx_stride, dw_gate, dw_up, dw_stride, db_gate, db_up, ws,
+                                             ws_bytes));
+    if (!dx && !dw_gate && !dw_up && !db_gate && !db_up) return BDLM_OK;
+    GatedBackwardPlan p(*d, x, w_gate, w_up, ws);
+    const int terms = grad_terms(*d);
+    const int32_t np = grad_pairs(terms), n = static_cast<int32_t>(d->out_features);
+    GatedPackArgs g{};
+    g.dh = dh;
+    g.gate = pre_gate;
+    g.up = pre_up;
+    g.ld_dh = dh_stride;
+    g.ld_pre = pre_stride;
+    g.ldz = p.ldz;
+    g.plane = p.plane;
+    g.rows = static_cast<int32_t>(d->rows);
+    g.n = n;
+    g.dh_bf16 = dh_dtype == BDLM_DTYPE_BF16;
+    g.pre_bf16 = d->in_dtype == BDLM_DTYPE_BF16;
+    g.terms = terms;
+    g.act = act;
+    g.dst = dx || dw_gate || dw_up ? p.dz : nullptr;
+    g.sum_gate = db_gate ? p.sum_gate : nullptr;
+    g.sum_up = db_up ? p.sum_up : nullptr;
+    TRY(launch_gated_pack(g, stream));
+    if (db_gate) TRY(launch_colsum(p.sum_gate, pack_row_blocks(g.rows), n, db_gate, stream));
+    if (db_up) TRY(launch_colsum(p.sum_up, pack_row_blocks(g.rows), n, db_up, stream));
+    const Mat dz{p.dz, 2 * p.ldz, p.plane};
+    if (dx && d->rows > 0) {
+        TRY(p.wg.lay(stream));
+        TRY(p.wu.lay(stream));
+        TileArgs a = product(dz, false, p.wg.mat, true, d->rows, d->in_features, n, 2 * np, p.sx);
+        a.half = np;
+        a.row_duo = p.ldz;
+        a.col_duo = between(p.wg.mat, p.wu.mat);
+        TRY(store_product(a, plain_store(dx, dx_stride, d->in_dtype), p.part, stream));
+    }
+    if (!dw_gate && !dw_up) return BDLM_OK;
+    TRY(p.x.lay(stream));
+    if (!dw_gate || !dw_up) {
+        const Mat one{p.dz + (dw_gate ? 0 : p.ldz), dz.ld, dz.plane};
+        return store_product(product(one, true, p.x.mat, true, n, d->in_features, d->rows, np, p.sw),
+                             plain_store(dw_gate ? dw_gate : dw_up, dw_stride, d->in_dtype), p.part, stream);
+    }
+    TileArgs a = product(dz, true, p.x.mat, true, p.ldz + n, d->in_features, d->rows, np, p.sw);
+    a.store = plain_store(dw_gate, dw_stride, d->in_dtype);
+    a.two_out = dw_up;
+    a.two_rows = n;
+    a.two_at = static_cast<int32_t>(p.ldz);
+    a.out = p.sw.splits > 1 ? kTilePartial : kTileTwo;
+    a.part = p.part;
+    TRY(launch_tile(a, stream));
+    return p.sw.splits > 1 ? launch_join_two(p.part, p.sw.splits, a.nrow, a.ncol, a.two_out, a.two_rows, a.two_at, a.store, stream)
+                           : BDLM_OK;
 }
 
 }  // extern "C"

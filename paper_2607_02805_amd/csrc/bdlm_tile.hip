@@ -117,6 +117,22 @@ struct Stage {
             }
         }
     }
+    // Rows of two matrices in turn, 32 of either (GatedArgs): a wave copies rows of one of them.  first: the tile's first
+    // column of the product; size: rows of either matrix.
+    __device__ __forceinline__ void init_gated(const Mat &m, int64_t duo, int64_t first, int64_t size, int wave, int lane) {
+        static_assert(!T && kLoads * 8 <= 32 && 32 % (kLoads * 8) == 0, "a wave's rows are of one matrix");
+        ld2 = m.ld * 2;
+        const int up = (wave * kLoads * 8 >> 5) & 1;
+        first >>= 1;
+        base = reinterpret_cast<const char *>(m.p + (up ? duo : 0)) + first * ld2 - kLast;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int piece = (wave * kLoads + i) * 64 + lane, more = kLast - i * 1024;
+            const int r = piece >> 3, c = (piece & 7) ^ ((r >> 1) & 7), own = (r >> 6) * 32 + (r & 31);
+            const int64_t rr = first + own < size ? own : size - 1 - first;
+            off[i] = static_cast<uint32_t>(rr * ld2 + c * 16) + more;
+        }
+    }
     __device__ __forceinline__ const char *at_step(int64_t plane, int kt) const {
         return base + plane * 2 + kt * stride();
     }
@@ -188,13 +204,24 @@ struct RowData {
     int label;           // kTileProb, kTileBest
 };
 
+// Four columns of a row that goes to one of two matrices, or to neither.
+__device__ __forceinline__ void store_two(const StoreArgs &s, void *two_out, int two_rows, int two_at, f32x4 v, int64_t r, int c,
+                                          int ncol) {
+    const int n = ncol - c < 4 ? ncol - c : 4;
+    if (n <= 0 || (r >= two_rows && r < two_at)) return;
+    const bool second = r >= two_at;
+    put4(second ? two_out : s.out, (second ? r - two_at : r) * s.ld_out + c, n, n == 4 && s.ld_out % 4 == 0, s.out_bf16, v);
+}
+
 // Four columns of one row of a tile, in their place.
 template <int OUT>
 __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias, const RowData &d, int64_t r, int c,
                                           int nrow, int split) {
     if constexpr (OUT == kTileStore) {
         store4(a.store, v, bias, r, c, a.ncol);
-    } else if constexpr (OUT == kTilePartial) {
+    } else if constexpr (OUT == kTileTwo) {
+        store_two(a.store, a.two_out, a.two_rows, a.two_at, v, r, c, a.ncol);
+    } else if constexpr (OUT == kTilePartial || OUT == kTileGatedPart) {
         float *to = a.part + (int64_t(split) * (a.splits ? a.nrow : nrow) + r) * a.ncol + c;
         if (c + 4 <= a.ncol && a.ncol % 4 == 0) {
             if (a.add) v += *reinterpret_cast<const f32x4 *>(to);
@@ -328,7 +355,9 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
 
     Stage<E, COLT, WAVES, true> sc;
     Stage<E, ROWT, WAVES, false> sr;
-    sc.init(a.col, col0, a.ncol, wave, lane);
+    constexpr bool kGated = OUT == kTileGated || OUT == kTileGatedPart;
+    if constexpr (kGated) sc.init_gated(a.col, a.col_duo, col0, a.gated.n, wave, lane);
+    else sc.init(a.col, col0, a.ncol, wave, lane);
     sr.init(a.row, row0, nrow, wave, lane);
     const int wr = wave % WR, wc = wave / WR % WC, half = wave / (WR * WC);
     Reader<E, COLT, FC, kWaveGroups> rc;
@@ -369,15 +398,15 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
         int left, skip;
     };
     int pair = it0 / (nkt > 0 ? nkt : 1), kt = it0 - pair * nkt;
-    From next{sc.at_step(col_term(a.npair, pair) * a.col.plane, kt),
-              sr.at_step(row_term(a.npair, pair) * a.row.plane, kt), K - kt * kDepth, a.skip - kt * kDepth};
+    auto col_at = [&](int i) { return i < a.half ? col_term(a.half, i) * a.col.plane : a.col_duo + col_term(a.half, i - a.half) * a.col.plane; };
+    auto row_at = [&](int i) { return i < a.half ? row_term(a.half, i) * a.row.plane : a.row_duo + row_term(a.half, i - a.half) * a.row.plane; };
+    From next{sc.at_step(col_at(pair), kt), sr.at_step(row_at(pair), kt), K - kt * kDepth, a.skip - kt * kDepth};
     auto advance = [&]() {   // (past the last stage: to addresses that are not read)
         next = From{next.c + sc.stride(), next.r + sr.stride(), next.left - kDepth, next.skip - kDepth};
         if (++kt == nkt) {   // (more than one pair of planes)
             kt = 0;
             ++pair;
-            next = From{sc.at_step(col_term(a.npair, pair) * a.col.plane, 0),
-                        sr.at_step(row_term(a.npair, pair) * a.row.plane, 0), K, a.skip};
+            next = From{sc.at_step(col_at(pair), 0), sr.at_step(row_at(pair), 0), K, a.skip};
         }
     };
     constexpr int kLoads = Stage<E, COLT, WAVES, true>::kLoads;   // of either operand
@@ -484,6 +513,13 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     const int quad = lane % kQuads, sub = lane / kQuads;
     f32x4 bias = {0.f, 0.f, 0.f, 0.f};
     if constexpr (OUT == kTileStore) bias = load_bias(a.store, col1 + 4 * quad, a.ncol);
+    // gated: lanes of eight quads, whose columns are half of the wave's
+    const int gate_quad = lane & 7, gate_sub = lane >> 3, gate_col = (col1 >> 1) + 4 * gate_quad;
+    f32x4 bias_up = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (OUT == kTileGated) {
+        bias = gated_bias(a.gated.bias_gate, gate_col, a.gated.n);
+        bias_up = gated_bias(a.gated.bias_up, gate_col, a.gated.n);
+    }
     auto part = [&](auto j0_) {
         constexpr int j0 = decltype(j0_)::value;
         const int r1 = wr * (E / WR) + 32 * j0;   // the part's first row in the tile
@@ -526,6 +562,16 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
                     a.best.label_logit[row0 + r1 + lane] = label == m.at ? m.top : v;
                 }
             }
+        } else if constexpr (OUT == kTileGated) {
+            static_assert(kCols == 64, "a fragment of either matrix");
+            const int most = static_cast<int>(rows_out - row0) - r1;
+            // (rows eight apart in a pass: their quads lie in both halves of the banks)
+#pragma unroll 4
+            for (int k = 0; k < 8 / KS; ++k) {
+                const int x = half * (8 / KS) + k + 8 * gate_sub;
+                const f32x4 gate = mine[x * kQuads + (gate_quad ^ (x & 15))], up = mine[x * kQuads + ((gate_quad + 8) ^ (x & 15))];
+                if (x < most) gated4(a.gated, gate + bias, up + bias_up, row0 + r1 + x, gate_col);
+            }
         } else {
             const int most = static_cast<int>(rows_out - row0) - r1;
 #pragma unroll 4
@@ -567,8 +613,23 @@ hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
     return hipGetLastError();
 }
 
-// out = epilogue(sum of the slices), four columns per thread; four slices are asked for at a time
-// (one after the other, 128 x 1,024 in 16 slices took 4 us more)
+// The sum of the slices at p, four columns.  Four slices are asked for at a time (one after the other, 128 x 1,024 in 16
+// slices took 4 us more).
+__device__ __forceinline__ f32x4 sum_slices(const float *p, int64_t slice, int splits) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    int k = 0;
+    for (; k + 4 <= splits; k += 4) {
+        f32x4 u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const f32x4 *>(p + (k + j) * slice);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v += u[j];
+    }
+    for (; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(p + k * slice);
+    return v;
+}
+
+// out = epilogue(sum of the slices), four columns per thread
 __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int splits, int edge, int nrow, int ncol,
                                                         const int32_t *nrow_dev, const float *scale, const StoreArgs s) {
     const int quads = (ncol + 3) / 4;
@@ -581,15 +642,7 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
         const float *p = part + r * ncol + c;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
         if (ncol % 4 == 0) {
-            int k = 0;
-            for (; k + 4 <= splits; k += 4) {
-                f32x4 u[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const f32x4 *>(p + (k + j) * slice);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v += u[j];
-            }
-            for (; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(p + k * slice);
+            v = sum_slices(p, slice, splits);
         } else {
             for (int k = 0; k < splits; ++k)
                 for (int e = 0; e < 4; ++e)
@@ -597,6 +650,38 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
         }
         if (scale) v *= scale[r];
         store4(s, v, load_bias(s, c, ncol), r, c, ncol);
+    }
+}
+
+__global__ void __launch_bounds__(256) bdlm_join_two_kernel(const float *part, int splits, int nrow, int ncol, void *two_out,
+                                                            int two_rows, int two_at, const StoreArgs s) {
+    const int quads = (ncol + 3) / 4;
+    const int64_t slice = int64_t(nrow) * ncol, all = int64_t(nrow) * quads;
+    for (int64_t x = blockIdx.x * int64_t(256) + threadIdx.x; x < all; x += gridDim.x * int64_t(256)) {
+        const int64_t r = x / quads;
+        const int c = static_cast<int>(x - r * quads) * 4;
+        const float *p = part + r * ncol + c;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (ncol % 4 == 0) {
+            v = sum_slices(p, slice, splits);
+        } else {
+            for (int k = 0; k < splits; ++k)
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < ncol) v[e] += p[k * slice + e];
+        }
+        store_two(s, two_out, two_rows, two_at, v, r, c, ncol);
+    }
+}
+
+__global__ void __launch_bounds__(256) bdlm_join_gated_kernel(const float *part, int splits, int nrow, const GatedArgs g) {
+    const int quads = (g.n + 3) / 4;
+    const int64_t ncol = int64_t(g.n + 31) / 32 * 64, slice = nrow * ncol, all = int64_t(nrow) * quads;
+    for (int64_t x = blockIdx.x * int64_t(256) + threadIdx.x; x < all; x += gridDim.x * int64_t(256)) {
+        const int64_t r = x / quads;
+        const int c = static_cast<int>(x - r * quads) * 4;
+        const float *p = part + r * ncol + (c >> 5) * 64 + (c & 31);
+        const f32x4 gate = sum_slices(p, slice, splits), up = sum_slices(p + 32, slice, splits);
+        gated4(g, gate + gated_bias(g.bias_gate, c, g.n), up + gated_bias(g.bias_up, c, g.n), r, c);
     }
 }
 
@@ -620,9 +705,13 @@ int launch_tile(const TileArgs &a, void *stream) {
         if (lay == 0) r = launch_one<false, false, kTilePartial>(a, g, s);
         else if (lay == 1) r = launch_one<false, true, kTilePartial>(a, g, s);
         else if (lay == 3) r = launch_one<true, true, kTilePartial>(a, g, s);
+    } else if (a.out == kTileTwo) {
+        if (lay == 3) r = launch_one<true, true, kTileTwo>(a, g, s);
     } else if (lay == 0) {
-        r = a.out == kTileBest ? launch_one<false, false, kTileBest>(a, g, s)
-                               : launch_one<false, false, kTileProb>(a, g, s);
+        if (a.out == kTileBest) r = launch_one<false, false, kTileBest>(a, g, s);
+        else if (a.out == kTileProb) r = launch_one<false, false, kTileProb>(a, g, s);
+        else if (a.out == kTileGated) r = launch_one<false, false, kTileGated>(a, g, s);
+        else if (a.out == kTileGatedPart) r = launch_one<false, false, kTileGatedPart>(a, g, s);
     }
     return r == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }
@@ -634,6 +723,23 @@ int launch_join(const float *part, int32_t splits, int32_t big, int32_t nrow, in
     const dim3 g(static_cast<unsigned>(blocks < 8192 ? blocks : 8192));
     hipLaunchKernelGGL(bdlm_join_kernel, g, dim3(256), 0, static_cast<hipStream_t>(stream), part, splits,
                        tile_edge(big), nrow, ncol, nrow_dev, scale, s);
+    return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
+}
+
+int launch_join_two(const float *part, int32_t splits, int32_t nrow, int32_t ncol, void *two_out, int32_t two_rows,
+                    int32_t two_at, const StoreArgs &s, void *stream) {
+    if (nrow <= 0 || ncol <= 0) return BDLM_OK;
+    const int64_t blocks = (int64_t(nrow) * ((ncol + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL(bdlm_join_two_kernel, dim3(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), part, splits, nrow, ncol, two_out, two_rows, two_at, s);
+    return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
+}
+
+int launch_join_gated(const float *part, int32_t splits, int32_t nrow, const GatedArgs &g, void *stream) {
+    if (nrow <= 0 || g.n <= 0) return BDLM_OK;
+    const int64_t blocks = (int64_t(nrow) * ((g.n + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL(bdlm_join_gated_kernel, dim3(static_cast<unsigned>(blocks < 8192 ? blocks : 8192)), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), part, splits, nrow, g);
     return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }
 

@@ -90,3 +90,105 @@ def test_norm_binding_refuses():
     for call in (lambda: bd.add_rmsnorm(x, w), lambda: bd.add_rmsnorm_backward(x, x, w)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+WG, WU, BG, BU, PG, PU, DWG, DWU, DBG, DBU, DX = (A * i for i in range(20, 31))
+
+
+def desc(rows=100, k=72, n=130, dtype=BF, **kw):
+    d = bd.DenseDesc()
+    assert bd.lib().bdlm_dense_desc_init(ctypes.byref(d), rows, k, n, dtype) == 0
+    for name, v in kw.items():
+        setattr(d, name, v)
+    return d
+
+
+def gated(d, act=1, ot=BF, x=X, wg=WG, wu=WU, bg=BG, bu=BU, out=OUT, ldo=None, pg=PG, pu=PU, ldp=None, ws=WS, size=BIG):
+    n = d.out_features
+    return bd.lib().bdlm_check_gated_projection(ctypes.byref(d), act, ot, x, wg, wu, bg, bu, out, n if ldo is None else ldo,
+                                                pg, pu, n if ldp is None else ldp, ws, size)
+
+
+def gated_grad(d, act=1, ht=BF, dh=DY, ldh=None, x=X, wg=WG, wu=WU, pg=PG, pu=PU, ldp=None, dx=DX, ldx=None, dwg=DWG,
+               dwu=DWU, ldw=None, dbg=DBG, dbu=DBU, ws=WS, size=BIG):
+    n, k = d.out_features, d.in_features
+    return bd.lib().bdlm_check_gated_projection_backward(
+        ctypes.byref(d), act, ht, dh, n if ldh is None else ldh, x, wg, wu, pg, pu, n if ldp is None else ldp, dx,
+        k if ldx is None else ldx, dwg, dwu, k if ldw is None else ldw, dbg, dbu, ws, size)
+
+
+@pytest.mark.parametrize("call", [gated, gated_grad])
+def test_gated_descriptor(call):
+    assert call(desc()) == bd.OK and call(desc(rows=0), x=None) == bd.OK
+    for bad in (dict(rows=-1), dict(k=0), dict(n=0), dict(rows=(1 << 22) + 1), dict(k=(1 << 22) + 1), dict(n=(1 << 22) + 1),
+                dict(x_stride=-1), dict(w_stride=-1), dict(w_stride=(1 << 40) + 1)):
+        assert call(desc(**bad)) == bd.E_SHAPE, bad
+    for bad in (dict(dtype=2), dict(reserved=1)):
+        assert call(desc(**bad)) == bd.E_DTYPE, bad
+    d = desc(rows=200)
+    for p in ("x", "wg", "wu"):
+        assert call(d, **{p: None}) == bd.E_NULL and call(d, **{p: X * 40 + 8}) == bd.E_ALIGN, p
+    assert call(d, act=3) == bd.E_SHAPE and call(d, act=-1) == bd.E_SHAPE
+    assert call(d, ws=None) == bd.E_WORKSPACE and call(d, size=255) == bd.E_WORKSPACE and call(d, ws=WS + 64) == bd.E_ALIGN
+    # more threads than a launch holds
+    assert call(desc(rows=1 << 22, k=64, n=1 << 22), size=1 << 62) == bd.E_SHAPE
+
+
+def test_gated_arguments():
+    d = desc()
+    assert gated(d, ot=2) == bd.E_DTYPE and gated(d, out=None) == bd.E_NULL and gated(d, out=OUT + 8) == bd.E_ALIGN
+    assert gated(d, pg=None) == bd.E_NULL and gated(d, pu=None) == bd.E_NULL and gated(d, pg=None, pu=None) == bd.OK
+    assert gated(d, bg=None, bu=None) == bd.OK and gated(d, bg=BG + 2) == bd.E_ALIGN and gated(d, bu=BU + 1) == bd.E_ALIGN
+    assert gated(d, ldo=129) == bd.E_SHAPE and gated(d, ldp=129) == bd.E_SHAPE
+    assert gated(d, wu=WG) == bd.OK                             # the same weights twice
+    for p in (X, WG, WU, BG, BU, PG, PU):
+        assert gated(d, out=p) == bd.E_SHAPE
+    assert gated(d, pg=PU) == bd.E_SHAPE and gated(d, pu=X) == bd.E_SHAPE
+    assert gated(d, pu=PG + 130 * 2 + 12, ldp=400) == bd.OK and gated(d, pu=PG + 96 * 2, ldp=400) == bd.E_SHAPE
+    for p in (X, WG, WU, BG, BU, PG, PU, OUT):
+        assert gated(d, ws=p) == bd.E_WORKSPACE
+    need = ctypes.c_int64(-1)
+    f = bd.lib().bdlm_gated_projection_workspace
+    assert f(ctypes.byref(desc(rows=32)), ctypes.byref(need)) == 0 and need.value == 0
+    assert gated(desc(rows=32), ws=None, size=0) == bd.OK
+    assert f(None, ctypes.byref(need)) == bd.E_NULL and f(ctypes.byref(d), None) == bd.E_NULL
+    assert f(ctypes.byref(d), ctypes.byref(need)) == 0
+    assert gated(d, size=need.value) == bd.OK and gated(d, size=need.value - 1) == bd.E_WORKSPACE
+
+
+def test_gated_backward_arguments():
+    d = desc()
+    assert gated_grad(d, ht=2) == bd.E_DTYPE
+    for p in ("dh", "pg", "pu"):
+        assert gated_grad(d, **{p: None}) == bd.E_NULL and gated_grad(d, **{p: A * 50 + 8}) == bd.E_ALIGN, p
+    assert gated_grad(d, act=0, pg=None) == bd.E_NULL           # the product needs them without an activation too
+    assert gated_grad(d, x=None, dwg=None, dwu=None) == bd.OK and gated_grad(d, wg=None, wu=None, dx=None) == bd.OK
+    assert gated_grad(d, dx=None, dwg=None, dwu=None, dbg=None, dbu=None) == bd.OK
+    assert gated_grad(d, ldx=71) == bd.E_SHAPE and gated_grad(d, ldw=71) == bd.E_SHAPE and gated_grad(d, ldh=-1) == bd.E_SHAPE
+    assert gated_grad(d, dbg=DBG + 2) == bd.E_ALIGN and gated_grad(d, dwu=DWU + 8) == bd.E_ALIGN
+    outs = ("dx", "dwg", "dwu", "dbg", "dbu")
+    at = dict(dx=DX, dwg=DWG, dwu=DWU, dbg=DBG, dbu=DBU)
+    for o in outs:
+        for p in (X, WG, WU, DY, PG, PU):
+            assert gated_grad(d, **{o: p}) == bd.E_SHAPE, o
+        for other in outs:
+            if other != o:
+                assert gated_grad(d, **{o: at[other]}) == bd.E_SHAPE, (o, other)
+        assert gated_grad(d, ws=at[o]) == bd.E_WORKSPACE
+
+
+def test_gated_binding_refuses():
+    x, w = torch.zeros(4, 8), torch.ones(6, 8)
+    pre = (torch.zeros(4, 6), torch.zeros(4, 6))
+    for call in (lambda: bd.gated_projection(x, w, w), lambda: bd.gated_projection_backward(pre[0], x, w, w, pre)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    wide = torch.ones(6, 16)[:, :8]
+    for bad in (lambda: bd.gated_projection(x, w, wide), lambda: bd.gated_projection(x, w, w[:5]),
+                lambda: bd.gated_projection(x, w, w.bfloat16()), lambda: bd.gated_projection(x, w, w, act="relu"),
+                lambda: bd.gated_projection(x, w, w, pre=pre[0]), lambda: bd.gated_projection(x, w, w, pre=(pre[0], True)),
+                lambda: bd.gated_projection(x, w, w, pre=(pre[0], torch.zeros(4, 9)[:, :6])),
+                lambda: bd.gated_projection_backward(pre[0], x, w, w, None),
+                lambda: bd.gated_projection_backward(pre[0], x, w, w, pre, dw_gate=torch.zeros(6, 9)[:, :8])):
+        with pytest.raises(ValueError):
+            bad()
