@@ -635,6 +635,29 @@ int bdlm_head_select(const bdlm_dense_desc_t *desc, int64_t exclude, const void 
                      void *stream);
 
 /*
+ * What a head says of its tokens, per row: the log-probability of a given one, the entropy of the distribution, and the
+ * most probable ones, without the logits in memory (of up to 32 rows, fp32 64, and with alternatives they lie in the workspace).
+ * With logits l = x w^T over the vocabulary but `exclude` (as bdlm_head_loss), p = softmax(l):
+ *     logprob = log p[token],   entropy = - sum p log p.
+ * tokens       device int64 [rows], or NULL with logprob NULL (not wanted).  The logprob of `exclude` is -infinity, of a number
+ *              that is no token (negative, past the vocabulary: padding) 0.
+ * entropy      device fp32 [rows], or NULL.
+ * n_top        0 .. BDLM_MAX_TOP, and at most the tokens that the softmax ranges over.
+ * top_token, top_logprob  device int64 and fp32 [rows][n_top]: the n_top most probable tokens in order, of equal logits the lower
+ *              token first.  Tokens whose logit is NaN or -infinity are not listed: places past the others hold -1 and -infinity.
+ *              (NULL for n_top 0.)
+ * A logit that is NaN or +infinity makes the row's entropy and log-probabilities NaN.
+ * workspace    as large as the query says for the same descriptor and n_top.
+ * Errors: as bdlm_head_select.  rows == 0 enqueues nothing.
+ */
+#define BDLM_MAX_TOP 16
+int bdlm_head_logprobs_workspace(const bdlm_dense_desc_t *desc, int64_t n_top, int64_t *bytes);
+int bdlm_head_logprobs(const bdlm_dense_desc_t *desc, const int64_t *tokens, int64_t exclude,
+                       int64_t n_top, const void *x, const void *w, float *logprob,
+                       float *entropy, int64_t *top_token, float *top_logprob, void *workspace,
+                       int64_t workspace_bytes, void *stream);
+
+/*
  * Host-only argument checks used by the entry points above, exported so they
  * can be exercised without a GPU.  Same arguments (the stream is not needed),
  * same return codes; nothing is enqueued and nothing is modified.
@@ -742,6 +765,11 @@ int bdlm_check_head_loss_backward(const bdlm_dense_desc_t *desc, const int64_t *
 int bdlm_check_head_select(const bdlm_dense_desc_t *desc, int64_t exclude, const void *x,
                            const void *w, const int64_t *token, const float *logprob,
                            const void *workspace, int64_t workspace_bytes);
+int bdlm_check_head_logprobs(const bdlm_dense_desc_t *desc, const int64_t *tokens,
+                             int64_t exclude, int64_t n_top, const void *x, const void *w,
+                             const float *logprob, const float *entropy,
+                             const int64_t *top_token, const float *top_logprob,
+                             const void *workspace, int64_t workspace_bytes);
 
 #ifdef __cplusplus
 }

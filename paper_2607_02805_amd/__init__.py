@@ -25,6 +25,7 @@ Entry points (same names as the C ABI):
 * :func:`head_select`, :func:`head_loss`, :func:`head_loss_backward` -- the language-model head
   without its logits: the most probable tokens of a denoising step, and the masked training
   loss with its gradient.
+* :func:`head_logprobs` -- log-probabilities of given tokens, entropies and the most probable tokens.
 
 :class:`Cache` bundles a state pool with its host-side bookkeeping.
 """
@@ -48,6 +49,7 @@ SCRATCH_BYTES = 64 << 20     # BDLM_SCRATCH_BYTES: the no-allocation prefill's d
 DTYPE_F32 = 0
 DTYPE_BF16 = 1
 DTYPE_E4M3 = 2
+MAX_TOP = 16                 # BDLM_MAX_TOP: alternatives of head_logprobs
 SCALE_BLOCK = 128            # columns that can share a scale of an 8-bit output
 
 OK, E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_OFFSET, E_SLOT, E_LAUNCH, E_WORKSPACE = \
@@ -179,7 +181,11 @@ def lib() -> ctypes.CDLL:
             getattr(L, "bdlm_check_" + name).argtypes = args
             dense += ["bdlm_" + name, "bdlm_check_" + name]
         L.bdlm_add_rmsnorm_backward_workspace.argtypes = [i64, i64, i64p]
-        dense.append("bdlm_add_rmsnorm_backward_workspace")
+        L.bdlm_check_head_logprobs.argtypes = [ddp, vp, i64, i64, vp, vp, fp, fp, vp, fp, vp, i64]
+        L.bdlm_head_logprobs.argtypes = L.bdlm_check_head_logprobs.argtypes + [vp]
+        L.bdlm_head_logprobs_workspace.argtypes = [ddp, i64, i64p]
+        dense += ["bdlm_add_rmsnorm_backward_workspace", "bdlm_head_logprobs", "bdlm_check_head_logprobs",
+                  "bdlm_head_logprobs_workspace"]
         for name in dense:
             getattr(L, name).restype = ctypes.c_int
         for name in ("bdlm_desc_init", "bdlm_check_block_step", "bdlm_check_commit",
@@ -562,9 +568,9 @@ def commit_step(clean, nxt, A, D, D_rev, h_pool, n_committed, n_blocks, expected
     return y_next, y_clean
 
 
-def _workspace_bytes(fn, d) -> int:
+def _workspace_bytes(fn, d, *more) -> int:
     n = ctypes.c_int64(0)
-    rc = fn(ctypes.byref(d), ctypes.byref(n))
+    rc = fn(ctypes.byref(d), *more, ctypes.byref(n))
     if rc != OK:
         raise BdlmError(rc, fn.__name__)
     return int(n.value)
@@ -893,13 +899,14 @@ def _on(stream, x):
     return _torch().cuda.stream(stream)
 
 
-def _dense_call(name: str, d, device, workspace, args):
-    """One call of a dense operator on ``device``'s current stream, with its workspace."""
+def _dense_call(name: str, d, device, workspace, args, query=()):
+    """One call of a dense operator on ``device``'s current stream, with its workspace (``query``: what its size
+    depends on beside the descriptor)."""
     torch = _torch()
     if device.type != "cuda":
         raise ValueError("x must be a GPU tensor (no CPU path exists)")
     fn = getattr(lib(), "bdlm_" + name)
-    need = _workspace_bytes(getattr(lib(), f"bdlm_{name}_workspace"), d)
+    need = _workspace_bytes(getattr(lib(), f"bdlm_{name}_workspace"), d, *query)
     with torch.cuda.device(device):
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
@@ -1318,6 +1325,44 @@ def head_select(x, w, exclude=-1, token=None, logprob=None, stream=None, workspa
     _dense_call("head_select", d, x.device, workspace,
                 (_token(exclude, d), _p(x), _p(w), _p(token), _p(logprob)))
     return token, logprob
+
+
+def head_logprobs(x, w, tokens=None, top=0, exclude=-1, logprob=None, entropy=None, top_token=None, top_logprob=None,
+                  stream=None, workspace=None):
+    """What the head says of its tokens, for hidden states x [..., in_features] and the vocabulary's weights w [tokens,
+    in_features]: (logprob, entropy, top_token, top_logprob), all over the tokens but ``exclude``.
+
+    ``logprob`` float32: the log-probability of ``tokens`` (int64, x's leading shape; -inf for ``exclude``, 0 for a number
+    that is no token), or None without tokens.  ``entropy`` float32 of the distribution; False if not wanted (then None).
+    ``top_token`` (int64) and ``top_logprob`` (float32), [..., top]: the ``top`` (at most 16) most probable tokens in order, of
+    equals the lowest, and their log-probabilities; None for ``top`` 0.  Tokens whose logit is NaN or -inf are not listed: -1
+    and -inf stand past the others.  Outputs are allocated if None."""
+    if stream is not None:
+        with _on(stream, x):
+            return head_logprobs(x, w, tokens, top, exclude, logprob, entropy, top_token, top_logprob, workspace=workspace)
+    torch = _torch()
+    d, lead = _dense(x, w)
+
+    def values(t, shape, dtype, what):
+        return _vector(_place(t, shape, dtype, x.device, what), shape, dtype, x.device, what)
+
+    if not 0 <= top <= MAX_TOP:
+        raise ValueError(f"top must be 0 to {MAX_TOP}, got {top!r}")
+    if tokens is not None:
+        _vector(tokens, lead, torch.int64, x.device, "tokens")
+        logprob = values(logprob, lead, torch.float32, "logprob")
+    elif logprob is not None:
+        raise ValueError("logprob needs tokens")
+    entropy = None if entropy is False else values(entropy, lead, torch.float32, "entropy")
+    if top > 0:
+        top_token = values(top_token, (*lead, top), torch.int64, "top_token")
+        top_logprob = values(top_logprob, (*lead, top), torch.float32, "top_logprob")
+    elif top_token is not None or top_logprob is not None:
+        raise ValueError("top_token and top_logprob need top")
+    _dense_call("head_logprobs", d, x.device, workspace,
+                (_p(tokens), _token(exclude, d), top, _p(x), _p(w), _p(logprob), _p(entropy), _p(top_token), _p(top_logprob)),
+                (top,))
+    return logprob, entropy, top_token, top_logprob
 
 
 def cache_reset(h_pool, slots=None, n_committed=None, n_blocks=None, stream=None):

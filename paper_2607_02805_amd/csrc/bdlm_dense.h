@@ -29,7 +29,8 @@ enum TileOut {
     kTileProb = 3,     // gradient of the loss by the logits, in bf16 terms
     kTileGated = 4,    // act(gate) * up -> out, of products with two weight matrices
     kTileGatedPart = 5,   // their fp32 partial sums
-    kTileTwo = 6       // kTileStore whose rows go to two matrices
+    kTileTwo = 6,      // kTileStore whose rows go to two matrices
+    kTileTop = 7       // per row: as kTileBest, with the slope of the exponentials' sum, and the largest values in order
 };
 
 // Store: the epilogue of a projection (also applied by the join of partial sums).
@@ -63,6 +64,19 @@ struct BestArgs {
     float *label_logit;        // [nrow]: written where label[row] is met (null: no labels)
     const int32_t *label;      // [nrow]
     int32_t ntile, exclude;
+};
+
+// Records of a softmax's alternatives, one per (row, group of columns): largest value, and over the other columns the sums
+// of exp(d) and of exp(d) d, d = value - largest.  With list > 0 also values in which the row's `list` largest are:
+// of a tile its own `list` largest in order with their columns (kNoColumn where there are none), of few rows all of
+// the group (the last one's up to its width; -infinity past the end).
+struct TopArgs {
+    float *top, *others, *slope;   // [nrow][ngroup]
+    float *token_logit;            // [nrow]: written where the row's token is met
+    const int64_t *token;          // [nrow] or null
+    int32_t ngroup, exclude, list;
+    float *value;                  // [nrow][ngroup][list, or the group's width]
+    int32_t *column;               // tiles: likewise
 };
 
 // Of one bf16 term, a row of the logits' gradients is divided by its label's entry: that one, which
@@ -111,6 +125,7 @@ struct TileArgs {
     // kTileTwo: rows below two_rows are store's, those from two_at on go to two_out from its row 0 on (same stride).
     void *two_out;
     int32_t two_rows, two_at;
+    TopArgs top;                       // kTileTop
 };
 int launch_tile(const TileArgs &a, void *stream);
 constexpr int32_t kChip = 256;   // workgroups of large tiles that run at once
@@ -150,6 +165,7 @@ struct SkinnyArgs {
     int32_t out;
     StoreArgs store;
     BestArgs best;
+    TopArgs top;                       // kTileTop
     const void *w2;                    // kTileGated: w_up, w being w_gate (ncol columns each)
     GatedArgs gated;
 };
@@ -225,6 +241,21 @@ struct FinishArgs {
     float *logprob;
 };
 int launch_finish(const FinishArgs &a, void *stream);
+
+// Merges the records of a softmax's alternatives (TopArgs) of each row.
+struct LogprobsArgs {
+    const float *top, *others, *slope;
+    int32_t ngroup, rows, vocab;
+    const int64_t *token;                // or null
+    const float *token_logit;
+    float *logprob, *entropy;            // entropy or null
+    int32_t list, width;                 // values of a group in value: the `list` largest, or all
+    const float *value;
+    const int32_t *column;               // null: column j of group g is g * width + j
+    int64_t *top_token;                  // [rows][list]
+    float *top_logprob;
+};
+int launch_logprobs(const LogprobsArgs &a, void *stream);
 
 // Zeros the rows of dx (bytes per row a multiple of the element) whose label does not count.
 int launch_zero_rows(const int64_t *labels, int64_t exclude, int32_t vocab, int32_t rows, void *dx,

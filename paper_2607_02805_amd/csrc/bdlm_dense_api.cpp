@@ -140,13 +140,6 @@ struct LossBackwardPlan {
     bool fits() const { return sp.fits && sx.fits && sw.fits; }
 };
 
-int check_head(const bdlm_dense_desc_t *d, int64_t exclude, const void *x, const void *w) {
-    TRY(check_inputs(d, x, w));
-    // the softmax has a token to range over
-    if (exclude == 0 && d->out_features == 1) return BDLM_E_SHAPE;
-    return BDLM_OK;
-}
-
 }  // namespace
 
 extern "C" {

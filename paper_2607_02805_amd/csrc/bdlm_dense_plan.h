@@ -287,6 +287,12 @@ template <class... S>
 inline bool apart(const Span &out, const S &...others) {
     return !(out.meets(others) || ...);
 }
+inline int check_head(const bdlm_dense_desc_t *d, int64_t exclude, const void *x, const void *w) {
+    TRY(check_inputs(d, x, w));
+    // the softmax has a token to range over
+    if (exclude == 0 && d->out_features == 1) return BDLM_E_SHAPE;
+    return BDLM_OK;
+}
 inline int32_t token_or_none(const bdlm_dense_desc_t *d, int64_t t) {
     return t >= 0 && t < d->out_features ? static_cast<int32_t>(t) : -1;
 }

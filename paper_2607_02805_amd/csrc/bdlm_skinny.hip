@@ -168,7 +168,45 @@ __global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const Sk
         const int r = x / kQuads, c = x % kQuads * 4;
         f32x4 v = *reinterpret_cast<const f32x4 *>(part + r * kPitch + c);
         for (int w = 1; w < waves; ++w) v += *reinterpret_cast<const f32x4 *>(part + (w * 16 * MT + r) * kPitch + c);
-        if constexpr (OUT == kTileStore) {
+        if constexpr (OUT == kTileTop) {
+            // kQuads consecutive lanes hold a row's columns
+            const TopArgs &b = a.top;
+            const int64_t token = b.token && r < nrow ? b.token[r] : -1;
+            float top = -INFINITY;
+            int at = kNoColumn;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int col = col0 + c + e;
+                if (col >= a.ncol || col == b.exclude) v[e] = -INFINITY;
+                if (v[e] > top) top = v[e], at = col;
+                if (col < a.ncol && col == token) b.token_logit[r] = v[e];
+            }
+            if (b.list > 0 && r < nrow)
+                *reinterpret_cast<f32x4 *>(b.value + (int64_t(r) * b.ngroup + blockIdx.x) * kCols + c) = v;
+#pragma unroll
+            for (int d = 1; d < kQuads; d *= 2) {
+                const float t = __shfl_xor(top, d, 64);
+                const int w = __shfl_xor(at, d, 64);
+                if (t > top || (t == top && w < at)) top = t, at = w;
+            }
+            const float ref = top == -INFINITY ? 0.f : top;
+            float sum = 0.f, slope = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (col0 + c + e == at) continue;
+                const float s = __builtin_amdgcn_exp2f((v[e] - ref) * kLog2e);
+                sum += s;
+                slope += slope_of(s, v[e] - ref);
+            }
+#pragma unroll
+            for (int d = 1; d < kQuads; d *= 2) sum += __shfl_xor(sum, d, 64), slope += __shfl_xor(slope, d, 64);
+            if (c == 0 && r < nrow) {
+                const int64_t o = int64_t(r) * b.ngroup + blockIdx.x;
+                b.top[o] = top;
+                b.others[o] = sum;
+                b.slope[o] = slope;
+            }
+        } else if constexpr (OUT == kTileStore) {
             if (r < nrow) store4(a.store, v, load_bias(a.store, col0 + c, a.ncol), r, col0 + c, a.ncol);
         } else {
             // kQuads consecutive lanes hold a row's columns
@@ -215,6 +253,7 @@ hipError_t launch_cols_of(const SkinnyArgs &a, hipStream_t s) {
     const dim3 g((a.ncol + across - 1) / across), blk(64 * waves);
     const size_t lds = size_t(waves) * 16 * MT * (16 * G + 4) * 4;   // at most 40 KB
     if (a.out == kTileStore) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileStore>), g, blk, lds, s, a);
+    else if (a.out == kTileTop) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileTop>), g, blk, lds, s, a);
     else if (a.out == kTileGated) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, 2, BF16, kTileGated>), g, blk, lds, s, a);
     else hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileBest>), g, blk, lds, s, a);
     return hipGetLastError();

@@ -303,6 +303,76 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
     return m;
 }
 
+// The record of a row's 64 columns from col1 on, which lie in LDS as row_best has them, and with LIST its `list` largest
+// values in order (the lower column first of equals): their values go to the row's first 16 places, their columns (kNoColumn where
+// there are none) to the next 16.  Taking one out costs some 80 instructions: it is found by the maxima of groups of eight columns,
+// which are kept in registers.
+__device__ __forceinline__ Spread row_top(const TileArgs &a, f32x4 *row, int swap, int col1, int list) {
+    constexpr int kOcts = 8;
+    int n = a.ncol - col1 < 64 ? a.ncol - col1 : 64;
+    n = n < 0 ? 0 : n;
+    auto place = [&](int c) { return reinterpret_cast<float *>(row + ((c >> 2) ^ swap)) + (c & 3); };
+    for (int c = n; c < 64; ++c) *place(c) = -INFINITY;
+    const int x = a.top.exclude - col1;
+    if (x >= 0 && x < n) *place(x) = -INFINITY;
+    float most[kOcts];
+#pragma unroll
+    for (int q = 0; q < kOcts; ++q) {
+        const f32x4 u = row[(2 * q) ^ swap], v = row[(2 * q + 1) ^ swap];
+        most[q] = fmaxf(fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+        most[q] = fmaxf(most[q], -INFINITY);   // (nothing but NaN)
+    }
+    // Takes the largest value out of the row, which holds -infinity in its place then.
+    auto take = [&](float &value, int &column) {
+        float m = most[0];
+#pragma unroll
+        for (int q = 1; q < kOcts; ++q) m = fmaxf(m, most[q]);
+        int o = 0;
+#pragma unroll
+        for (int q = kOcts - 1; q >= 0; --q) o = most[q] == m ? q : o;
+        const f32x4 u = row[(2 * o) ^ swap], v = row[(2 * o + 1) ^ swap];
+        const float w[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+        int e = 0;
+#pragma unroll
+        for (int k = 7; k >= 0; --k) e = w[k] == m ? k : e;
+        float rest = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) rest = fmaxf(rest, k == e ? -INFINITY : w[k]);
+        if (m > -INFINITY) *place(8 * o + e) = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kOcts; ++q) most[q] = q == o ? rest : most[q];
+        value = m;
+        column = m > -INFINITY ? col1 + 8 * o + e : kNoColumn;
+    };
+    float value[BDLM_MAX_TOP];
+    int column[BDLM_MAX_TOP];
+    take(value[0], column[0]);
+    Spread r{value[0], 0.f, 0.f};
+    const float ref = r.top == -INFINITY ? 0.f : r.top;
+#pragma unroll 8
+    for (int q = 0; q < 16; ++q) {
+        const f32x4 v = row[q ^ swap];
+        float s[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = __builtin_amdgcn_exp2f((v[e] - ref) * kLog2e);
+        r.others += (s[0] + s[1]) + (s[2] + s[3]);
+        r.slope += (slope_of(s[0], v[0] - ref) + slope_of(s[1], v[1] - ref)) + (slope_of(s[2], v[2] - ref) + slope_of(s[3], v[3] - ref));
+    }
+    if (list == 0) return r;
+#pragma unroll
+    for (int j = 1; j < BDLM_MAX_TOP; ++j) {
+        if (j >= list) break;
+        take(value[j], column[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < BDLM_MAX_TOP; ++j) {
+        if (j >= list) break;
+        *place(j) = value[j];
+        *place(16 + j) = __int_as_float(column[j]);
+    }
+    return r;
+}
+
 // WR x WC waves of (E / WR) x (E / WC) outputs: of 128 x 64 in a tile of 256, of 64 x 64 in one of
 // 128, where KS = 2 such sets of waves take half of a stage's contraction each and add up at the
 // end.  (With one set a SIMD has a wave too few: instructions come at most every four cycles from a
@@ -321,11 +391,13 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     static_assert(64 * WR * WC * KS == kTileThreads, "what the launch has, and the host's check counts on");
     constexpr int WAVES = WR * WC * KS, kWaveGroups = kGroups / KS, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
     constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's stage
-    constexpr int kRec = OUT == kTileBest ? E : 1;
+    constexpr bool kTop = OUT == kTileTop;
+    constexpr int kRec = OUT == kTileBest || kTop ? E : 1;
     __shared__ uint4 sm[BUFS][2 * kBuf];                 // [buffer][col, then row]
-    __shared__ RowData rows[OUT == kTileProb || OUT == kTileBest ? E : 1];
+    __shared__ RowData rows[OUT == kTileProb || OUT == kTileBest || kTop ? E : 1];
     __shared__ float top[WC][kRec], others[WC][kRec];    // softmax records of the waves' columns
-    __shared__ int at[WC][kRec];
+    __shared__ int at[WC][kTop ? 1 : kRec];
+    __shared__ float slope[WC][kTop ? kRec : 1];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nrow = a.nrow_dev ? *a.nrow_dev : a.nrow;
@@ -382,6 +454,14 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     } else if constexpr (OUT == kTileBest) {
         if (a.best.label)
             for (int x = threadIdx.x; x < E; x += 64 * WAVES) rows[x].label = row0 + x < nrow ? a.best.label[row0 + x] : -1;
+    }
+
+    if constexpr (kTop) {
+        if (a.top.token)
+            for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
+                const int64_t token = row0 + x < nrow ? a.top.token[row0 + x] : -1;
+                rows[x].label = token >= 0 && token < a.ncol ? static_cast<int>(token) : -1;
+            }
     }
 
     f32x16 acc[FC][FR];   // [column fragment][row fragment]
@@ -536,8 +616,10 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
                         *to = add ? u + *to : u;
                     }
         };
+        // (with kTileTop the waves meet again, so all of them stay)
+        const bool live = row0 + r1 < rows_out;
         if constexpr (KS == 1) {
-            if (row0 + r1 >= rows_out) return;
+            if (!kTop && !live) return;
             put(false);
             __builtin_amdgcn_wave_barrier();
         } else {
@@ -546,9 +628,57 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             __syncthreads();
             if (half == 0) put(true);
             __syncthreads();
-            if (row0 + r1 >= rows_out) return;
+            if (!kTop && !live) return;
         }
-        if constexpr (OUT == kTileBest) {
+        if constexpr (kTop) {
+            const TopArgs &b = a.top;
+            if (live && half == 0) {
+                if (b.token) {
+                    const int token = rows[r1 + lane].label, x = token - col1;
+                    if (x >= 0 && x < kCols)
+                        b.token_logit[row0 + r1 + lane] = token == b.exclude ? -INFINITY : mine[lane * kQuads + ((x >> 2) ^ (lane & 15))][x & 3];
+                }
+                const Spread m = row_top(a, mine + lane * kQuads, lane & 15, col1, b.list);
+                top[wc][r1 + lane] = m.top;
+                others[wc][r1 + lane] = m.others;
+                slope[wc][r1 + lane] = m.slope;
+            }
+            if (b.list == 0) return;
+            __syncthreads();
+            // a thread a row merges the lists of its WC waves
+            const int x = threadIdx.x & 63, w0 = threadIdx.x >> 6;
+            const int r = w0 * (E / WR) + 32 * j0 + x;   // (of the tile)
+            if (w0 < WR && row0 + r < nrow) {
+                const f32x4 *from = reinterpret_cast<const f32x4 *>(sm) + (w0 * 64 + x) * kQuads;
+                auto entry = [&](int w, int j) {   // value or column j of wave w's list
+                    return reinterpret_cast<const float *>(from + w * (WR * 64 * kQuads) + ((j >> 2) ^ (x & 15)))[j & 3];
+                };
+                float head[WC];
+                int pos[WC];
+#pragma unroll
+                for (int w = 0; w < WC; ++w) head[w] = entry(w, 0), pos[w] = 0;
+                const int64_t o = ((row0 + r) * b.ngroup + tile_c) * b.list;
+                for (int j = 0; j < b.list; ++j) {
+                    int best = 0, p = pos[0];
+                    float v = head[0];
+#pragma unroll
+                    for (int w = 1; w < WC; ++w)
+                        if (head[w] > v) v = head[w], best = w, p = pos[w];   // (equal: the lower columns)
+                    b.value[o + j] = v;
+                    b.column[o + j] = __float_as_int(entry(best, 16 + p));
+                    const float after = p + 1 < b.list ? entry(best, p + 1) : -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < WC; ++w) {
+                        head[w] = w == best ? after : head[w];
+                        pos[w] += w == best && p + 1 < b.list;
+                    }
+                }
+            }
+            __syncthreads();   // before the next part's sums take the place
+            return;
+        }
+        if constexpr (kTop) {
+        } else if constexpr (OUT == kTileBest) {
             if (half != 0) return;
             const Best m = row_best(a, mine + lane * kQuads, lane & 15, kCols, col1);
             top[wc][r1 + lane] = m.top;
@@ -587,6 +717,19 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     part(Int<0>{});
     if constexpr (FR > 2) part(Int<2>{});
     static_assert(FR == 2 || (FR == 4 && KS == 1), "parts of 64 rows, one where the halves meet");
+    if constexpr (kTop) {
+        __syncthreads();
+        for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
+            if (row0 + x >= nrow) continue;
+            Spread m{top[0][x], others[0][x], slope[0][x]};
+#pragma unroll
+            for (int w = 1; w < WC; ++w) m = merge(m, Spread{top[w][x], others[w][x], slope[w][x]});
+            const int64_t o = (row0 + x) * a.top.ngroup + tile_c;
+            a.top.top[o] = m.top;
+            a.top.others[o] = m.others;
+            a.top.slope[o] = m.slope;
+        }
+    }
     if constexpr (OUT == kTileBest) {
         __syncthreads();
         for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
@@ -711,6 +854,7 @@ int launch_tile(const TileArgs &a, void *stream) {
         if (a.out == kTileBest) r = launch_one<false, false, kTileBest>(a, g, s);
         else if (a.out == kTileProb) r = launch_one<false, false, kTileProb>(a, g, s);
         else if (a.out == kTileGated) r = launch_one<false, false, kTileGated>(a, g, s);
+        else if (a.out == kTileTop) r = launch_one<false, false, kTileTop>(a, g, s);
         else if (a.out == kTileGatedPart) r = launch_one<false, false, kTileGatedPart>(a, g, s);
     }
     return r == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;

@@ -1,4 +1,4 @@
-"""Refusals of a sublayer's operators, on the host: the checks run before anything is enqueued, so every
+"""Refusals of a sublayer's operators and of the head's log-probabilities, on the host: the checks run before anything is enqueued, so every
 error path is reached without a GPU (the pointers here are never read)."""
 import ctypes
 
@@ -192,3 +192,59 @@ def test_gated_binding_refuses():
                 lambda: bd.gated_projection_backward(pre[0], x, w, w, pre, dw_gate=torch.zeros(6, 9)[:, :8])):
         with pytest.raises(ValueError):
             bad()
+
+
+TOK, LP, ENT, TT, TL = (A * i for i in range(40, 45))
+
+
+def logprobs(d, tokens=TOK, exclude=-1, top=4, x=X, w=W, lp=LP, ent=ENT, tt=TT, tl=TL, ws=WS, size=BIG):
+    return bd.lib().bdlm_check_head_logprobs(ctypes.byref(d), tokens, exclude, top, x, w, lp, ent, tt, tl, ws, size)
+
+
+def test_logprobs_arguments():
+    d = desc()
+    assert logprobs(d) == bd.OK and logprobs(desc(rows=0), tokens=None, lp=None, tt=None, tl=None, x=None) == bd.OK
+    for bad in (dict(rows=-1), dict(k=0), dict(n=0), dict(rows=(1 << 22) + 1), dict(n=(1 << 22) + 1), dict(x_stride=-1)):
+        assert logprobs(desc(**bad), top=0) == bd.E_SHAPE, bad
+    assert logprobs(desc(dtype=2)) == bd.E_DTYPE
+    assert logprobs(d, x=None) == bd.E_NULL and logprobs(d, w=W + 2) == bd.E_ALIGN
+    assert logprobs(d, tokens=None) == bd.E_NULL and logprobs(d, lp=None) == bd.E_NULL
+    assert logprobs(d, tokens=None, lp=None) == bd.OK and logprobs(d, ent=None) == bd.OK
+    assert logprobs(d, tt=None) == bd.E_NULL and logprobs(d, tl=None) == bd.E_NULL
+    assert logprobs(d, top=0, tt=None, tl=None) == bd.OK
+    assert logprobs(d, top=-1) == bd.E_SHAPE and logprobs(d, top=17) == bd.E_SHAPE and logprobs(d, top=16) == bd.OK
+    few = desc(n=5)
+    assert logprobs(few, top=5) == bd.OK and logprobs(few, top=6) == bd.E_SHAPE and logprobs(few, top=5, exclude=1) == bd.E_SHAPE
+    assert logprobs(few, top=5, exclude=5) == bd.OK and logprobs(desc(n=1), exclude=0, top=0) == bd.E_SHAPE
+    for p, at in (("tokens", TOK + 4), ("lp", LP + 2), ("ent", ENT + 1), ("tt", TT + 4), ("tl", TL + 2)):
+        assert logprobs(d, **{p: at}) == bd.E_ALIGN, p
+    ins, outs = dict(x=X, w=W, tokens=TOK), dict(lp=LP, ent=ENT, tt=TT, tl=TL)
+    for o in outs:
+        for p in ins.values():
+            assert logprobs(d, **{o: p}) == bd.E_SHAPE, o
+        for other, p in outs.items():
+            if other != o:
+                assert logprobs(d, **{o: p}) == bd.E_SHAPE, (o, other)
+    for p in (*ins.values(), *outs.values()):
+        assert logprobs(d, ws=p) == bd.E_WORKSPACE
+    need = ctypes.c_int64(-1)
+    f = bd.lib().bdlm_head_logprobs_workspace
+    assert f(None, 1, ctypes.byref(need)) == bd.E_NULL and f(ctypes.byref(d), 1, None) == bd.E_NULL
+    assert f(ctypes.byref(d), 17, ctypes.byref(need)) == bd.E_SHAPE and f(ctypes.byref(few), 6, ctypes.byref(need)) == bd.E_SHAPE
+    for rows in (3, 100):
+        for top in (0, 4):
+            d = desc(rows=rows)
+            assert f(ctypes.byref(d), top, ctypes.byref(need)) == bd.OK
+            assert logprobs(d, top=top, size=need.value) == bd.OK
+            assert logprobs(d, top=top, size=need.value - 1) == bd.E_WORKSPACE and logprobs(d, top=top, ws=None) == bd.E_WORKSPACE
+            assert logprobs(d, top=top, ws=WS + 64) == bd.E_ALIGN
+
+
+def test_logprobs_binding_refuses():
+    x, w, t = torch.zeros(4, 8), torch.ones(6, 8), torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError, match="GPU"):
+        bd.head_logprobs(x, w, t, top=2)
+    for bad in (dict(top=17), dict(top=-1), dict(tokens=t[:3]), dict(tokens=t.int()), dict(logprob=torch.zeros(4)),
+                dict(top_token=t), dict(top=2, top_token=t), dict(tokens=t, logprob=torch.zeros(5))):
+        with pytest.raises(ValueError):
+            bd.head_logprobs(x, w, **bad)
