@@ -962,6 +962,9 @@ def add_rmsnorm(x, w, residual=None, eps=1e-5, out_dtype=None, out=None, sum=Non
     if stream is not None:
         with _on(stream, x):
             return add_rmsnorm(x, w, residual, eps, out_dtype, out, sum, scale, scale_block)
+    got = _native().add_rmsnorm(x, w, residual, eps, out_dtype, out, sum, scale, scale_block, stream)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_add_rmsnorm")
     if x.dim() < 1 or x.shape[-1] == 0:
         raise ValueError("x [..., width] expected")
     if x.device.type != "cuda":
@@ -1010,6 +1013,9 @@ def add_rmsnorm_backward(dy, s, w, dsum=None, eps=1e-5, ds=True, dw=True, stream
     if stream is not None:
         with _on(stream, s):
             return add_rmsnorm_backward(dy, s, w, dsum, eps, ds, dw, workspace=workspace)
+    got = _native().add_rmsnorm_backward(dy, s, w, dsum, eps, ds, dw, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_add_rmsnorm_backward")
     if s.dim() < 1 or s.shape[-1] == 0:
         raise ValueError("s [..., width] expected")
     if s.device.type != "cuda":
@@ -1181,6 +1187,9 @@ def gated_projection(x, w_gate, w_up, bias_gate=None, bias_up=None, act="silu", 
     if stream is not None:
         with _on(stream, x):
             return gated_projection(x, w_gate, w_up, bias_gate, bias_up, act, out, pre, workspace=workspace)
+    got = _native().gated_projection(x, w_gate, w_up, bias_gate, bias_up, act, out, pre, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_gated_projection")
     torch = _torch()
     code = _act_code(act)
     d, lead = _two_weights(x, w_gate, w_up)
@@ -1213,6 +1222,9 @@ def gated_projection_backward(dh, x, w_gate, w_up, pre, act="silu", dx=True, dw_
     if stream is not None:
         with _on(stream, x):
             return gated_projection_backward(dh, x, w_gate, w_up, pre, act, dx, dw_gate, dw_up, dbg, dbu, workspace=workspace)
+    got = _native().gated_projection_backward(dh, x, w_gate, w_up, pre, act, dx, dw_gate, dw_up, dbg, dbu, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_gated_projection_backward")
     torch = _torch()
     code = _act_code(act)
     d, lead = _two_weights(x, w_gate, w_up)
@@ -1340,6 +1352,9 @@ def head_logprobs(x, w, tokens=None, top=0, exclude=-1, logprob=None, entropy=No
     if stream is not None:
         with _on(stream, x):
             return head_logprobs(x, w, tokens, top, exclude, logprob, entropy, top_token, top_logprob, workspace=workspace)
+    got = _native().head_logprobs(x, w, tokens, top, exclude, logprob, entropy, top_token, top_logprob, stream, workspace)
+    if got is not NotImplemented:
+        return _answer(got, "bdlm_head_logprobs")
     torch = _torch()
     d, lead = _dense(x, w)
 

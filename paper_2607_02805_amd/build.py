@@ -44,7 +44,7 @@ def _run(cmd: list[str]) -> None:
 HIP_SRCS = ("bdlm_scan.hip", "bdlm_seq.hip", "bdlm_seq16.hip", "bdlm_mask.hip", "bdlm_maskw.hip",
             "bdlm_conv.hip",
             "bdlm_mix.hip", "bdlm_norm.hip", "bdlm_scratch.hip", "bdlm_tile.hip", "bdlm_skinny.hip",
-            "bdlm_dense.hip", "bdlm_addnorm.hip")
+            "bdlm_dense.hip", "bdlm_addnorm.hip", "bdlm_logprobs.hip")
 CPP_SRCS = ("bdlm_api.cpp", "bdlm_dense_api.cpp", "bdlm_sublayer_api.cpp", "bdlm_logprobs_api.cpp")
 
 

@@ -24,6 +24,7 @@
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -666,6 +667,255 @@ BDLM_ENTRY(head_select, 7) {
     return enqueue(pair(token, logprob), [&] { return bdlm_head_select(&d, exclude, x, w, tp, lp, ws.p, ws.bytes, s); });
 } BDLM_END
 
+// Two tensors [..., cols] of x's type at one row stride: new ones for True, else a tuple.
+struct Two {
+    at::Tensor a, b;
+    int64_t ld = 0;
+    Two() = default;
+    Two(PyObject *o, const Dense &t, int64_t cols) {
+        const auto full = t.shape(cols);
+        if (o == Py_True) {
+            a = t.output(Py_True, full, t.type);
+            b = t.output(Py_True, full, t.type);
+        } else {
+            need(PyTuple_CheckExact(o) && PyTuple_GET_SIZE(o) == 2);
+            a = t.output(PyTuple_GET_ITEM(o, 0), full, t.type);
+            b = t.output(PyTuple_GET_ITEM(o, 1), full, t.type);
+            need(PyTuple_GET_ITEM(o, 0) != Py_None && PyTuple_GET_ITEM(o, 1) != Py_None);
+            need(PyTuple_GET_ITEM(o, 0) != Py_True && PyTuple_GET_ITEM(o, 1) != Py_True);
+        }
+        ld = row_stride(a, t.d.rows);
+        need(row_stride(b, t.d.rows) == ld);
+    }
+};
+// The second weight matrix, laid out as the first.
+const at::Tensor &second(PyObject *o, const Dense &t) {
+    const at::Tensor &w = tensor(o);
+    need(t.here(w) && w.scalar_type() == t.type && w.sizes() == t.w.sizes() && row_stride(w, t.d.out_features) == t.d.w_stride);
+    return w;
+}
+const float *bias_of(PyObject *o, const Dense &t) {
+    if (o == Py_None) return nullptr;
+    const float *p = vec(o, t.d.out_features);
+    need(t.here(tensor(o)));
+    return p;
+}
+void *any_ptr(const at::Tensor &t) { return t.defined() ? ptr(t) : nullptr; }
+
+// x w_gate w_up bias_gate bias_up act out pre stream workspace
+BDLM_ENTRY(gated_projection, 10) {
+    const Dense t(a[0], a[1]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[8] == Py_None);
+    const at::Tensor &w2 = second(a[2], t);
+    const float *bg = bias_of(a[3], t), *bu = bias_of(a[4], t);
+    const int32_t act = act_of(a[5]);
+    need(a[6] != Py_True);
+    const at::Tensor out = a[6] == Py_None ? t.output(Py_None, t.shape(d.out_features), t.type) : t.input(a[6], d.out_features);
+    const Two pre = a[7] == Py_None ? Two() : Two(a[7], t, d.out_features);
+    const int64_t ldo = row_stride(out, d.rows);
+    const Workspace ws = dense_space(a[9], bytes_of(bdlm_gated_projection_workspace, d), t);
+    void *s = stream_of(a[8]);
+    const int32_t odt = Dense::code(out.scalar_type());
+    const void *x = ptr(t.x), *wg = ptr(t.w), *wu = ptr(w2);
+    void *op = ptr(out), *gp = any_ptr(pre.a), *up = any_ptr(pre.b);
+    PyObject *r = item(out);
+    if (pre.a.defined()) {
+        PyObject *both = PyTuple_New(2);
+        if (!r || !both) general();
+        PyTuple_SET_ITEM(both, 0, r);
+        PyTuple_SET_ITEM(both, 1, pair(pre.a, pre.b));
+        r = both;
+    }
+    return enqueue(r, [&] {
+        return bdlm_gated_projection(&d, act, odt, x, wg, wu, bg, bu, op, ldo, gp, up, pre.ld, ws.p, ws.bytes, s);
+    });
+} BDLM_END
+
+// dh x w_gate w_up pre act dx dw_gate dw_up dbg dbu stream workspace
+BDLM_ENTRY(gated_projection_backward, 13) {
+    const Dense t(a[1], a[2]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[11] == Py_None && a[4] != Py_True);
+    const at::Tensor &w2 = second(a[3], t);
+    const at::Tensor &dh = t.input(a[0], d.out_features);
+    const Two pre(a[4], t, d.out_features);
+    const int32_t act = act_of(a[5]);
+    const at::Tensor dx = t.wanted(a[6], t.x.sizes(), t.type), dg = t.wanted(a[7], t.w.sizes(), t.type),
+                     du = t.wanted(a[8], t.w.sizes(), t.type), bg = t.wanted(a[9], {d.out_features}, at::kFloat),
+                     bu = t.wanted(a[10], {d.out_features}, at::kFloat);
+    need((!bg.defined() || bg.is_contiguous()) && (!bu.defined() || bu.is_contiguous()));
+    const int64_t ldh = row_stride(dh, d.rows), ldx = dx.defined() ? row_stride(dx, d.rows) : 0;
+    const int64_t ldg = dg.defined() ? row_stride(dg, d.out_features) : 0, ldu = du.defined() ? row_stride(du, d.out_features) : 0;
+    need(!dg.defined() || !du.defined() || ldg == ldu);
+    const Workspace ws = dense_space(a[12], bytes_of(bdlm_gated_projection_backward_workspace, d), t);
+    void *s = stream_of(a[11]);
+    const int32_t hdt = Dense::code(dh.scalar_type());
+    const void *hp = ptr(dh), *x = ptr(t.x), *wg = ptr(t.w), *wu = ptr(w2), *pg = ptr(pre.a), *pu = ptr(pre.b);
+    void *xp = any_ptr(dx), *gp = any_ptr(dg), *up = any_ptr(du);
+    float *bgp = opt_ptr(bg), *bup = opt_ptr(bu);
+    PyObject *r = PyTuple_New(5);
+    if (!r) general();
+    PyTuple_SET_ITEM(r, 0, item(dx));
+    PyTuple_SET_ITEM(r, 1, item(dg));
+    PyTuple_SET_ITEM(r, 2, item(du));
+    PyTuple_SET_ITEM(r, 3, item(bg));
+    PyTuple_SET_ITEM(r, 4, item(bu));
+    return enqueue(r, [&] {
+        return bdlm_gated_projection_backward(&d, act, hdt, hp, ldh, x, wg, wu, pg, pu, pre.ld, xp, ldx, gp, up,
+                                              dg.defined() ? ldg : ldu, bgp, bup, ws.p, ws.bytes, s);
+    });
+} BDLM_END
+
+// x w tokens top exclude logprob entropy top_token top_logprob stream workspace
+BDLM_ENTRY(head_logprobs, 11) {
+    const Dense t(a[0], a[1]);
+    const bdlm_dense_desc_t &d = t.d;
+    need(a[9] == Py_None);
+    const int64_t top = integer(a[3]), exclude = integer(a[4]);
+    need(top >= 0 && top <= BDLM_MAX_TOP && (a[2] != Py_None || a[5] == Py_None) &&
+         (top > 0 || (a[7] == Py_None && a[8] == Py_None)));
+    const at::Tensor tokens = a[2] == Py_None ? at::Tensor() : t.values(a[2], at::kLong, false),
+                     logprob = a[2] == Py_None ? at::Tensor() : t.values(a[5], at::kFloat, true),
+                     entropy = a[6] == Py_False ? at::Tensor() : t.values(a[6], at::kFloat, true);
+    at::Tensor tt, tl;
+    if (top > 0) {
+        const auto full = t.shape(top);
+        tt = t.output(a[7], full, at::kLong);
+        tl = t.output(a[8], full, at::kFloat);
+        need(tt.is_contiguous() && tl.is_contiguous());
+    }
+    int64_t bytes = 0;
+    need(bdlm_head_logprobs_workspace(&d, top, &bytes) == BDLM_OK);
+    const Workspace ws = dense_space(a[10], bytes, t);
+    void *s = stream_of(a[9]);
+    const int64_t *kp = tokens.defined() ? ptr<int64_t>(tokens) : nullptr;
+    const void *x = ptr(t.x), *w = ptr(t.w);
+    float *lp = opt_ptr(logprob), *ep = opt_ptr(entropy), *vp = opt_ptr(tl);
+    int64_t *ip = tt.defined() ? ptr<int64_t>(tt) : nullptr;
+    PyObject *r = PyTuple_New(4);
+    if (!r) general();
+    PyTuple_SET_ITEM(r, 0, item(logprob));
+    PyTuple_SET_ITEM(r, 1, item(entropy));
+    PyTuple_SET_ITEM(r, 2, item(tt));
+    PyTuple_SET_ITEM(r, 3, item(tl));
+    return enqueue(r, [&] { return bdlm_head_logprobs(&d, kp, exclude, top, x, w, lp, ep, ip, vp, ws.p, ws.bytes, s); });
+} BDLM_END
+
+// The rows of a norm and their leading shape.
+struct Norm {
+    const at::Tensor &x;
+    int64_t width, rows;
+    explicit Norm(PyObject *o) : x(tensor(o)) {
+        need(x.dim() >= 1 && (x.scalar_type() == at::kBFloat16 || x.scalar_type() == at::kFloat));
+        width = x.size(x.dim() - 1);
+        need(width > 0 && x.get_device() == c10::hip::current_device());
+        rows = x.numel() / width;
+        need(rows > 0);
+    }
+    bool here(const at::Tensor &t) const { return t.get_device() == x.get_device(); }
+    const at::Tensor &like(PyObject *o) const {
+        const at::Tensor &t = tensor(o);
+        need(here(t) && t.sizes() == x.sizes() && (t.scalar_type() == at::kBFloat16 || t.scalar_type() == at::kFloat));
+        return t;
+    }
+    at::Tensor output(PyObject *o, at::IntArrayRef shape, at::ScalarType ty) const {
+        if (o == Py_None || o == Py_True) {
+            const Unlocked u;
+            return at::empty(shape, x.options().dtype(ty));
+        }
+        const at::Tensor &t = tensor(o);
+        need(here(t) && t.scalar_type() == ty && t.sizes() == shape);
+        return t;
+    }
+    const float *weights(PyObject *o) const {
+        const float *p = vec(o, width);
+        need(here(tensor(o)));
+        return p;
+    }
+    int64_t stride(const at::Tensor &t) const { return t.defined() ? row_stride(t, rows) : 0; }
+};
+int32_t code_of(at::ScalarType t) {
+    return t == at::kFloat8_e4m3fn ? BDLM_DTYPE_E4M3 : t == at::kBFloat16 ? BDLM_DTYPE_BF16 : BDLM_DTYPE_F32;
+}
+
+// x w residual eps out_dtype out sum scale scale_block stream
+BDLM_ENTRY(add_rmsnorm, 10) {
+    const Norm t(a[0]);
+    need(a[9] == Py_None && PyFloat_CheckExact(a[3]));
+    const float *w = t.weights(a[1]);
+    const float eps = static_cast<float>(PyFloat_AS_DOUBLE(a[3]));
+    const at::Tensor res = a[2] == Py_None ? at::Tensor() : t.like(a[2]);
+    at::Tensor sum, scale;
+    need(res.defined() || a[6] == Py_None || a[6] == Py_False);
+    if (res.defined() && a[6] != Py_False) sum = t.output(a[6], t.x.sizes(), res.scalar_type());
+    at::ScalarType ty = t.x.scalar_type();
+    if (a[4] != Py_None) {
+        need(THPDtype_Check(a[4]));
+        ty = reinterpret_cast<THPDtype *>(a[4])->scalar_type;
+    } else if (a[5] != Py_None && a[5] != Py_True) {
+        ty = tensor(a[5]).scalar_type();
+    }
+    const bool e4m3 = ty == at::kFloat8_e4m3fn;
+    need(e4m3 || ty == at::kBFloat16 || ty == at::kFloat);
+    need(a[5] != Py_True);
+    const at::Tensor out = t.output(a[5], t.x.sizes(), ty);
+    const int64_t block = integer(a[8]);
+    need(block == 0 || (e4m3 && block == 128));
+    if (e4m3) {
+        c10::SmallVector<int64_t, 5> shape(t.x.sizes().begin(), t.x.sizes().end());
+        shape.back() = block ? (t.width + block - 1) / block : 1;
+        scale = t.output(a[7], shape, at::kFloat);
+        need(scale.is_contiguous());
+    } else {
+        need(a[7] == Py_None);
+    }
+    const int64_t ldx = t.stride(t.x), ldr = t.stride(res), lds = t.stride(sum), ldo = t.stride(out);
+    void *s = stream_of(a[9]);
+    const int32_t xdt = code_of(t.x.scalar_type()), rdt = res.defined() ? code_of(res.scalar_type()) : 0, odt = code_of(ty);
+    const void *x = ptr(t.x), *rp = any_ptr(res);
+    void *sp = any_ptr(sum), *op = ptr(out);
+    float *cp = opt_ptr(scale);
+    PyObject *r = PyTuple_New(3);
+    if (!r) general();
+    PyTuple_SET_ITEM(r, 0, item(out));
+    PyTuple_SET_ITEM(r, 1, item(sum));
+    PyTuple_SET_ITEM(r, 2, item(scale));
+    return enqueue(r, [&] {
+        return bdlm_add_rmsnorm(t.rows, t.width, xdt, x, ldx, rdt, rp, ldr, sp, lds, w, eps, odt, op, ldo, cp, block, s);
+    });
+} BDLM_END
+
+// dy s w dsum eps ds dw stream workspace
+BDLM_ENTRY(add_rmsnorm_backward, 9) {
+    const Norm t(a[1]);
+    need(a[7] == Py_None && PyFloat_CheckExact(a[4]));
+    const at::Tensor &dy = t.like(a[0]);
+    const float *w = t.weights(a[2]);
+    const float eps = static_cast<float>(PyFloat_AS_DOUBLE(a[4]));
+    const at::Tensor dsum = a[3] == Py_None ? at::Tensor() : t.like(a[3]);
+    at::ScalarType ty = dsum.defined() ? dsum.scalar_type() : t.x.scalar_type();
+    if (!dsum.defined() && a[5] != Py_None && a[5] != Py_True) ty = tensor(a[5]).scalar_type();
+    need(ty == at::kBFloat16 || ty == at::kFloat);
+    const at::Tensor ds = a[5] == Py_None ? at::Tensor() : t.output(a[5], t.x.sizes(), ty);
+    const at::Tensor dw = a[6] == Py_None ? at::Tensor() : t.output(a[6], {t.width}, at::kFloat);
+    need(!dw.defined() || dw.is_contiguous());
+    int64_t bytes = 0;
+    if (dw.defined()) need(bdlm_add_rmsnorm_backward_workspace(t.rows, t.width, &bytes) == BDLM_OK);
+    const Workspace ws(a[8], bytes, t.x);
+    need(!ws.t.defined() || t.here(ws.t));
+    const int64_t ldy = t.stride(dy), lds = t.stride(t.x), ldt = t.stride(dsum), ldd = t.stride(ds);
+    void *s = stream_of(a[7]);
+    const int32_t ydt = code_of(dy.scalar_type()), sdt = code_of(t.x.scalar_type()), ddt = code_of(ty);
+    const void *yp = ptr(dy), *sp = ptr(t.x), *bp = any_ptr(dsum);
+    void *op = any_ptr(ds);
+    float *gp = opt_ptr(dw);
+    return enqueue(pair(ds, dw), [&] {
+        return bdlm_add_rmsnorm_backward(t.rows, t.width, ydt, yp, ldy, sdt, sp, lds, w, eps, ddt, bp, ldt, op, ldd, gp, ws.p,
+                                         ws.bytes, s);
+    });
+} BDLM_END
+
 #define BDLM_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     BDLM_METHOD(scan_block_step), BDLM_METHOD(scan_block_step_sep), BDLM_METHOD(commit_boundary),
@@ -673,7 +923,9 @@ PyMethodDef methods[] = {
     BDLM_METHOD(scan_full_window), BDLM_METHOD(prefill),
     BDLM_METHOD(prefill_noalloc), BDLM_METHOD(gated_rmsnorm), BDLM_METHOD(projection),
     BDLM_METHOD(projection_backward), BDLM_METHOD(head_loss), BDLM_METHOD(head_loss_backward),
-    BDLM_METHOD(head_select), {nullptr, nullptr, 0, nullptr}};
+    BDLM_METHOD(head_select), BDLM_METHOD(gated_projection), BDLM_METHOD(gated_projection_backward),
+    BDLM_METHOD(head_logprobs), BDLM_METHOD(add_rmsnorm), BDLM_METHOD(add_rmsnorm_backward),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -15,11 +15,6 @@
 namespace bdlm {
 namespace {
 
-template <int V>
-struct Number {
-    static constexpr int value = V;
-};
-
 template <int TERMS>
 __device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, const float (&v)[8]) {
     if constexpr (TERMS == 1) {
@@ -276,128 +271,6 @@ __global__ void __launch_bounds__(256) bdlm_finish_kernel(const FinishArgs a) {
     }
 }
 
-// The largest of a wave's values and the lowest of numbers, in every lane.
-__device__ __forceinline__ float wave_max(float v) {
-    auto step = [&](auto ctrl, auto mask) {
-        const int o = __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value,
-                                                  decltype(mask)::value, 0xf, false);
-        v = fmaxf(v, __int_as_float(o));
-    };
-    step(Number<0x111>{}, Number<0xf>{});   // row_shr:1, 2, 4, 8
-    step(Number<0x112>{}, Number<0xf>{});
-    step(Number<0x114>{}, Number<0xf>{});
-    step(Number<0x118>{}, Number<0xf>{});
-    step(Number<0x142>{}, Number<0xa>{});   // row_bcast:15 into rows 1 and 3
-    step(Number<0x143>{}, Number<0xc>{});   // row_bcast:31 into rows 2 and 3
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
-}
-
-// A wave's list of the k largest values seen, in order, entry j in lane j: of equal ones the lowest number first.  An empty
-// entry is (-infinity, kNoColumn), and so is a value that is not to be listed.
-struct TopList {
-    float v;
-    int at;
-    __device__ __forceinline__ TopList() : v(-INFINITY), at(kNoColumn) {}
-    // One value a lane.  Every turn lists the best of those that beat the last entry.
-    __device__ __forceinline__ void add(float u, int n, int k, int lane) {
-        if (!(u > -INFINITY)) n = kNoColumn;   // (NaN as well)
-        for (;;) {
-            const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), k - 1));
-            const int last_at = __builtin_amdgcn_readlane(at, k - 1);
-            const bool can = n != kNoColumn && (u > last || (u == last && n < last_at));
-            if (!__ballot(can)) return;
-            const float m = wave_max(can ? u : -INFINITY);
-            uint64_t eq = __ballot(can && u == m);
-            int src = __ffsll(static_cast<unsigned long long>(eq)) - 1;
-            int number = __builtin_amdgcn_readlane(n, src);
-            for (eq &= eq - 1; eq; eq &= eq - 1) {   // equal values: the lowest number
-                const int other = __ffsll(static_cast<unsigned long long>(eq)) - 1, t = __builtin_amdgcn_readlane(n, other);
-                if (t < number) number = t, src = other;
-            }
-            if (lane == src) n = kNoColumn;
-            const int before = __popcll(__ballot(lane < k && (v > m || (v == m && at < number))));
-            const float up_v = __shfl_up(v, 1, 64);
-            const int up_at = __shfl_up(at, 1, 64);
-            if (lane > before) v = up_v, at = up_at;
-            if (lane == before) v = m, at = number;
-        }
-    }
-};
-
-// One workgroup per row: its records merged, and the row's largest values.  The k largest lie in the k groups whose
-// largest values (then the lower columns) come first: were one in another group, each of those k would hold a larger one.  So
-// the groups are chosen first, each wave its own k and the first wave among all of these, and then the values of k groups.
-__global__ void __launch_bounds__(256) bdlm_logprobs_kernel(const LogprobsArgs a) {
-    __shared__ Spread waves[4];
-    __shared__ float best[64];
-    __shared__ int best_at[64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t i = blockIdx.x;
-    const int k = a.list;
-    Spread m{-INFINITY, 0.f, 0.f};
-    TopList list;
-    for (int t = threadIdx.x; t - lane < a.ngroup; t += 1024) {
-        Spread o[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t at = i * a.ngroup + t + 256 * j;
-            const bool here = t + 256 * j < a.ngroup;
-            o[j] = here ? Spread{a.top[at], a.others[at], a.slope[at]} : Spread{-INFINITY, 0.f, 0.f};
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            m = merge(m, o[j]);
-            if (k > 0) list.add(o[j].top, t + 256 * j, k, lane);
-        }
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        m = merge(m, Spread{__shfl_xor(m.top, d, 64), __shfl_xor(m.others, d, 64), __shfl_xor(m.slope, d, 64)});
-    if (lane == 0) waves[wave] = m;
-    if (lane < 16) best[wave * 16 + lane] = lane < k ? list.v : -INFINITY, best_at[wave * 16 + lane] = list.at;
-    __syncthreads();
-    if (wave != 0) return;
-    m = waves[0];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) m = merge(m, waves[w]);
-    const float rest = fabsf(m.top) < INFINITY ? log1pf(m.others) : NAN;
-    if (lane == 0) {
-        if (a.entropy) a.entropy[i] = rest - m.slope / (1.f + m.others);
-        if (a.token) {
-            const int64_t token = a.token[i];
-            a.logprob[i] = token >= 0 && token < a.vocab ? (a.token_logit[i] - m.top) - rest : 0.f;
-        }
-    }
-    if (k == 0) return;
-    list = TopList();
-    list.add(best[lane], best_at[lane], k, lane);
-    // the values of those groups: at most 16 groups of 32
-    const int all = k * a.width;
-    float v[8];
-    int c[8];
-#pragma unroll
-    for (int b = 0; b < 8; ++b) {
-        const int x = b * 64 + lane, which = x < all ? x / a.width : 0, j = x - which * a.width;
-        const int group = __shfl(list.at, which, 64);
-        v[b] = -INFINITY;
-        c[b] = kNoColumn;
-        if (x < all && group != kNoColumn) {
-            const int64_t at = (i * a.ngroup + group) * a.width + j;
-            v[b] = a.value[at];
-            c[b] = a.column ? a.column[at] : group * a.width + j;
-        }
-    }
-    list = TopList();
-#pragma unroll
-    for (int b = 0; b < 8; ++b)
-        if (b * 64 < all) list.add(v[b], c[b], k, lane);
-    if (lane < k) {
-        const bool here = list.at != kNoColumn;
-        a.top_token[i * k + lane] = here ? list.at : -1;
-        a.top_logprob[i * k + lane] = here ? (list.v - m.top) - rest : -INFINITY;
-    }
-}
-
 __global__ void __launch_bounds__(256) bdlm_zero_rows_kernel(const int64_t *labels, int64_t exclude, int vocab,
                                                              int rows, char *dx, int64_t ld, int cols, int esz) {
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
@@ -473,13 +346,6 @@ int launch_rows(const RowsArgs &a, void *stream) {
 int launch_finish(const FinishArgs &a, void *stream) {
     if (a.rows <= 0) return BDLM_OK;
     hipLaunchKernelGGL(bdlm_finish_kernel, dim3(a.rows), dim3(256), 0, static_cast<hipStream_t>(stream), a);
-    return done();
-}
-
-int launch_logprobs(const LogprobsArgs &a, void *stream) {
-    if (a.rows <= 0) return BDLM_OK;
-    static_assert(BDLM_MAX_TOP == 16 && BDLM_MAX_TOP * 32 == 8 * 64, "a list of 16 lanes; groups of at most 32 values");
-    hipLaunchKernelGGL(bdlm_logprobs_kernel, dim3(a.rows), dim3(256), 0, static_cast<hipStream_t>(stream), a);
     return done();
 }
 

@@ -1,0 +1,234 @@
+// bdlm_logprobs.hip -- gfx950 kernel that makes a row's log-probability, entropy and most probable tokens of the records and
+// values that the products of the head leave (TopArgs in bdlm_dense.h).
+//
+// One workgroup per row.  With M the largest value, o and l a group's sums of exp(d) and exp(d) d over all but one of its
+// columns, and f = exp(top - M), D = top - M:
+//     Z = 1 + others,  others = sum (1 + o) f less the largest one's own 1,  slope = sum f (l + D (1 + o)),
+//     lse = M + log Z,  entropy = log Z - slope / Z   (both terms positive).
+// The k largest values: of sixteen parts of the groups, the k-th largest part's maximum is a bound that at least k values
+// reach.  Values that reach it, mostly a few more than k, are gathered and each counts the ones before it, in the order of
+// values and then columns: a count below k is its place.  (Listing them one after the other took 18 us for one row of
+// 1,024 groups.)  Where too many reach the bound, as where all are equal, the first wave lists them one after the other.
+//
+// Bound by latency: the records, the values, three meetings of the waves.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "bdlm.h"
+#include "bdlm_dense.h"
+#include "bdlm_dense_device.h"
+
+namespace bdlm {
+namespace {
+
+template <int V>
+struct Number {
+    static constexpr int value = V;
+};
+
+// Largest value of 16 lanes (in their last) or of 64 (WAVE; in every lane).
+template <bool WAVE>
+__device__ __forceinline__ float largest(float v) {
+    auto step = [&](auto ctrl, auto mask) {
+        const int o = __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value,
+                                                  decltype(mask)::value, 0xf, false);
+        v = fmaxf(v, __int_as_float(o));
+    };
+    step(Number<0x111>{}, Number<0xf>{});   // row_shr:1, 2, 4, 8
+    step(Number<0x112>{}, Number<0xf>{});
+    step(Number<0x114>{}, Number<0xf>{});
+    step(Number<0x118>{}, Number<0xf>{});
+    if constexpr (WAVE) {
+        step(Number<0x142>{}, Number<0xa>{});   // row_bcast:15 into rows 1 and 3
+        step(Number<0x143>{}, Number<0xc>{});   // row_bcast:31 into rows 2 and 3
+        v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+    }
+    return v;
+}
+__device__ __forceinline__ float wave_total(float v) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(wave_inclusive_sum(v)), 63));
+}
+__device__ __forceinline__ bool before(float v, int at, float u, int n) { return v > u || (v == u && at < n); }
+
+// A wave's list of the k largest values seen, in order, entry j in lane j: of equal ones the lowest number first.  An empty
+// entry is (-infinity, kNoColumn).
+struct TopList {
+    float v;
+    int at;
+    __device__ __forceinline__ TopList() : v(-INFINITY), at(kNoColumn) {}
+    // One value a lane.  Every turn lists the first of those that come before the last entry.
+    __device__ __forceinline__ void add(float u, int n, int k, int lane) {
+        if (!(u > -INFINITY)) n = kNoColumn;   // (NaN as well)
+        for (;;) {
+            const float last = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), k - 1));
+            const int last_at = __builtin_amdgcn_readlane(at, k - 1);
+            const bool can = n != kNoColumn && before(u, n, last, last_at);
+            if (!__ballot(can)) return;
+            const float m = largest<true>(can ? u : -INFINITY);
+            uint64_t eq = __ballot(can && u == m);
+            int src = __ffsll(static_cast<unsigned long long>(eq)) - 1;
+            int number = __builtin_amdgcn_readlane(n, src);
+            for (eq &= eq - 1; eq; eq &= eq - 1) {   // equal values: the lowest number
+                const int other = __ffsll(static_cast<unsigned long long>(eq)) - 1, t = __builtin_amdgcn_readlane(n, other);
+                if (t < number) number = t, src = other;
+            }
+            if (lane == src) n = kNoColumn;
+            const int place = __popcll(__ballot(lane < k && before(v, at, m, number)));
+            const float up_v = __shfl_up(v, 1, 64);
+            const int up_at = __shfl_up(at, 1, 64);
+            if (lane > place) v = up_v, at = up_at;
+            if (lane == place) v = m, at = number;
+        }
+    }
+};
+
+constexpr int kParts = 16;         // of the groups: no fewer than BDLM_MAX_TOP
+constexpr int kRoom = 256;         // gathered groups, and values
+
+template <int T>   // threads
+__global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) {
+    constexpr int kWaves = T / 64, kLanes = T / kParts, kKeep = 4;   // lanes of a part: 16 or 64
+    static_assert(kLanes == 16 || kLanes == 64, "a row of lanes or a wave");
+    static_assert(BDLM_MAX_TOP <= kParts, "as many parts as values");
+    __shared__ float parts[kParts], sums[2][kWaves];
+    __shared__ int firsts[kWaves];
+    __shared__ int ngathered, nvalues;
+    __shared__ int group[kRoom];
+    __shared__ float value[kRoom];
+    __shared__ int column[kRoom];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t i = blockIdx.x;
+    const int k = a.list;
+    const float *top = a.top + i * a.ngroup, *others = a.others + i * a.ngroup, *slopes = a.slope + i * a.ngroup;
+    // the first kKeep * T groups stay in registers
+    Spread g[kKeep];
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) {
+        const int x = tid + T * j;
+        g[j] = x < a.ngroup ? Spread{top[x], others[x], slopes[x]} : Spread{-INFINITY, 0.f, 0.f};
+    }
+    const int64_t token = a.token ? a.token[i] : -1;
+    const bool given = token >= 0 && token < a.vocab;
+    const float token_logit = given ? a.token_logit[i] : 0.f;
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) most = fmaxf(most, g[j].top);
+    for (int x = tid + T * kKeep; x < a.ngroup; x += T) most = fmaxf(most, top[x]);
+    most = largest<kLanes == 64>(most);
+    if ((tid & (kLanes - 1)) == kLanes - 1) parts[tid / kLanes] = most;
+    if (tid == 0) ngathered = nvalues = 0;
+    __syncthreads();
+    const float mine = parts[lane & (kParts - 1)];
+    const float m = largest<true>(mine);
+    // the k-th largest of the parts' maxima
+    float bound = -INFINITY;
+    if (k > 0) {
+        int rank = 0;
+#pragma unroll
+        for (int j = 0; j < kParts; ++j) {
+            const float v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j));
+            rank += before(v, j, mine, lane & (kParts - 1));
+        }
+        const uint64_t at = __ballot(rank == k - 1);
+        bound = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), __ffsll(static_cast<unsigned long long>(at)) - 1));
+    }
+    float s_others = 0.f, s_slope = 0.f;
+    int largest_ones = 0;
+    auto take = [&](const Spread &s, int x) {
+        const float f = share(s.top, m);
+        if (s.top == m && m > -INFINITY) {
+            ++largest_ones;
+            s_others += s.others;
+            s_slope += s.slope;
+        } else if (f != 0.f) {
+            s_others = fmaf(1.f + s.others, f, s_others);
+            s_slope = fmaf(fmaf(s.top - m, 1.f + s.others, s.slope), f, s_slope);
+        } else if (s.others != s.others) {   // a NaN stays one
+            s_others = s_slope = s.others;
+        }
+        if (k > 0 && s.top >= bound && s.top > -INFINITY) {
+            const int n = atomicAdd(&ngathered, 1);   // (whatever the order: the places are counted below)
+            if (n < kRoom) group[n] = x;
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kKeep; ++j) take(g[j], tid + T * j);
+    for (int x = tid + T * kKeep; x < a.ngroup; x += T) take(Spread{top[x], others[x], slopes[x]}, x);
+    s_others = wave_total(s_others);
+    s_slope = wave_total(s_slope);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) largest_ones += __shfl_xor(largest_ones, d, 64);
+    if (lane == 0) sums[0][wave] = s_others, sums[1][wave] = s_slope, firsts[wave] = largest_ones;
+    __syncthreads();
+    float z = 0.f, slope = 0.f;
+    int ones = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) z += sums[0][w], slope += sums[1][w], ones += firsts[w];
+    z += static_cast<float>(ones > 0 ? ones - 1 : 0);   // the largest one's own 1 stays out
+    const float rest = fabsf(m) < INFINITY ? log1pf(z) : NAN;
+    if (tid == 0) {
+        if (a.entropy) a.entropy[i] = rest - slope / (1.f + z);
+        if (a.token) a.logprob[i] = given ? (token_logit - m) - rest : 0.f;
+    }
+    if (k == 0) return;
+    auto put = [&](int place, float v, int at) {
+        const bool here = at != kNoColumn;
+        a.top_token[i * k + place] = here ? at : -1;
+        a.top_logprob[i * k + place] = here ? (v - m) - rest : -INFINITY;
+    };
+    auto column_of = [&](int64_t at, int x, int j) { return a.column ? a.column[at] : x * a.width + j; };
+    const int ng = ngathered;
+    if (ng <= kRoom) {
+        for (int x = tid; x < ng * a.width; x += T) {
+            const int from = group[x / a.width], j = x % a.width;
+            const int64_t at = (i * a.ngroup + from) * a.width + j;
+            const float v = a.value[at];
+            if (v >= bound && v > -INFINITY) {
+                const int n = atomicAdd(&nvalues, 1);
+                if (n < kRoom) value[n] = v, column[n] = column_of(at, from, j);
+            }
+        }
+    }
+    __syncthreads();
+    const int nv = nvalues;
+    if (ng <= kRoom && nv <= kRoom) {
+        for (int x = tid; x < nv; x += T) {
+            const float v = value[x];
+            const int c = column[x];
+            int place = 0;
+            for (int j = 0; j < nv; ++j) place += before(value[j], column[j], v, c);
+            if (place < k) put(place, v, c);
+        }
+        if (tid >= nv && tid < k) put(tid, 0.f, kNoColumn);   // fewer than k: the rest of the list is empty
+        return;
+    }
+    // The k largest lie in the k groups whose largest values (then the lower columns) come first: were one in another group, each of
+    // those k would hold one before it.
+    if (wave != 0) return;
+    TopList list;
+    for (int x = lane; x - lane < a.ngroup; x += 64) list.add(x < a.ngroup ? top[x] : -INFINITY, x, k, lane);
+    const TopList groups = list;
+    list = TopList();
+    for (int x0 = 0; x0 < k * a.width; x0 += 64) {
+        const int x = x0 + lane, which = x < k * a.width ? x / a.width : 0, j = x - which * a.width;
+        const int from = __shfl(groups.at, which, 64);
+        const int64_t at = (i * a.ngroup + from) * a.width + j;
+        const bool here = x < k * a.width && from != kNoColumn;
+        const float v = here ? a.value[at] : -INFINITY;
+        list.add(v, here ? column_of(at, from, j) : kNoColumn, k, lane);
+    }
+    if (lane < k) put(lane, list.v, list.at);
+}
+
+}  // namespace
+
+int launch_logprobs(const LogprobsArgs &a, void *stream) {
+    if (a.rows <= 0) return BDLM_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    // Many groups, which few rows have: more threads hold them all.
+    if (a.ngroup > 1024) hipLaunchKernelGGL(bdlm_logprobs_kernel<1024>, dim3(a.rows), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL(bdlm_logprobs_kernel<256>, dim3(a.rows), dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
+}
+
+}  // namespace bdlm

@@ -117,6 +117,15 @@ def test_ties(rows):
         got = bd.head_logprobs(x, w, top=16, exclude=exclude)
         assert torch.equal(got[2].cpu(), torch.tensor(want).expand(rows, 16)), exclude
         check(got, x, w, None, 16, exclude)
+    # more groups, and more values, than are gathered before they are counted
+    for many in (10000, 40000):
+        v = torch.zeros(many, k, dtype=BF, device=DEV)
+        for first in (0, many - 700):
+            v.zero_()
+            v[first:] = 0.5
+            assert torch.equal(bd.head_logprobs(x, v, top=16)[2].cpu(), torch.arange(first, first + 16).expand(rows, 16)), (many, first)
+            assert torch.equal(bd.head_logprobs(x, v, top=3, exclude=first + 1)[2].cpu(),
+                               torch.tensor([first, first + 2, first + 3]).expand(rows, 3))
     # far apart, and equal: in every group of columns one
     w.zero_()
     w[5::37] = 1.0

@@ -1,0 +1,102 @@
+"""The native marshalling of a sublayer's operators and of the head's log-probabilities against the Python code that takes
+every other call: the same answers, the same refusals, and which calls are taken."""
+import pytest
+import torch
+
+import paper_2607_02805_amd as bd
+from tests.test_native_binding import _Absent, _Counting
+
+E4 = torch.float8_e4m3fn
+
+
+def _calls(dev, dtype):
+    g = torch.Generator().manual_seed(1)
+    r = lambda *s: torch.randn(*s, generator=g).to(dev)
+    x, res, wide = r(2, 5, 64).to(dtype), r(2, 5, 64), r(2, 5, 80).to(dtype)
+    wg, wu, wn = r(48, 64).to(dtype), r(48, 64).to(dtype), r(64)
+    bg = r(48)
+    pre = (r(2, 5, 48).to(dtype), r(2, 5, 48).to(dtype))
+    dh, tok = r(2, 5, 48), torch.randint(0, 48, (2, 5), generator=g).to(dev)
+    out = torch.zeros(2, 5, 48, device=dev)
+    return {
+        "norm": lambda: bd.add_rmsnorm(x, wn),
+        "norm_res": lambda: bd.add_rmsnorm(x, wn, res, eps=1e-3, out_dtype=torch.float32),
+        "norm_e4m3": lambda: bd.add_rmsnorm(x, wn, res, out_dtype=E4, scale_block=128, sum=False),
+        "norm_e4m3_row": lambda: bd.add_rmsnorm(wide[..., :64], wn, out_dtype=E4),
+        "norm_place": lambda: bd.add_rmsnorm(x, wn, res, out=torch.zeros(2, 5, 64, device=dev), sum=res.clone()),
+        "norm_back": lambda: bd.add_rmsnorm_backward(x, res, wn, res),
+        "norm_back_one": lambda: bd.add_rmsnorm_backward(x, x, wn, ds=torch.zeros(2, 5, 64, device=dev), dw=None),
+        "gated": lambda: bd.gated_projection(x, wg, wu),
+        "gated_keep": lambda: bd.gated_projection(x, wg, wu, bg, None, act="gelu", pre=True),
+        "gated_place": lambda: bd.gated_projection(x, wg, wu, act=None, out=out, pre=pre),
+        "gated_back": lambda: bd.gated_projection_backward(dh, x, wg, wu, pre, dbg=True, dbu=True),
+        "gated_back_one": lambda: bd.gated_projection_backward(dh, x, wg, wu, pre, dx=None, dw_gate=None),
+        "logprobs": lambda: bd.head_logprobs(x, wg, tok, top=3, exclude=2),
+        "logprobs_top": lambda: bd.head_logprobs(x, wg, top=16, entropy=False),
+        "logprobs_given": lambda: bd.head_logprobs(x, wg, tok),
+        # refused by the C ABI
+        "bad_eps": lambda: bd.add_rmsnorm(x, wn, eps=-1.0),
+        "bad_overlap": lambda: bd.gated_projection(x, wg, wu, pre=(pre[0], pre[0])),
+        "bad_space": lambda: bd.head_logprobs(x, wg, top=2, workspace=torch.zeros(256, dtype=torch.uint8, device=dev)),
+        # left to the Python code, which converts or refuses
+        "int_eps": lambda: bd.add_rmsnorm(x, wn, eps=1),
+        "list_pre": lambda: bd.gated_projection(x, wg, wu, pre=list(pre)),
+        "empty": lambda: bd.add_rmsnorm(x[:0], wn),
+        "bad_sum": lambda: bd.add_rmsnorm(x, wn, sum=res),
+        "bad_block": lambda: bd.add_rmsnorm(x, wn, out_dtype=E4, scale_block=64),
+        "bad_type": lambda: bd.add_rmsnorm(x, wn, out_dtype=torch.float16),
+        "bad_scale": lambda: bd.add_rmsnorm(x, wn, scale=res),
+        "no_pre": lambda: bd.gated_projection_backward(dh, x, wg, wu, None),
+        "short_pre": lambda: bd.gated_projection_backward(dh, x, wg, wu, (pre[0], pre[1][..., :40])),
+        "other_w": lambda: bd.gated_projection(x, wg, wu[:40]),
+        "many": lambda: bd.head_logprobs(x, wg, top=17),
+        "too_many": lambda: bd.head_logprobs(x, wg[:5], top=6),
+        "int_tokens": lambda: bd.head_logprobs(x, wg, tok.int()),
+    }
+
+
+NAMES = list(_calls("cpu", torch.float32))
+PLAIN = NAMES[:NAMES.index("int_eps")]
+
+
+def _flat(v):
+    if isinstance(v, (tuple, list)):
+        return [t for u in v for t in _flat(u)]
+    return [v]
+
+
+def _run(monkeypatch, native, name, dtype, dev):
+    monkeypatch.setattr(bd, "_marshal", native)
+    err = out = None
+    try:
+        out = _calls(dev, dtype)[name]()
+    except Exception as e:                                # compared between the two sides
+        err = (type(e), str(e))
+    if dev == "cuda":
+        torch.cuda.synchronize()
+    return err, [None if t is None else t.cpu() for t in _flat(out)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("name", NAMES)
+def test_native_and_python_marshalling_agree(monkeypatch, name, dtype):
+    native = _Counting(bd._native())
+    err, got = _run(monkeypatch, native, name, dtype, "cuda")
+    err2, want = _run(monkeypatch, _Absent(), name, dtype, "cuda")
+    assert native.taken == (name in PLAIN)
+    assert err == err2 and len(got) == len(want)
+    assert (err is not None) == (name.startswith(("bad", "no_", "short", "other", "many", "too", "int_tok")))
+    for a, b in zip(got, want):
+        assert (a is None) == (b is None)
+        if a is not None:
+            assert a.dtype == b.dtype and a.shape == b.shape and a.stride() == b.stride()
+            assert torch.equal(a.view(torch.uint8) if a.dtype == E4 else a, b.view(torch.uint8) if b.dtype == E4 else b)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_off_the_gpu_are_refused_as_before(monkeypatch, name):
+    native = _Counting(bd._native())
+    err, _ = _run(monkeypatch, native, name, torch.float32, "cpu")
+    err2, _ = _run(monkeypatch, _Absent(), name, torch.float32, "cpu")
+    assert native.taken == 0 and err is not None and err == err2
