@@ -197,6 +197,9 @@ struct PackArgs {
     float *colsum;             // [pack_row_blocks(rows)][cols] partial column sums of dst, or null
 };
 int launch_pack(const PackArgs &a, void *stream);
+// Up to kPackMost plain copies (no activation, no column sums) of one type in one launch.
+constexpr int32_t kPackMost = 3;
+int launch_pack_some(const PackArgs *a, int32_t n, void *stream);
 constexpr int32_t kPackRows = 16;   // rows per workgroup
 #ifdef __HIPCC__
 __host__ __device__
@@ -214,6 +217,8 @@ struct GatedPackArgs {
 int launch_gated_pack(const GatedPackArgs &a, void *stream);
 // out[c] = sum over the blocks of part[b][c]
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream);
+// Of two matrices (an out that is null is not wanted).
+int launch_colsum2(const float *part, const float *part2, int32_t blocks, int32_t cols, float *out, float *out2, void *stream);
 
 // The rows that count: row_of[0 .. *count) the rows whose label is a token of the vocabulary
 // other than `exclude`, in order; label[i] that token, and (if given) weight, loss, lse by row.

@@ -41,13 +41,13 @@ __device__ __forceinline__ void store_terms(uint16_t *dst, int64_t plane, const 
 constexpr int kPackBatch = 4;
 static_assert(kPackRows % (4 * kPackBatch) == 0, "whole batches");
 template <bool GRAD, bool BF16, bool PRE16, int TERMS>
-__global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
-    __shared__ float sums[4][64 * 8];
+__device__ __forceinline__ void pack_blocks(const PackArgs &a, int64_t first, int64_t step) {
+    __shared__ float sums[4][GRAD ? 64 * 8 : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t rows = a.rows_dev ? *a.rows_dev : a.rows, rows_up = (rows + 63) / 64 * 64;
     const bool slope = GRAD && a.act != BDLM_ACT_NONE;
     const int64_t across = (a.ld_dst + 511) / 512, blocks = across * pack_row_blocks(a.rows);
-    for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+    for (int64_t block = first; block < blocks; block += step) {
         const int64_t down = block / across;
         const int c0 = static_cast<int>(block - down * across) * 512, c = c0 + lane * 8;
         const int64_t r0 = down * kPackRows;
@@ -99,6 +99,21 @@ __global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
         }
     }
 }
+template <bool GRAD, bool BF16, bool PRE16, int TERMS>
+__global__ void __launch_bounds__(256) bdlm_pack_kernel(const PackArgs a) {
+    pack_blocks<GRAD, BF16, PRE16, TERMS>(a, blockIdx.x, gridDim.x);
+}
+// Several operands in one launch: operand i has the workgroups from first[i] on.
+struct PackSome {
+    PackArgs a[kPackMost];
+    uint32_t first[kPackMost + 1];
+};
+template <bool BF16, int TERMS>
+__global__ void __launch_bounds__(256) bdlm_pack_some_kernel(const PackSome p) {
+    int i = 0;
+    for (int j = 1; j < kPackMost; ++j) i = blockIdx.x >= p.first[j] ? j : i;
+    pack_blocks<false, BF16, BF16, TERMS>(p.a[i], blockIdx.x - p.first[i], p.first[i + 1] - p.first[i]);
+}
 
 // The gradients of a gated product by its factors, as bdlm_pack_kernel lays out the one of a projection: a workgroup takes
 // kPackRows rows of 64 x 8 columns, a thread eight columns of two rows at a time, and writes both parts.
@@ -121,27 +136,35 @@ __global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArg
                 Eight<PRE16> gate[kBatch], up[kBatch];
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    const int64_t r = q + 4 * k, from = r < a.rows ? r : 0;
-                    const int there = r < a.rows ? n : 0;
-                    dh[k].load(a.dh, from * a.ld_dh + c, there);
-                    gate[k].load(a.gate, from * a.ld_pre + c, there);
-                    up[k].load(a.up, from * a.ld_pre + c, there);
+                    const int64_t r = q + 4 * k;
+                    if (r >= a.rows) continue;
+                    dh[k].load(a.dh, r * a.ld_dh + c, n);
+                    gate[k].load(a.gate, r * a.ld_pre + c, n);
+                    up[k].load(a.up, r * a.ld_pre + c, n);
                 }
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
                     const int64_t r = q + 4 * k;
+                    if (r >= a.rows) {   // up to a multiple of 64
+                        const float zero[8] = {};
+                        if (a.dst && r < rows_up) {
+                            store_terms<TERMS>(a.dst + r * 2 * a.ldz + c, a.plane, zero);
+                            store_terms<TERMS>(a.dst + r * 2 * a.ldz + a.ldz + c, a.plane, zero);
+                        }
+                        continue;
+                    }
                     float f[2][8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         float value, slope;
                         act_both<!PRE16>(gate[k].value(e), a.act, value, slope);
-                        const bool here = r < a.rows && e < n;   // (a slope of no column is not 0)
+                        const bool here = e < n;   // (a slope of no column is not 0)
                         f[0][e] = here ? dh[k].value(e) * up[k].value(e) * slope : 0.f;
                         f[1][e] = here ? dh[k].value(e) * value : 0.f;
                         sum[0][e] += f[0][e];
                         sum[1][e] += f[1][e];
                     }
-                    if (a.dst && r < rows_up) {
+                    if (a.dst) {
                         store_terms<TERMS>(a.dst + r * 2 * a.ldz + c, a.plane, f[0]);
                         store_terms<TERMS>(a.dst + r * 2 * a.ldz + a.ldz + c, a.plane, f[1]);
                     }
@@ -163,10 +186,12 @@ __global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArg
     }
 }
 
-// Column sums of the blocks' partial sums: 64 columns a workgroup, sixteen waves over the blocks,
+// Column sums of the blocks' partial sums, of one matrix or two: 64 columns a workgroup, sixteen waves over the blocks,
 // eight loads in flight in each.
-__global__ void __launch_bounds__(1024) bdlm_colsum_kernel(const float *part, int blocks, int cols, float *out) {
+__global__ void __launch_bounds__(1024) bdlm_colsum_kernel(const float *part, const float *part2, int blocks, int cols, float *out,
+                                                          float *out2) {
     __shared__ float sums[16][64];
+    if (blockIdx.y) part = part2, out = out2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = blockIdx.x * 64 + lane;
     float s = 0.f;
@@ -332,9 +357,40 @@ int launch_gated_pack(const GatedPackArgs &a, void *stream) {
     return done();
 }
 
+int launch_pack_some(const PackArgs *a, int32_t n, void *stream) {
+    if (n <= 0) return BDLM_OK;
+    if (n == 1) return launch_pack(a[0], stream);
+    if (n > kPackMost) return BDLM_E_LAUNCH;
+    PackSome p{};
+    uint32_t at = 0;
+    for (int i = 0; i < kPackMost; ++i) {
+        p.first[i] = at;
+        if (i < n) {
+            p.a[i] = a[i];
+            const int64_t blocks = a[i].rows > 0 ? (a[i].ld_dst + 511) / 512 * pack_row_blocks(a[i].rows) : 0;
+            at += static_cast<uint32_t>(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22);
+        }
+        p.first[i + 1] = at;
+    }
+    if (at == 0) return BDLM_OK;
+    const dim3 g(at), b(256);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    // (as PackArgs of Operand::pack: bf16 in one term, fp32 in three)
+    if (a[0].src_bf16) hipLaunchKernelGGL((bdlm_pack_some_kernel<true, 1>), g, b, 0, s, p);
+    else hipLaunchKernelGGL((bdlm_pack_some_kernel<false, 3>), g, b, 0, s, p);
+    return done();
+}
+
+int launch_colsum2(const float *part, const float *part2, int32_t blocks, int32_t cols, float *out, float *out2, void *stream) {
+    if (!out || !out2) return out || out2 ? launch_colsum(out ? part : part2, blocks, cols, out ? out : out2, stream) : BDLM_OK;
+    hipLaunchKernelGGL(bdlm_colsum_kernel, dim3((cols + 63) / 64, 2), dim3(1024), 0, static_cast<hipStream_t>(stream), part,
+                       part2, blocks, cols, out, out2);
+    return done();
+}
+
 int launch_colsum(const float *part, int32_t blocks, int32_t cols, float *out, void *stream) {
     hipLaunchKernelGGL(bdlm_colsum_kernel, dim3((cols + 63) / 64), dim3(1024), 0, static_cast<hipStream_t>(stream),
-                       part, blocks, cols, out);
+                       part, part, blocks, cols, out, out);
     return done();
 }
 

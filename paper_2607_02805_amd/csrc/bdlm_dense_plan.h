@@ -148,9 +148,7 @@ struct Operand {
             mat = Mat{copy, w, up(r, 64) * w};
         }
     }
-    int lay(void *stream, const int32_t *row_of = nullptr, const int32_t *rows_dev = nullptr,
-            const float *scale = nullptr) const {
-        if (direct) return BDLM_OK;
+    PackArgs pack(const int32_t *row_of = nullptr, const int32_t *rows_dev = nullptr, const float *scale = nullptr) const {
         PackArgs a{};
         a.src = src;
         a.ld = ld;
@@ -164,9 +162,23 @@ struct Operand {
         a.ld_dst = mat.ld;
         a.plane = mat.plane;
         a.terms = terms_of(dtype);
-        return launch_pack(a, stream);
+        return a;
+    }
+    int lay(void *stream, const int32_t *row_of = nullptr, const int32_t *rows_dev = nullptr,
+            const float *scale = nullptr) const {
+        return direct ? BDLM_OK : launch_pack(pack(row_of, rows_dev, scale), stream);
     }
 };
+
+// Lays out those of the operands (of one type) that need it, in one launch.
+template <class... O>
+int lay_all(void *stream, const O &...operands) {
+    PackArgs a[sizeof...(operands)];
+    int32_t n = 0;
+    for (const Operand *o : {&operands...})
+        if (!o->direct) a[n++] = o->pack();
+    return launch_pack_some(a, n, stream);
+}
 
 inline TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, int64_t nrow, int64_t ncol, int64_t k,
                  int32_t npair, const Shape &s) {

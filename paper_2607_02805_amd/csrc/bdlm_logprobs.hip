@@ -100,12 +100,14 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
     const int64_t i = blockIdx.x;
     const int k = a.list;
     const float *top = a.top + i * a.ngroup, *others = a.others + i * a.ngroup, *slopes = a.slope + i * a.ngroup;
-    // the first kKeep * T groups stay in registers
+    // Groups go to the parts in turn, so that few of them do not lie in few parts (34 groups for each of 4,032 rows, in the
+    // lanes' order: 26 us instead of 9).  The first kKeep * T groups stay in registers.
+    const int own = (tid & (kLanes - 1)) * kParts + tid / kLanes;
     Spread g[kKeep];
     float most = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kKeep; ++j) {
-        const int x = tid + T * j;
+        const int x = own + T * j;
         g[j] = x < a.ngroup ? Spread{top[x], others[x], slopes[x]} : Spread{-INFINITY, 0.f, 0.f};
     }
     const int64_t token = a.token ? a.token[i] : -1;
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
     const float token_logit = given ? a.token_logit[i] : 0.f;
 #pragma unroll
     for (int j = 0; j < kKeep; ++j) most = fmaxf(most, g[j].top);
-    for (int x = tid + T * kKeep; x < a.ngroup; x += T) most = fmaxf(most, top[x]);
+    for (int x = own + T * kKeep; x < a.ngroup; x += T) most = fmaxf(most, top[x]);
     most = largest<kLanes == 64>(most);
     if ((tid & (kLanes - 1)) == kLanes - 1) parts[tid / kLanes] = most;
     if (tid == 0) ngathered = nvalues = 0;
@@ -152,8 +154,8 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
         }
     };
 #pragma unroll
-    for (int j = 0; j < kKeep; ++j) take(g[j], tid + T * j);
-    for (int x = tid + T * kKeep; x < a.ngroup; x += T) take(Spread{top[x], others[x], slopes[x]}, x);
+    for (int j = 0; j < kKeep; ++j) take(g[j], own + T * j);
+    for (int x = own + T * kKeep; x < a.ngroup; x += T) take(Spread{top[x], others[x], slopes[x]}, x);
     s_others = wave_total(s_others);
     s_slope = wave_total(s_slope);
 #pragma unroll

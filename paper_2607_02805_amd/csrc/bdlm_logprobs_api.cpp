@@ -90,8 +90,7 @@ int bdlm_head_logprobs(const bdlm_dense_desc_t *d, const int64_t *tokens, int64_
         a.top = top;
         TRY(launch_skinny(a, stream));
     } else {
-        TRY(p.x.lay(stream));
-        TRY(p.w.lay(stream));
+        TRY(lay_all(stream, p.x, p.w));
         TileArgs a = product(p.x.mat, false, p.w.mat, false, d->rows, vocab, d->in_features, pairs_of(d->in_dtype), p.shape);
         a.out = kTileTop;
         a.top = top;

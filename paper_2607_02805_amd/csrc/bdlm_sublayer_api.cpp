@@ -28,8 +28,10 @@ int check_rows(const void *p, int64_t rows, int64_t ld) {
 }
 int64_t scales_of(int64_t width, int64_t block) { return block ? (width + block - 1) / block : 1; }
 
+// Partial sums of dw, unless one workgroup writes dw itself.
 int64_t norm_space(int64_t rows, int64_t width) {
-    return up(int64_t(bdlm::add_norm_grad_blocks(rows, width)) * width * 4, 256);
+    const int64_t blocks = bdlm::add_norm_grad_blocks(rows, width);
+    return blocks > 1 ? up(blocks * width * 4, 256) : 0;
 }
 
 // From one operand to the other, in elements.
@@ -205,7 +207,8 @@ int bdlm_add_rmsnorm_backward(int64_t rows, int64_t width, int32_t dy_dtype, con
     a.dsum = dsum;
     a.ds = ds;
     a.w = norm_w;
-    a.part = dw ? static_cast<float *>(ws) : nullptr;
+    const int32_t blocks = add_norm_grad_blocks(rows, width);
+    a.part = dw && blocks > 1 ? static_cast<float *>(ws) : dw;
     a.ldy = dy_stride;
     a.lds = s_stride;
     a.ldt = dsum_stride;
@@ -217,7 +220,7 @@ int bdlm_add_rmsnorm_backward(int64_t rows, int64_t width, int32_t dy_dtype, con
     a.ds_bf16 = ds_dtype == BDLM_DTYPE_BF16;
     a.eps = eps;
     TRY(launch_add_norm_grad(a, stream));
-    return dw ? launch_colsum(a.part, add_norm_grad_blocks(rows, width), a.width, dw, stream) : BDLM_OK;
+    return dw && blocks != 1 ? launch_colsum(a.part, blocks, a.width, dw, stream) : BDLM_OK;
 }
 
 int bdlm_gated_projection_workspace(const bdlm_dense_desc_t *d, int64_t *bytes) { return gated_query<GatedPlan>(d, bytes); }
@@ -268,9 +271,7 @@ int bdlm_gated_projection(const bdlm_dense_desc_t *d, int32_t act, int32_t out_d
         a.gated = g;
         return launch_skinny(a, stream);
     }
-    TRY(p.x.lay(stream));
-    TRY(p.wg.lay(stream));
-    TRY(p.wu.lay(stream));
+    TRY(lay_all(stream, p.x, p.wg, p.wu));
     TileArgs a = product(p.x.mat, false, p.wg.mat, false, d->rows, gated_columns(d->out_features), d->in_features,
                          pairs_of(d->in_dtype), p.shape);
     a.col_duo = between(p.wg.mat, p.wu.mat);
@@ -345,20 +346,21 @@ int bdlm_gated_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int3
     g.sum_gate = db_gate ? p.sum_gate : nullptr;
     g.sum_up = db_up ? p.sum_up : nullptr;
     TRY(launch_gated_pack(g, stream));
-    if (db_gate) TRY(launch_colsum(p.sum_gate, pack_row_blocks(g.rows), n, db_gate, stream));
-    if (db_up) TRY(launch_colsum(p.sum_up, pack_row_blocks(g.rows), n, db_up, stream));
+    TRY(launch_colsum2(p.sum_gate, p.sum_up, pack_row_blocks(g.rows), n, db_gate, db_up, stream));
+    // (what both products need, in one launch)
+    const bool wanted = dw_gate || dw_up, for_dx = dx && d->rows > 0;
+    if (for_dx && wanted) TRY(lay_all(stream, p.wg, p.wu, p.x));
+    else if (for_dx) TRY(lay_all(stream, p.wg, p.wu));
+    else if (wanted) TRY(lay_all(stream, p.x));
     const Mat dz{p.dz, 2 * p.ldz, p.plane};
-    if (dx && d->rows > 0) {
-        TRY(p.wg.lay(stream));
-        TRY(p.wu.lay(stream));
+    if (for_dx) {
         TileArgs a = product(dz, false, p.wg.mat, true, d->rows, d->in_features, n, 2 * np, p.sx);
         a.half = np;
         a.row_duo = p.ldz;
         a.col_duo = between(p.wg.mat, p.wu.mat);
         TRY(store_product(a, plain_store(dx, dx_stride, d->in_dtype), p.part, stream));
     }
-    if (!dw_gate && !dw_up) return BDLM_OK;
-    TRY(p.x.lay(stream));
+    if (!wanted) return BDLM_OK;
     if (!dw_gate || !dw_up) {
         const Mat one{p.dz + (dw_gate ? 0 : p.ldz), dz.ld, dz.plane};
         return store_product(product(one, true, p.x.mat, true, n, d->in_features, d->rows, np, p.sw),
