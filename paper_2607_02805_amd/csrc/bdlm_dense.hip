@@ -116,11 +116,16 @@ __global__ void __launch_bounds__(256) bdlm_pack_some_kernel(const PackSome p) {
 }
 
 // The gradients of a gated product by its factors, as bdlm_pack_kernel lays out the one of a projection: a workgroup takes
-// kPackRows rows of 64 x 8 columns, a thread eight columns of two rows at a time, and writes both parts.
-template <bool DH16, bool PRE16, int TERMS>
-__global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArgs a) {
-    __shared__ float sums[2][4][64 * 8];
+// kPackRows rows of 64 x 8 columns, a thread eight columns of two rows at a time, and writes both parts.  With eight waves each
+// waits for memory once: with four, which take two turns, 768 x 832 takes 10 us instead of 7.5; where there are workgroups
+// for more than a round of the chip four are better, 113 us for 16,384 x 4,096 instead of 124 (kPackWide).  (Four rows a thread at
+// a time leave too few waves: 179.)
+constexpr int64_t kPackWide = 2048;   // workgroups
+template <int WAVES, bool DH16, bool PRE16, int TERMS>
+__global__ void __launch_bounds__(64 * WAVES) bdlm_gated_pack_kernel(const GatedPackArgs a) {
     constexpr int kBatch = 2;
+    __shared__ float sums[2][WAVES][64 * 8];
+    static_assert(kPackRows % (kBatch * WAVES) == 0, "whole turns");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t rows_up = (int64_t(a.rows) + 63) / 64 * 64;
     const int64_t across = (a.ldz + 511) / 512, blocks = across * pack_row_blocks(a.rows);
@@ -131,12 +136,12 @@ __global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArg
         const int n = a.n - c;
         float sum[2][8] = {};
         if (c < a.ldz) {
-            for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += 4 * kBatch) {
+            for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += WAVES * kBatch) {
                 Eight<DH16> dh[kBatch];
                 Eight<PRE16> gate[kBatch], up[kBatch];
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    const int64_t r = q + 4 * k;
+                    const int64_t r = q + WAVES * k;
                     if (r >= a.rows) continue;
                     dh[k].load(a.dh, r * a.ld_dh + c, n);
                     gate[k].load(a.gate, r * a.ld_pre + c, n);
@@ -144,7 +149,7 @@ __global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArg
                 }
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
-                    const int64_t r = q + 4 * k;
+                    const int64_t r = q + WAVES * k;
                     if (r >= a.rows) {   // up to a multiple of 64
                         const float zero[8] = {};
                         if (a.dst && r < rows_up) {
@@ -177,10 +182,13 @@ __global__ void __launch_bounds__(256) bdlm_gated_pack_kernel(const GatedPackArg
 #pragma unroll
             for (int e = 0; e < 8; ++e) sums[p][wave][lane * 8 + e] = sum[p][e];
         __syncthreads();
-        for (int x = threadIdx.x; x < 1024; x += 256) {
+        for (int x = threadIdx.x; x < 1024; x += 64 * WAVES) {
             const int p = x >> 9, y = x & 511;
             float *to = p ? a.sum_up : a.sum_gate;
-            if (to && c0 + y < a.n) to[down * a.n + c0 + y] = (sums[p][0][y] + sums[p][1][y]) + (sums[p][2][y] + sums[p][3][y]);
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) t += sums[p][w][y];
+            if (to && c0 + y < a.n) to[down * a.n + c0 + y] = t;
         }
         __syncthreads();
     }
@@ -338,23 +346,22 @@ int launch_pack(const PackArgs &a, void *stream) {
     return done();
 }
 
+template <bool DH16, bool PRE16, int TERMS>
+int gated_pack_of(const GatedPackArgs &a, hipStream_t s) {
+    const int64_t blocks = (a.ldz + 511) / 512 * pack_row_blocks(a.rows);
+    const dim3 g(static_cast<unsigned>(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22));
+    if (blocks > kPackWide) hipLaunchKernelGGL((bdlm_gated_pack_kernel<4, DH16, PRE16, TERMS>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((bdlm_gated_pack_kernel<8, DH16, PRE16, TERMS>), g, dim3(512), 0, s, a);
+    return done();
+}
+
 int launch_gated_pack(const GatedPackArgs &a, void *stream) {
     if (a.rows <= 0) return BDLM_OK;
-    const int64_t blocks = (a.ldz + 511) / 512 * pack_row_blocks(a.rows);
-    const dim3 g(static_cast<unsigned>(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22)), b(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     // (bf16 inputs: one or two terms; fp32: three)
-    if (a.terms == 1) {
-        if (a.dh_bf16) hipLaunchKernelGGL((bdlm_gated_pack_kernel<true, true, 1>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((bdlm_gated_pack_kernel<false, true, 1>), g, b, 0, s, a);
-    } else if (a.terms == 2) {
-        if (a.dh_bf16) hipLaunchKernelGGL((bdlm_gated_pack_kernel<true, true, 2>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((bdlm_gated_pack_kernel<false, true, 2>), g, b, 0, s, a);
-    } else {
-        if (a.dh_bf16) hipLaunchKernelGGL((bdlm_gated_pack_kernel<true, false, 3>), g, b, 0, s, a);
-        else hipLaunchKernelGGL((bdlm_gated_pack_kernel<false, false, 3>), g, b, 0, s, a);
-    }
-    return done();
+    if (a.terms == 1) return a.dh_bf16 ? gated_pack_of<true, true, 1>(a, s) : gated_pack_of<false, true, 1>(a, s);
+    if (a.terms == 2) return a.dh_bf16 ? gated_pack_of<true, true, 2>(a, s) : gated_pack_of<false, true, 2>(a, s);
+    return a.dh_bf16 ? gated_pack_of<true, false, 3>(a, s) : gated_pack_of<false, false, 3>(a, s);
 }
 
 int launch_pack_some(const PackArgs *a, int32_t n, void *stream) {

@@ -5,7 +5,7 @@
 // columns, and f = exp(top - M), D = top - M:
 //     Z = 1 + others,  others = sum (1 + o) f less the largest one's own 1,  slope = sum f (l + D (1 + o)),
 //     lse = M + log Z,  entropy = log Z - slope / Z   (both terms positive).
-// The k largest values: of sixteen parts of the groups, the k-th largest part's maximum is a bound that at least k values
+// The k largest values: of 16 or 64 parts of the groups, the k-th largest part's maximum is a bound that at least k values
 // reach.  Values that reach it, mostly a few more than k, are gathered and each counts the ones before it, in the order of
 // values and then columns: a count below k is its place.  (Listing them one after the other took 18 us for one row of
 // 1,024 groups.)  Where too many reach the bound, as where all are equal, the first wave lists them one after the other.
@@ -26,19 +26,25 @@ struct Number {
     static constexpr int value = V;
 };
 
-// Largest value of 16 lanes (in their last) or of 64 (WAVE; in every lane).
-template <bool WAVE>
+// Largest value of LANES consecutive lanes (1 or 4: in each of them, 16: in the last, 64: in every lane).
+template <int LANES>
 __device__ __forceinline__ float largest(float v) {
     auto step = [&](auto ctrl, auto mask) {
         const int o = __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value,
                                                   decltype(mask)::value, 0xf, false);
         v = fmaxf(v, __int_as_float(o));
     };
+    if constexpr (LANES == 1) return v;
+    if constexpr (LANES == 4) {
+        step(Number<0xb1>{}, Number<0xf>{});    // quad_perm [1,0,3,2], [2,3,0,1]
+        step(Number<0x4e>{}, Number<0xf>{});
+        return v;
+    }
     step(Number<0x111>{}, Number<0xf>{});   // row_shr:1, 2, 4, 8
     step(Number<0x112>{}, Number<0xf>{});
     step(Number<0x114>{}, Number<0xf>{});
     step(Number<0x118>{}, Number<0xf>{});
-    if constexpr (WAVE) {
+    if constexpr (LANES == 64) {
         step(Number<0x142>{}, Number<0xa>{});   // row_bcast:15 into rows 1 and 3
         step(Number<0x143>{}, Number<0xc>{});   // row_bcast:31 into rows 2 and 3
         v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
@@ -64,7 +70,7 @@ struct TopList {
             const int last_at = __builtin_amdgcn_readlane(at, k - 1);
             const bool can = n != kNoColumn && before(u, n, last, last_at);
             if (!__ballot(can)) return;
-            const float m = largest<true>(can ? u : -INFINITY);
+            const float m = largest<64>(can ? u : -INFINITY);
             uint64_t eq = __ballot(can && u == m);
             int src = __ffsll(static_cast<unsigned long long>(eq)) - 1;
             int number = __builtin_amdgcn_readlane(n, src);
@@ -82,20 +88,26 @@ struct TopList {
     }
 };
 
-constexpr int kParts = 16;         // of the groups: no fewer than BDLM_MAX_TOP
+constexpr int kParts = 64;         // of the groups
 constexpr int kRoom = 256;         // gathered groups, and values
+
+// A gathered value.
+struct alignas(8) Entry {
+    float v;
+    int at;
+};
+
+constexpr int32_t kWaveRows = 256;
 
 template <int T>   // threads
 __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) {
-    constexpr int kWaves = T / 64, kLanes = T / kParts, kKeep = 4;   // lanes of a part: 16 or 64
-    static_assert(kLanes == 16 || kLanes == 64, "a row of lanes or a wave");
-    static_assert(BDLM_MAX_TOP <= kParts, "as many parts as values");
+    constexpr int kWaves = T / 64, kLanes = T / kParts, kKeep = 4;   // lanes of a part
+    static_assert(kLanes == 1 || kLanes == 4 || kLanes == 16, "a lane, a quad or a row of lanes");
     __shared__ float parts[kParts], sums[2][kWaves];
-    __shared__ int firsts[kWaves];
+    __shared__ float firsts[kWaves];
     __shared__ int ngathered, nvalues;
     __shared__ int group[kRoom];
-    __shared__ float value[kRoom];
-    __shared__ int column[kRoom];
+    __shared__ Entry entry[kRoom];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t i = blockIdx.x;
     const int k = a.list;
@@ -116,30 +128,43 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
 #pragma unroll
     for (int j = 0; j < kKeep; ++j) most = fmaxf(most, g[j].top);
     for (int x = own + T * kKeep; x < a.ngroup; x += T) most = fmaxf(most, top[x]);
-    most = largest<kLanes == 64>(most);
+    most = largest<kLanes>(most);
     if ((tid & (kLanes - 1)) == kLanes - 1) parts[tid / kLanes] = most;
     if (tid == 0) ngathered = nvalues = 0;
+    static_assert(kRoom % 16 == 0, "whole turns of the count");
+    for (int x = tid; x < kRoom; x += T) entry[x] = Entry{-INFINITY, kNoColumn};   // (before none)
     __syncthreads();
-    const float mine = parts[lane & (kParts - 1)];
-    const float m = largest<true>(mine);
-    // the k-th largest of the parts' maxima
+    float mine = parts[lane];
+    const float m = largest<64>(mine);
+    // The k-th largest of the parts' maxima.  Of 64 parts a few more than k groups reach it; 16 of them, each of four, are
+    // enough up to k = 8 (11 groups), not for 16 (54).
     float bound = -INFINITY;
     if (k > 0) {
         int rank = 0;
+        auto count = [&](auto step_) {
+            constexpr int step = decltype(step_)::value;
 #pragma unroll
-        for (int j = 0; j < kParts; ++j) {
-            const float v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j));
-            rank += before(v, j, mine, lane & (kParts - 1));
+            for (int j = 0; j < kParts; j += step) {
+                const float v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j));
+                rank += before(v, j, mine, lane);
+            }
+            return __ballot(rank == k - 1 && lane % step == 0);
+        };
+        uint64_t at;
+        if (k > 8) {
+            at = count(Number<1>{});
+        } else {
+            mine = largest<4>(mine);
+            at = count(Number<4>{});
         }
-        const uint64_t at = __ballot(rank == k - 1);
         bound = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), __ffsll(static_cast<unsigned long long>(at)) - 1));
     }
     float s_others = 0.f, s_slope = 0.f;
-    int largest_ones = 0;
+    float largest_ones = 0.f;
     auto take = [&](const Spread &s, int x) {
         const float f = share(s.top, m);
         if (s.top == m && m > -INFINITY) {
-            ++largest_ones;
+            largest_ones += 1.f;
             s_others += s.others;
             s_slope += s.slope;
         } else if (f != 0.f) {
@@ -158,15 +183,14 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
     for (int x = own + T * kKeep; x < a.ngroup; x += T) take(Spread{top[x], others[x], slopes[x]}, x);
     s_others = wave_total(s_others);
     s_slope = wave_total(s_slope);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) largest_ones += __shfl_xor(largest_ones, d, 64);
+    largest_ones = wave_total(largest_ones);
     if (lane == 0) sums[0][wave] = s_others, sums[1][wave] = s_slope, firsts[wave] = largest_ones;
     __syncthreads();
     float z = 0.f, slope = 0.f;
-    int ones = 0;
+    float ones = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) z += sums[0][w], slope += sums[1][w], ones += firsts[w];
-    z += static_cast<float>(ones > 0 ? ones - 1 : 0);   // the largest one's own 1 stays out
+    z += fmaxf(ones - 1.f, 0.f);   // the largest one's own 1 stays out
     const float rest = fabsf(m) < INFINITY ? log1pf(z) : NAN;
     if (tid == 0) {
         if (a.entropy) a.entropy[i] = rest - slope / (1.f + z);
@@ -178,28 +202,49 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
         a.top_token[i * k + place] = here ? at : -1;
         a.top_logprob[i * k + place] = here ? (v - m) - rest : -INFINITY;
     };
-    auto column_of = [&](int64_t at, int x, int j) { return a.column ? a.column[at] : x * a.width + j; };
     const int ng = ngathered;
     if (ng <= kRoom) {
-        for (int x = tid; x < ng * a.width; x += T) {
-            const int from = group[x / a.width], j = x % a.width;
-            const int64_t at = (i * a.ngroup + from) * a.width + j;
-            const float v = a.value[at];
-            if (v >= bound && v > -INFINITY) {
-                const int n = atomicAdd(&nvalues, 1);
-                if (n < kRoom) value[n] = v, column[n] = column_of(at, from, j);
+        // Four values of a thread are asked for at a time, with their columns.  (x / width by a product: x is below 2^16.)
+        const uint32_t inverse = (0xffffffffu / static_cast<uint32_t>(a.width)) + 1u;
+        const int all = ng * a.width;
+        for (int x0 = tid; x0 < all; x0 += 4 * T) {
+            float v[4];
+            int c[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int x = x0 + T * q;
+                const bool here = x < all;
+                const int which = here ? (a.width > 1 ? static_cast<int>(__umulhi(x, inverse)) : x) : 0, j = x - which * a.width;
+                const int from = group[which];
+                const int64_t at = (i * a.ngroup + from) * a.width + j;
+                v[q] = here ? a.value[at] : -INFINITY;
+                c[q] = !here ? kNoColumn : a.column ? a.column[at] : from * a.width + j;
             }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (v[q] >= bound && v[q] > -INFINITY) {
+                    const int n = atomicAdd(&nvalues, 1);
+                    if (n < kRoom) entry[n] = Entry{v[q], c[q]};
+                }
         }
     }
     __syncthreads();
     const int nv = nvalues;
     if (ng <= kRoom && nv <= kRoom) {
-        for (int x = tid; x < nv; x += T) {
-            const float v = value[x];
-            const int c = column[x];
+        // four lanes count for an entry
+        for (int x = tid >> 2; x < nv; x += T / 4) {
+            const Entry e = entry[x];
             int place = 0;
-            for (int j = 0; j < nv; ++j) place += before(value[j], column[j], v, c);
-            if (place < k) put(place, v, c);
+            for (int j = tid & 3; j < nv; j += 16) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const Entry o = entry[j + 4 * q];
+                    place += before(o.v, o.at, e.v, e.at);
+                }
+            }
+            place += __builtin_amdgcn_update_dpp(0, place, 0xb1, 0xf, 0xf, true);
+            place += __builtin_amdgcn_update_dpp(0, place, 0x4e, 0xf, 0xf, true);
+            if ((tid & 3) == 0 && place < k) put(place, e.v, e.at);
         }
         if (tid >= nv && tid < k) put(tid, 0.f, kNoColumn);   // fewer than k: the rest of the list is empty
         return;
@@ -217,7 +262,7 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
         const int64_t at = (i * a.ngroup + from) * a.width + j;
         const bool here = x < k * a.width && from != kNoColumn;
         const float v = here ? a.value[at] : -INFINITY;
-        list.add(v, here ? column_of(at, from, j) : kNoColumn, k, lane);
+        list.add(v, !here ? kNoColumn : a.column ? a.column[at] : from * a.width + j, k, lane);
     }
     if (lane < k) put(lane, list.v, list.at);
 }
@@ -227,8 +272,9 @@ __global__ void __launch_bounds__(T) bdlm_logprobs_kernel(const LogprobsArgs a) 
 int launch_logprobs(const LogprobsArgs &a, void *stream) {
     if (a.rows <= 0) return BDLM_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    // Many groups, which few rows have: more threads hold them all.
-    if (a.ngroup > 1024) hipLaunchKernelGGL(bdlm_logprobs_kernel<1024>, dim3(a.rows), dim3(1024), 0, s, a);
+    // Few rows, or many groups: more threads hold them all.  Many rows of few groups: a wave each.
+    if (a.ngroup <= 256 && a.rows > kWaveRows) hipLaunchKernelGGL(bdlm_logprobs_kernel<64>, dim3(a.rows), dim3(64), 0, s, a);
+    else if (a.ngroup > 1024 || a.rows <= 256) hipLaunchKernelGGL(bdlm_logprobs_kernel<1024>, dim3(a.rows), dim3(1024), 0, s, a);
     else hipLaunchKernelGGL(bdlm_logprobs_kernel<256>, dim3(a.rows), dim3(256), 0, s, a);
     return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }

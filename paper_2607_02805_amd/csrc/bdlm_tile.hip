@@ -303,74 +303,92 @@ __device__ __forceinline__ Best row_best(const TileArgs &a, f32x4 *row, int swap
     return m;
 }
 
-// The record of a row's 64 columns from col1 on, which lie in LDS as row_best has them, and with LIST its `list` largest
-// values in order (the lower column first of equals): their values go to the row's first 16 places, their columns (kNoColumn where
-// there are none) to the next 16.  Taking one out costs some 80 instructions: it is found by the maxima of groups of eight columns,
-// which are kept in registers.
-__device__ __forceinline__ Spread row_top(const TileArgs &a, f32x4 *row, int swap, int col1, int list) {
-    constexpr int kOcts = 8;
-    int n = a.ncol - col1 < 64 ? a.ncol - col1 : 64;
+// Largest value and sum of four consecutive lanes, in each.
+template <int CTRL>
+__device__ __forceinline__ float quad_other(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float quad_largest(float v) {
+    v = fmaxf(v, quad_other<0xb1>(v));
+    return fmaxf(v, quad_other<0x4e>(v));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += quad_other<0xb1>(v);
+    return v + quad_other<0x4e>(v);
+}
+
+// The record of a row and with b.list > 0 its largest values in order (the lower column first of equals), by four consecutive
+// lanes: each has the row's 8 OCTS columns from col1 on, which lie in LDS as quads row[(at + q) ^ swap].  Every step takes the largest
+// value out, some 80 instructions: the lane that has it finds it by the maxima of its groups of eight columns, which are kept in
+// registers, and puts -infinity in its place.  o: the row's place in the records, or less than 0 (nothing is written).
+// (With a lane for 64 columns of a row, and the waves' lists merged by a lane a row, 512 rows of 50,257 of 1,024 with five listed
+// took 88 us instead of 83, with sixteen 120 instead of 108, and 1,800 of 25,757 of 254, in small tiles, 156 instead of 125.)
+template <int OCTS>
+__device__ __forceinline__ void row_top(const TopArgs &b, int ncol, f32x4 *row, int at, int swap, int col1, int lane, int64_t o) {
+    constexpr int kCols = 8 * OCTS;
+    auto place = [&](int c) { return reinterpret_cast<float *>(row + ((at + (c >> 2)) ^ swap)) + (c & 3); };
+    int n = ncol - col1 < kCols ? ncol - col1 : kCols;
     n = n < 0 ? 0 : n;
-    auto place = [&](int c) { return reinterpret_cast<float *>(row + ((c >> 2) ^ swap)) + (c & 3); };
-    for (int c = n; c < 64; ++c) *place(c) = -INFINITY;
-    const int x = a.top.exclude - col1;
+    for (int c = n; c < kCols; ++c) *place(c) = -INFINITY;
+    const int x = b.exclude - col1;
     if (x >= 0 && x < n) *place(x) = -INFINITY;
-    float most[kOcts];
+    float most[OCTS];
 #pragma unroll
-    for (int q = 0; q < kOcts; ++q) {
-        const f32x4 u = row[(2 * q) ^ swap], v = row[(2 * q + 1) ^ swap];
+    for (int q = 0; q < OCTS; ++q) {
+        const f32x4 u = row[(at + 2 * q) ^ swap], v = row[(at + 2 * q + 1) ^ swap];
         most[q] = fmaxf(fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3])), fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
         most[q] = fmaxf(most[q], -INFINITY);   // (nothing but NaN)
     }
-    // Takes the largest value out of the row, which holds -infinity in its place then.
-    auto take = [&](float &value, int &column) {
-        float m = most[0];
+    const int s = lane & 3;
+    auto take = [&](int j) {
+        float own = most[0];
 #pragma unroll
-        for (int q = 1; q < kOcts; ++q) m = fmaxf(m, most[q]);
-        int o = 0;
+        for (int q = 1; q < OCTS; ++q) own = fmaxf(own, most[q]);
+        const float m = quad_largest(own);
+        // the lowest of the lanes that hold it (numbers that are exact as floats)
+        const float first = -quad_largest(own == m ? -static_cast<float>(s) : -4.f);
+        if (first == static_cast<float>(s)) {
+            int g = 0;
 #pragma unroll
-        for (int q = kOcts - 1; q >= 0; --q) o = most[q] == m ? q : o;
-        const f32x4 u = row[(2 * o) ^ swap], v = row[(2 * o + 1) ^ swap];
-        const float w[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-        int e = 0;
+            for (int q = OCTS - 1; q >= 0; --q) g = most[q] == m ? q : g;
+            const f32x4 u = row[(at + 2 * g) ^ swap], v = row[(at + 2 * g + 1) ^ swap];
+            const float w[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+            int e = 0;
 #pragma unroll
-        for (int k = 7; k >= 0; --k) e = w[k] == m ? k : e;
-        float rest = -INFINITY;
+            for (int k = 7; k >= 0; --k) e = w[k] == m ? k : e;
+            float rest = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) rest = fmaxf(rest, k == e ? -INFINITY : w[k]);
-        if (m > -INFINITY) *place(8 * o + e) = -INFINITY;
+            for (int k = 0; k < 8; ++k) rest = fmaxf(rest, k == e ? -INFINITY : w[k]);
+            if (m > -INFINITY) *place(8 * g + e) = -INFINITY;
 #pragma unroll
-        for (int q = 0; q < kOcts; ++q) most[q] = q == o ? rest : most[q];
-        value = m;
-        column = m > -INFINITY ? col1 + 8 * o + e : kNoColumn;
+            for (int q = 0; q < OCTS; ++q) most[q] = q == g ? rest : most[q];
+            if (j < b.list && o >= 0) {
+                b.value[o * b.list + j] = m;
+                b.column[o * b.list + j] = m > -INFINITY ? col1 + 8 * g + e : kNoColumn;
+            }
+        }
+        return m;
     };
-    float value[BDLM_MAX_TOP];
-    int column[BDLM_MAX_TOP];
-    take(value[0], column[0]);
-    Spread r{value[0], 0.f, 0.f};
-    const float ref = r.top == -INFINITY ? 0.f : r.top;
-#pragma unroll 8
-    for (int q = 0; q < 16; ++q) {
-        const f32x4 v = row[q ^ swap];
-        float s[4];
+    const float top = take(0);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float others = 0.f, slope = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = __builtin_amdgcn_exp2f((v[e] - ref) * kLog2e);
-        r.others += (s[0] + s[1]) + (s[2] + s[3]);
-        r.slope += (slope_of(s[0], v[0] - ref) + slope_of(s[1], v[1] - ref)) + (slope_of(s[2], v[2] - ref) + slope_of(s[3], v[3] - ref));
-    }
-    if (list == 0) return r;
+    for (int q = 0; q < 2 * OCTS; ++q) {
+        const f32x4 v = row[(at + q) ^ swap];
+        float t[4];
 #pragma unroll
-    for (int j = 1; j < BDLM_MAX_TOP; ++j) {
-        if (j >= list) break;
-        take(value[j], column[j]);
+        for (int e = 0; e < 4; ++e) t[e] = __builtin_amdgcn_exp2f((v[e] - ref) * kLog2e);
+        others += (t[0] + t[1]) + (t[2] + t[3]);
+        slope += (slope_of(t[0], v[0] - ref) + slope_of(t[1], v[1] - ref)) + (slope_of(t[2], v[2] - ref) + slope_of(t[3], v[3] - ref));
     }
-#pragma unroll
-    for (int j = 0; j < BDLM_MAX_TOP; ++j) {
-        if (j >= list) break;
-        *place(j) = value[j];
-        *place(16 + j) = __int_as_float(column[j]);
+    others = quad_sum(others);
+    slope = quad_sum(slope);
+    if (s == 0 && o >= 0) {
+        b.top[o] = top;
+        b.others[o] = others;
+        b.slope[o] = slope;
     }
-    return r;
+    for (int j = 1; j < b.list; ++j) take(j);
 }
 
 // WR x WC waves of (E / WR) x (E / WC) outputs: of 128 x 64 in a tile of 256, of 64 x 64 in one of
@@ -392,12 +410,11 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     constexpr int WAVES = WR * WC * KS, kWaveGroups = kGroups / KS, FR = E / WR / 32, FC = E / WC / 32;   // fragments of a wave
     constexpr int kBuf = E * kDepth / 8;                 // pieces of an operand's stage
     constexpr bool kTop = OUT == kTileTop;
-    constexpr int kRec = OUT == kTileBest || kTop ? E : 1;
+    constexpr int kRec = OUT == kTileBest ? E : 1;
     __shared__ uint4 sm[BUFS][2 * kBuf];                 // [buffer][col, then row]
     __shared__ RowData rows[OUT == kTileProb || OUT == kTileBest || kTop ? E : 1];
     __shared__ float top[WC][kRec], others[WC][kRec];    // softmax records of the waves' columns
-    __shared__ int at[WC][kTop ? 1 : kRec];
-    __shared__ float slope[WC][kTop ? kRec : 1];
+    __shared__ int at[WC][kRec];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nrow = a.nrow_dev ? *a.nrow_dev : a.nrow;
@@ -583,8 +600,8 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     __syncthreads();   // every wave has read the last stage
 
     // 64 rows of the wave at a time through LDS (a region of its own): consecutive lanes then store
-    // consecutive columns, or a lane has a whole row; quads are permuted by the row against bank
-    // conflicts.
+    // consecutive columns, or a lane has a whole row, or four lanes one (kTileTop); quads are permuted by the row, and then by
+    // the wave, against bank conflicts.
     constexpr int kCols = E / WC, kQuads = kCols / 4, kRows = 64 / kQuads;   // rows of one pass of the wave
     static_assert(WR * WC * 64 * kCols * 4 <= int(sizeof(sm)), "the waves' regions fit");
     f32x4 *mine = reinterpret_cast<f32x4 *>(sm) + (wave % (WR * WC)) * 64 * kQuads;   // (both halves')
@@ -611,7 +628,7 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const f32x16 &v = acc[i][j0 + j];
-                        f32x4 *to = mine + (32 * j + (lane & 31)) * kQuads + ((8 * i + 2 * e + (lane >> 5)) ^ (lane & 15));
+                        f32x4 *to = mine + (32 * j + (lane & 31)) * kQuads + ((8 * i + 2 * e + (lane >> 5)) ^ (lane & 15) ^ (kTop ? 4 * wc : 0));
                         const f32x4 u = {v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
                         *to = add ? u + *to : u;
                     }
@@ -631,54 +648,27 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             if (!kTop && !live) return;
         }
         if constexpr (kTop) {
+            // four lanes a row of all the waves' columns
+            static_assert(64 * WAVES == 4 * 64 * WR && E / WC == 64, "four lanes for each of the part's rows; a wave's columns");
+            if constexpr (KS == 1) __syncthreads();
             const TopArgs &b = a.top;
-            if (live && half == 0) {
-                if (b.token) {
-                    const int token = rows[r1 + lane].label, x = token - col1;
-                    if (x >= 0 && x < kCols)
-                        b.token_logit[row0 + r1 + lane] = token == b.exclude ? -INFINITY : mine[lane * kQuads + ((x >> 2) ^ (lane & 15))][x & 3];
-                }
-                const Spread m = row_top(a, mine + lane * kQuads, lane & 15, col1, b.list);
-                top[wc][r1 + lane] = m.top;
-                others[wc][r1 + lane] = m.others;
-                slope[wc][r1 + lane] = m.slope;
+            const int r = threadIdx.x >> 2, s = threadIdx.x & 3, x = r & 63;
+            const int tile_row = (r >> 6) * (E / WR) + 32 * j0 + x;
+            constexpr int kOcts = E / 32;   // of a lane
+            const int w = kOcts == 8 ? s : s >> 1, at = kOcts == 8 ? 0 : 8 * (s & 1), swap = (x & 15) ^ (4 * w);
+            f32x4 *row = reinterpret_cast<f32x4 *>(sm) + (((r >> 6) + WR * w) * 64 + x) * kQuads;
+            const int mine1 = static_cast<int>(col0) + 8 * kOcts * s;
+            const bool counts = row0 + tile_row < nrow;
+            if (b.token) {
+                const int token = rows[tile_row].label, y = token - mine1;
+                if (counts && y >= 0 && y < 8 * kOcts)
+                    b.token_logit[row0 + tile_row] = token == b.exclude ? -INFINITY : row[(at + (y >> 2)) ^ swap][y & 3];
             }
-            if (b.list == 0) return;
-            __syncthreads();
-            // a thread a row merges the lists of its WC waves
-            const int x = threadIdx.x & 63, w0 = threadIdx.x >> 6;
-            const int r = w0 * (E / WR) + 32 * j0 + x;   // (of the tile)
-            if (w0 < WR && row0 + r < nrow) {
-                const f32x4 *from = reinterpret_cast<const f32x4 *>(sm) + (w0 * 64 + x) * kQuads;
-                auto entry = [&](int w, int j) {   // value or column j of wave w's list
-                    return reinterpret_cast<const float *>(from + w * (WR * 64 * kQuads) + ((j >> 2) ^ (x & 15)))[j & 3];
-                };
-                float head[WC];
-                int pos[WC];
-#pragma unroll
-                for (int w = 0; w < WC; ++w) head[w] = entry(w, 0), pos[w] = 0;
-                const int64_t o = ((row0 + r) * b.ngroup + tile_c) * b.list;
-                for (int j = 0; j < b.list; ++j) {
-                    int best = 0, p = pos[0];
-                    float v = head[0];
-#pragma unroll
-                    for (int w = 1; w < WC; ++w)
-                        if (head[w] > v) v = head[w], best = w, p = pos[w];   // (equal: the lower columns)
-                    b.value[o + j] = v;
-                    b.column[o + j] = __float_as_int(entry(best, 16 + p));
-                    const float after = p + 1 < b.list ? entry(best, p + 1) : -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < WC; ++w) {
-                        head[w] = w == best ? after : head[w];
-                        pos[w] += w == best && p + 1 < b.list;
-                    }
-                }
-            }
-            __syncthreads();   // before the next part's sums take the place
+            row_top<kOcts>(b, a.ncol, row, at, swap, mine1, lane, counts ? (row0 + tile_row) * b.ngroup + tile_c : -1);
+            if constexpr (KS == 1) __syncthreads();   // before the next part's sums take the place
             return;
         }
-        if constexpr (kTop) {
-        } else if constexpr (OUT == kTileBest) {
+        if constexpr (OUT == kTileBest) {
             if (half != 0) return;
             const Best m = row_best(a, mine + lane * kQuads, lane & 15, kCols, col1);
             top[wc][r1 + lane] = m.top;
@@ -717,19 +707,6 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     part(Int<0>{});
     if constexpr (FR > 2) part(Int<2>{});
     static_assert(FR == 2 || (FR == 4 && KS == 1), "parts of 64 rows, one where the halves meet");
-    if constexpr (kTop) {
-        __syncthreads();
-        for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
-            if (row0 + x >= nrow) continue;
-            Spread m{top[0][x], others[0][x], slope[0][x]};
-#pragma unroll
-            for (int w = 1; w < WC; ++w) m = merge(m, Spread{top[w][x], others[w][x], slope[w][x]});
-            const int64_t o = (row0 + x) * a.top.ngroup + tile_c;
-            a.top.top[o] = m.top;
-            a.top.others[o] = m.others;
-            a.top.slope[o] = m.slope;
-        }
-    }
     if constexpr (OUT == kTileBest) {
         __syncthreads();
         for (int x = threadIdx.x; x < E; x += 64 * WAVES) {
