@@ -80,16 +80,19 @@ __device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, f32x4 bias, 
     }
 }
 
-// Four consecutive values to a row of bf16 or fp32, n of which there are.
+// Four consecutive values to a row of bf16 or fp32, n of which there are.  Nontemporal: what a tile stores is not read again by the
+// launch, whose operands keep the L2 (the gated product of 16,384 x 1,024 x 4,096, kept: 321 us with plain stores, 313 so).
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ void put4(void *dst, int64_t o, int n, bool whole, bool bf16, f32x4 v) {
     if (bf16) {
         uint16_t *p = static_cast<uint16_t *>(dst) + o;
-        if (whole) *reinterpret_cast<uint2 *>(p) = uint2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+        if (whole)
+            __builtin_nontemporal_store(u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])}, reinterpret_cast<u32x2 *>(p));
         else
             for (int e = 0; e < n; ++e) p[e] = static_cast<uint16_t>(bf16_bits(v[e]));
     } else {
         float *p = static_cast<float *>(dst) + o;
-        if (whole) *reinterpret_cast<f32x4 *>(p) = v;
+        if (whole) __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(p));
         else
             for (int e = 0; e < n; ++e) p[e] = v[e];
     }
