@@ -29,7 +29,7 @@ enum TileOut {
     kTileProb = 3,     // gradient of the loss by the logits, in bf16 terms
     kTileGated = 4,    // act(gate) * up -> out, of products with two weight matrices
     kTileGatedPart = 5,   // their fp32 partial sums
-    kTileTwo = 6,      // kTileStore whose rows go to two matrices
+    kTileTwo = 6,      // stored as they are, without a projection's epilogue; rows may go to two matrices
     kTileTop = 7       // per row: as kTileBest, with the slope of the exponentials' sum, and the largest values in order
 };
 

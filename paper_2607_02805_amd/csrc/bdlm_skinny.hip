@@ -153,13 +153,13 @@ __global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const Sk
     if constexpr (kGated) {
         for (int x = threadIdx.x; x < 16 * MT * 4; x += blockDim.x) {
             const int r = x >> 2, c = (x & 3) * 4;
-            f32x4 gate = gated_bias(a.gated.bias_gate, col0 + c, a.gated.n), up = gated_bias(a.gated.bias_up, col0 + c, a.gated.n);
+            f32x4 gate[1] = {gated_bias(a.gated.bias_gate, col0 + c, a.gated.n)}, up[1] = {gated_bias(a.gated.bias_up, col0 + c, a.gated.n)};
             for (int w = 0; w < waves; ++w) {
                 const float *p = part + (w * 16 * MT + r) * kPitch + c;
-                gate += *reinterpret_cast<const f32x4 *>(p);
-                up += *reinterpret_cast<const f32x4 *>(p + 16);
+                gate[0] += *reinterpret_cast<const f32x4 *>(p);
+                up[0] += *reinterpret_cast<const f32x4 *>(p + 16);
             }
-            if (r < nrow) gated4(a.gated, gate, up, r, col0 + c);
+            gated4(a.gated, gate, up, r, nrow - r, col0 + c);
         }
         return;
     }

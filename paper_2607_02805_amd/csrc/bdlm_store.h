@@ -106,24 +106,44 @@ __device__ __forceinline__ f32x4 gated_bias(const float *bias, int col, int n) {
     }
     return v;
 }
-// Four consecutive columns of one row of a gated product, biases added already: act(gate) * up, of the unrounded ones.
-__device__ __forceinline__ void gated4(const GatedArgs &a, f32x4 gate, f32x4 up, int64_t row, int col) {
+// Four consecutive columns of N consecutive rows (`there` of which there are) of a gated product, biases added already:
+// act(gate) * up, of the unrounded ones.  All rows take a step before any takes the next: one after the other, whose chains of
+// reads, exponentials and reciprocals wait for each, the end of a small tile took 2.4 us instead
+// of 1.1 (512 x 1,024 x 4,096 13.7 instead of 12.3, 16,384 rows of it 273 instead of 250).
+template <int N>
+__device__ __forceinline__ void gated4(const GatedArgs &a, f32x4 (&gate)[N], f32x4 (&up)[N], int64_t row, int there, int col) {
     const int n = a.n - col < 4 ? a.n - col : 4;
-    if (n <= 0) return;
+    if (n <= 0 || there <= 0) return;
     if (a.pre_gate) {
-        const int64_t o = row * a.ld_pre + col;
         const bool whole = n == 4 && a.ld_pre % 4 == 0;
-        put4(a.pre_gate, o, n, whole, a.pre_bf16, gate);
-        put4(a.pre_up, o, n, whole, a.pre_bf16, up);
-    }
-    if (a.act == BDLM_ACT_GELU && !a.out_bf16) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) gate[e] = act_value<true>(gate[e], BDLM_ACT_GELU);
-    } else if (a.act != BDLM_ACT_NONE) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) gate[e] = act_value<false>(gate[e], a.act);
+        for (int k = 0; k < N; ++k)
+            if (k < there) {
+                const int64_t o = (row + k) * a.ld_pre + col;
+                put4(a.pre_gate, o, n, whole, a.pre_bf16, gate[k]);
+                put4(a.pre_up, o, n, whole, a.pre_bf16, up[k]);
+            }
     }
-    put4(a.out, row * a.ld_out + col, n, n == 4 && a.ld_out % 4 == 0, a.out_bf16, gate * up);
+    if (a.act == BDLM_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) gate[k][e] = act_value<false>(gate[k][e], BDLM_ACT_SILU);
+    } else if (a.act == BDLM_ACT_GELU && a.out_bf16) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) gate[k][e] = act_value<false>(gate[k][e], BDLM_ACT_GELU);
+    } else if (a.act == BDLM_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) gate[k][e] = act_value<true>(gate[k][e], BDLM_ACT_GELU);
+    }
+    const bool whole = n == 4 && a.ld_out % 4 == 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (k < there) put4(a.out, (row + k) * a.ld_out + col, n, whole, a.out_bf16, gate[k] * up[k]);
 }
 
 }  // namespace

@@ -101,6 +101,18 @@ int gated_space(const bdlm_dense_desc_t *d, const void *ws, int64_t bytes) {
     if (!ws || bytes < plan.ws.used) return BDLM_E_WORKSPACE;
     return aligned(ws, 256) ? BDLM_OK : BDLM_E_ALIGN;
 }
+// A product stored without an epilogue, split and joined where its shape says so: rows below two_rows go to s.out, those
+// from two_at on to two_out.
+int store_plain(TileArgs a, const StoreArgs &s, void *two_out, int32_t two_rows, int32_t two_at, float *part, void *stream) {
+    a.store = s;
+    a.two_out = two_out;
+    a.two_rows = two_rows;
+    a.two_at = two_at;
+    a.out = a.splits > 1 ? kTilePartial : kTileTwo;
+    a.part = part;
+    TRY(launch_tile(a, stream));
+    return a.splits > 1 ? launch_join_two(part, a.splits, a.nrow, a.ncol, two_out, two_rows, two_at, s, stream) : BDLM_OK;
+}
 int check_act(int32_t act) { return act < BDLM_ACT_NONE || act > BDLM_ACT_GELU ? BDLM_E_SHAPE : BDLM_OK; }
 
 }  // namespace
@@ -358,24 +370,16 @@ int bdlm_gated_projection_backward(const bdlm_dense_desc_t *d, int32_t act, int3
         a.half = np;
         a.row_duo = p.ldz;
         a.col_duo = between(p.wg.mat, p.wu.mat);
-        TRY(store_product(a, plain_store(dx, dx_stride, d->in_dtype), p.part, stream));
+        TRY(store_plain(a, plain_store(dx, dx_stride, d->in_dtype), nullptr, a.nrow, a.nrow, p.part, stream));
     }
     if (!wanted) return BDLM_OK;
     if (!dw_gate || !dw_up) {
         const Mat one{p.dz + (dw_gate ? 0 : p.ldz), dz.ld, dz.plane};
-        return store_product(product(one, true, p.x.mat, true, n, d->in_features, d->rows, np, p.sw),
-                             plain_store(dw_gate ? dw_gate : dw_up, dw_stride, d->in_dtype), p.part, stream);
+        return store_plain(product(one, true, p.x.mat, true, n, d->in_features, d->rows, np, p.sw),
+                           plain_store(dw_gate ? dw_gate : dw_up, dw_stride, d->in_dtype), nullptr, n, n, p.part, stream);
     }
-    TileArgs a = product(dz, true, p.x.mat, true, p.ldz + n, d->in_features, d->rows, np, p.sw);
-    a.store = plain_store(dw_gate, dw_stride, d->in_dtype);
-    a.two_out = dw_up;
-    a.two_rows = n;
-    a.two_at = static_cast<int32_t>(p.ldz);
-    a.out = p.sw.splits > 1 ? kTilePartial : kTileTwo;
-    a.part = p.part;
-    TRY(launch_tile(a, stream));
-    return p.sw.splits > 1 ? launch_join_two(p.part, p.sw.splits, a.nrow, a.ncol, a.two_out, a.two_rows, a.two_at, a.store, stream)
-                           : BDLM_OK;
+    return store_plain(product(dz, true, p.x.mat, true, p.ldz + n, d->in_features, d->rows, np, p.sw),
+                       plain_store(dw_gate, dw_stride, d->in_dtype), dw_up, n, static_cast<int32_t>(p.ldz), p.part, stream);
 }
 
 }  // extern "C"

@@ -219,8 +219,6 @@ __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias
                                           int nrow, int split) {
     if constexpr (OUT == kTileStore) {
         store4(a.store, v, bias, r, c, a.ncol);
-    } else if constexpr (OUT == kTileTwo) {
-        store_two(a.store, a.two_out, a.two_rows, a.two_at, v, r, c, a.ncol);
     } else if constexpr (OUT == kTilePartial || OUT == kTileGatedPart) {
         float *to = a.part + (int64_t(split) * (a.splits ? a.nrow : nrow) + r) * a.ncol + c;
         if (c + 4 <= a.ncol && a.ncol % 4 == 0) {
@@ -438,9 +436,13 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
     const int64_t row0 = int64_t(tile_r) * E, col0 = int64_t(tile_c) * E;
 
     const int nkt = (K + kDepth - 1) / kDepth;
-    const int64_t steps = int64_t(nkt) * a.npair;
-    const int it0 = static_cast<int>(steps * split / splits);
-    const int n = static_cast<int>(steps * (split + 1) / splits) - it0;
+    // (below 2^31: 2^16 stages, twelve pairs, 16 splits)
+    const uint32_t steps = static_cast<uint32_t>(nkt) * a.npair;
+    int it0 = 0, n = static_cast<int>(steps);
+    if (splits > 1) {
+        it0 = static_cast<int>(steps * split / splits);
+        n = static_cast<int>(steps * (split + 1) / splits) - it0;
+    }
 
     Stage<E, COLT, WAVES, true> sc;
     Stage<E, ROWT, WAVES, false> sr;
@@ -494,7 +496,7 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
         const char *c, *r;
         int left, skip;
     };
-    int pair = it0 / (nkt > 0 ? nkt : 1), kt = it0 - pair * nkt;
+    int pair = it0 > 0 ? it0 / nkt : 0, kt = it0 - pair * nkt;
     auto col_at = [&](int i) { return i < a.half ? col_term(a.half, i) * a.col.plane : a.col_duo + col_term(a.half, i - a.half) * a.col.plane; };
     auto row_at = [&](int i) { return i < a.half ? row_term(a.half, i) * a.row.plane : a.row_duo + row_term(a.half, i - a.half) * a.row.plane; };
     From next{sc.at_step(col_at(pair), kt), sr.at_step(row_at(pair), kt), K - kt * kDepth, a.skip - kt * kDepth};
@@ -686,11 +688,35 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             static_assert(kCols == 64, "a fragment of either matrix");
             const int most = static_cast<int>(rows_out - row0) - r1;
             // (rows eight apart in a pass: their quads lie in both halves of the banks)
-#pragma unroll 4
-            for (int k = 0; k < 8 / KS; ++k) {
-                const int x = half * (8 / KS) + k + 8 * gate_sub;
-                const f32x4 gate = mine[x * kQuads + (gate_quad ^ (x & 15))], up = mine[x * kQuads + ((gate_quad + 8) ^ (x & 15))];
-                if (x < most) gated4(a.gated, gate + bias, up + bias_up, row0 + r1 + x, gate_col);
+            constexpr int kBatch = 4;
+#pragma unroll
+            for (int k0 = 0; k0 < 8 / KS; k0 += kBatch) {
+                f32x4 gate[kBatch], up[kBatch];
+                const int x0 = half * (8 / KS) + k0 + 8 * gate_sub;
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const f32x4 *from = mine + (x0 + k) * kQuads;
+                    gate[k] = from[gate_quad ^ ((x0 + k) & 15)] + bias;
+                    up[k] = from[(gate_quad + 8) ^ ((x0 + k) & 15)] + bias_up;
+                }
+                gated4(a.gated, gate, up, row0 + r1 + x0, most - x0, gate_col);
+            }
+        } else if constexpr (OUT == kTileTwo) {
+            // (four rows' reads, then their stores)
+            const int most = static_cast<int>(rows_out - row0) - r1;
+            constexpr int kBatch = 4, kTurns = 64 / KS / kRows;
+            static_assert(kTurns % kBatch == 0, "whole batches");
+#pragma unroll
+            for (int t = 0; t < kTurns; t += kBatch) {
+                const int x0 = sub + half * (64 / KS) + t * kRows;
+                f32x4 v[kBatch];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) v[k] = mine[(x0 + k * kRows) * kQuads + (quad ^ ((x0 + k * kRows) & 15))];
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const int x = x0 + k * kRows;
+                    if (x < most) store_two(a.store, a.two_out, a.two_rows, a.two_at, v[k], row0 + r1 + x, col1 + 4 * quad, a.ncol);
+                }
             }
         } else {
             const int most = static_cast<int>(rows_out - row0) - r1;
@@ -801,7 +827,8 @@ __global__ void __launch_bounds__(256) bdlm_join_gated_kernel(const float *part,
         const int c = static_cast<int>(x - r * quads) * 4;
         const float *p = part + r * ncol + (c >> 5) * 64 + (c & 31);
         const f32x4 gate = sum_slices(p, slice, splits), up = sum_slices(p + 32, slice, splits);
-        gated4(g, gate + gated_bias(g.bias_gate, c, g.n), up + gated_bias(g.bias_up, c, g.n), r, c);
+        f32x4 both[2][1] = {{gate + gated_bias(g.bias_gate, c, g.n)}, {up + gated_bias(g.bias_up, c, g.n)}};
+        gated4(g, both[0], both[1], r, 1, c);
     }
 }
 
@@ -827,6 +854,7 @@ int launch_tile(const TileArgs &a, void *stream) {
         else if (lay == 3) r = launch_one<true, true, kTilePartial>(a, g, s);
     } else if (a.out == kTileTwo) {
         if (lay == 3) r = launch_one<true, true, kTileTwo>(a, g, s);
+        else if (lay == 1) r = launch_one<false, true, kTileTwo>(a, g, s);
     } else if (lay == 0) {
         if (a.out == kTileBest) r = launch_one<false, false, kTileBest>(a, g, s);
         else if (a.out == kTileProb) r = launch_one<false, false, kTileProb>(a, g, s);

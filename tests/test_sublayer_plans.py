@@ -69,7 +69,7 @@ extern "C" int64_t between_copies(int64_t m, int64_t k, int64_t n, int32_t dt, i
 }
 """
 
-STORE, PARTIAL, GATED, GATED_PART, TWO, TOP = 0, 1, 4, 5, 6, 7
+PARTIAL, GATED, GATED_PART, TWO, TOP = 1, 4, 5, 6, 7
 F32, BF = bd.DTYPE_F32, bd.DTYPE_BF16
 
 
@@ -94,32 +94,35 @@ def launches(plans, op, m, k, n, dt, top=0):
     return [tuple(out[i:i + 7]) for i in range(0, got, 7)]
 
 
-# The sizes of tests/test_gpu_sublayer_chain.py, and what each is there for: (kind, tile edge, buffers, whether split)
+# The sizes of tests/test_gpu_sublayer_chain.py, and what each is there for: (kind, tile edge, buffers, whether split, which
+# operands are read across their rows: 0 none, 1 the weights, for dx, 3 both, for dw)
 GATED_SIZES = {
-    (20, 64, 70): {(GATED, 0, 0, False)},
-    (40, 64, 30000): {(GATED, 128, 2, False)},
-    (40, 64, 70): {(GATED, 128, 4, False)},
-    (300, 64, 12000): {(GATED, 256, 2, False)},
-    (40, 1600, 70): {(GATED_PART, 128, 4, True)},
-    (20000, 4096, 70): {(GATED_PART, 256, 2, True)},
+    (20, 64, 70): {(GATED, 0, 0, False, 0)},
+    (40, 64, 30000): {(GATED, 128, 2, False, 0)},
+    (40, 64, 70): {(GATED, 128, 4, False, 0)},
+    (300, 64, 12000): {(GATED, 256, 2, False, 0)},
+    (40, 1600, 70): {(GATED_PART, 128, 4, True, 0)},
+    (20000, 4096, 70): {(GATED_PART, 256, 2, True, 0)},
 }
 GRAD_SIZES = {
-    (20, 64, 30000): {(TWO, 128, 2, False)},
-    (20, 64, 70): {(TWO, 128, 4, False), (STORE, 128, 4, False)},
-    (20, 512, 4100): {(TWO, 256, 2, False)},
-    (1000, 64, 70): {(PARTIAL, 128, 4, True)},
-    (20000, 64, 4100): {(PARTIAL, 128, 2, True)},
-    (4500, 192, 4100): {(PARTIAL, 256, 2, True)},
-    (20000, 192, 70): {(STORE, 128, 2, False)},
-    (4500, 2048, 70): {(STORE, 256, 2, False)},
-    (20, 4096, 12000): {(PARTIAL, 128, 2, True)},
+    (20, 64, 30000): {(TWO, 128, 2, False, 3)},
+    (20, 64, 70): {(TWO, 128, 4, False, 3), (TWO, 128, 4, False, 1)},
+    (20, 512, 4100): {(TWO, 256, 2, False, 3)},
+    (1000, 64, 70): {(PARTIAL, 128, 4, True, 3)},
+    (20, 64, 260): {(PARTIAL, 128, 4, True, 1)},
+    (20000, 64, 4100): {(PARTIAL, 128, 2, True, 3)},
+    (4500, 192, 4100): {(PARTIAL, 256, 2, True, 3)},
+    (20000, 192, 2048): {(PARTIAL, 256, 2, True, 1)},
+    (20000, 192, 70): {(TWO, 128, 2, False, 1)},
+    (4500, 2048, 70): {(TWO, 256, 2, False, 1)},
+    (20, 4096, 12000): {(PARTIAL, 128, 2, True, 1)},
 }
-TOP_SIZES = {(20, 64, 70): {(TOP, 0, 0, False)}, (40, 64, 70): {(TOP, 128, 4, False)}, (300, 64, 12000): {(TOP, 128, 2, False)},
-             (2000, 64, 4100): {(TOP, 256, 2, False)}}
+TOP_SIZES = {(20, 64, 70): {(TOP, 0, 0, False, 0)}, (40, 64, 70): {(TOP, 128, 4, False, 0)}, (300, 64, 12000): {(TOP, 128, 2, False, 0)},
+             (2000, 64, 4100): {(TOP, 256, 2, False, 0)}}
 
 
 def kinds(got):
-    return {(g[0], g[1], g[2], g[3] > 1) for g in got}
+    return {(g[0], g[1], g[2], g[3] > 1, g[4]) for g in got}
 
 
 def test_the_gpu_tests_reach_every_kind_of_launch(plans):
