@@ -636,7 +636,7 @@ int bdlm_head_select(const bdlm_dense_desc_t *desc, int64_t exclude, const void 
 
 /*
  * What a head says of its tokens, per row: the log-probability of a given one, the entropy of the distribution, and the
- * most probable ones, without the logits in memory (of up to 32 rows, fp32 64, and with alternatives they lie in the workspace).
+ * most probable ones, without all the logits in memory at once (of few rows, or few tiles, they lie in the workspace).
  * With logits l = x w^T over the vocabulary but `exclude` (as bdlm_head_loss), p = softmax(l):
  *     logprob = log p[token],   entropy = - sum p log p.
  * tokens       device int64 [rows], or NULL with logprob NULL (not wanted).  The logprob of `exclude` is -infinity, of a number

@@ -154,7 +154,8 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_kernel(const Add
     float w[K][8];
     auto load_w = [&](int c, float (&v)[8]) {
         Eight<false> t;
-        t.load(a.w, c, a.width - c);
+        t.load(a.w, c, a.width - c, c);
+        t.settle();
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = t.value(e);
     };
@@ -168,10 +169,12 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_kernel(const Add
     };
     auto load = [&](int64_t r, int c, Raw &t) {
         const int n = a.width - c;
-        t.x.load(a.x, r * a.ldx + c, n);
-        if constexpr (RES != Types::kNone) t.r.load(a.residual, r * a.ldr + c, n);
+        t.x.load(a.x, r * a.ldx + c, n, c);
+        if constexpr (RES != Types::kNone) t.r.load(a.residual, r * a.ldr + c, n, c);
     };
-    auto add = [&](const Raw &t, float (&s)[8]) {
+    auto add = [&](Raw &t, float (&s)[8]) {
+        t.x.settle();
+        if constexpr (RES != Types::kNone) t.r.settle();
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             s[e] = t.x.value(e);
@@ -307,7 +310,8 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
     Row<W> row{&lds};
     auto load_w = [&](int c, float (&v)[8]) {
         Eight<false> t;
-        t.load(a.w, c, a.width - c);
+        t.load(a.w, c, a.width - c, c);
+        t.settle();
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = t.value(e);
     };
@@ -316,10 +320,15 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
         Eight<true> h;
         Eight<false> f;
     };
-    auto load_behind = [&](int64_t at, int n, Behind &t) {
+    auto load_behind = [&](int64_t at, int n, int c, Behind &t) {
         if (!a.dsum) return;
-        if (a.ds_bf16) t.h.load(a.dsum, at, n);
-        else t.f.load(a.dsum, at, n);
+        if (a.ds_bf16) t.h.load(a.dsum, at, n, c);
+        else t.f.load(a.dsum, at, n, c);
+    };
+    auto settle_behind = [&](Behind &t) {
+        if (!a.dsum) return;
+        if (a.ds_bf16) t.h.settle();
+        else t.f.settle();
     };
     auto value = [&](const Behind &t, int e) { return !a.dsum ? 0.f : a.ds_bf16 ? t.h.value(e) : t.f.value(e); };
     float *part = a.part ? a.part + int64_t(blockIdx.x) * a.width : nullptr;
@@ -340,11 +349,13 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
 #pragma unroll
             for (int k = 0; k < C; ++k) {
                 const int c = k * kAcross + lane * 8, n = a.width - c;
-                rs[k].load(a.s, r * a.lds + c, n);
-                ry[k].load(a.dy, r * a.ldy + c, n);
-                if (a.ds) load_behind(r * a.ldt + c, n, rb[k]);
+                rs[k].load(a.s, r * a.lds + c, n, c);
+                ry[k].load(a.dy, r * a.ldy + c, n, c);
+                if (a.ds) load_behind(r * a.ldt + c, n, c, rb[k]);
             }
             float ss = 0.f;
+#pragma unroll
+            for (int k = 0; k < C; ++k) rs[k].settle(), ry[k].settle();
 #pragma unroll
             for (int k = 0; k < C; ++k)
 #pragma unroll
@@ -371,6 +382,7 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
             for (int k = 0; k < C; ++k) {
                 const int c = k * kAcross + lane * 8;
                 float d[8];
+                settle_behind(rb[k]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float n = rs[k].value(e) * rstd;
@@ -400,7 +412,8 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
             auto each = [&](auto f) {
                 for (int c = lane * 8; c < a.width; c += kAcross) {
                     Eight<S16> t;
-                    t.load(a.s, r * a.lds + c, a.width - c);
+                    t.load(a.s, r * a.lds + c, a.width - c, c);
+                    t.settle();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f(t.value(e));
                 }
@@ -414,9 +427,11 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
                 Eight<S16> s;
                 Eight<Y16> y;
                 float w[8], d[8];
-                s.load(a.s, r * a.lds + c, a.width - c);
-                y.load(a.dy, r * a.ldy + c, a.width - c);
+                s.load(a.s, r * a.lds + c, a.width - c, c);
+                y.load(a.dy, r * a.ldy + c, a.width - c, c);
                 load_w(c, w);
+                s.settle();
+                y.settle();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float n = s.value(e) * rstd;
@@ -426,7 +441,8 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
                 if (part) {
                     if (r != static_cast<int64_t>(blockIdx.x)) {
                         Eight<false> before;   // (this lane's own writes)
-                        before.load(part, c, a.width - c);
+                        before.load(part, c, a.width - c, c);
+                        before.settle();
 #pragma unroll
                         for (int e = 0; e < 8; ++e) d[e] += before.value(e);
                     }
@@ -440,10 +456,13 @@ __global__ void __launch_bounds__(64 * kWaves) bdlm_add_rmsnorm_grad_kernel(cons
                 Eight<Y16> y;
                 Behind b;
                 float w[8], d[8];
-                s.load(a.s, r * a.lds + c, a.width - c);
-                y.load(a.dy, r * a.ldy + c, a.width - c);
-                load_behind(r * a.ldt + c, a.width - c, b);
+                s.load(a.s, r * a.lds + c, a.width - c, c);
+                y.load(a.dy, r * a.ldy + c, a.width - c, c);
+                load_behind(r * a.ldt + c, a.width - c, c, b);
                 load_w(c, w);
+                s.settle();
+                y.settle();
+                settle_behind(b);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     d[e] = fmaf(rstd, fmaf(-s.value(e) * rstd, dot, w[e] * y.value(e)), value(b, e));

@@ -262,6 +262,11 @@ struct LogprobsArgs {
 };
 int launch_logprobs(const LogprobsArgs &a, void *stream);
 
+// The records and values of TopArgs from the partial sums of a split product, in groups of kJoinGroup columns, all of whose values
+// are kept (where t.list > 0).
+constexpr int32_t kJoinGroup = 64;
+int launch_join_top(const float *part, int32_t splits, int32_t nrow, int32_t ncol, const TopArgs &t, void *stream);
+
 // Zeros the rows of dx (bytes per row a multiple of the element) whose label does not count.
 int launch_zero_rows(const int64_t *labels, int64_t exclude, int32_t vocab, int32_t rows, void *dx,
                      int64_t ld, int32_t cols, int32_t bf16, void *stream);

@@ -61,13 +61,15 @@ __device__ __forceinline__ void pack_blocks(const PackArgs &a, int64_t first, in
                 for (int k = 0; k < kPackBatch; ++k) {
                     const int64_t r = q + 4 * k;
                     const int64_t from = r >= rows ? 0 : a.row_of ? a.row_of[r] : r;
-                    v[k].load(a.src, from * a.ld + c, r < rows ? n : 0);
-                    if (slope) z[k].load(a.pre, from * a.ld_pre + c, r < rows ? n : 0);
+                    v[k].load(a.src, from * a.ld + c, r < rows ? n : 0, c);
+                    if (slope) z[k].load(a.pre, from * a.ld_pre + c, r < rows ? n : 0, c);
                 }
 #pragma unroll
                 for (int k = 0; k < kPackBatch; ++k) {
                     const int64_t r = q + 4 * k;
                     float f[8];
+                    v[k].settle();
+                    if (slope) z[k].settle();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] = v[k].value(e);
                     if constexpr (!GRAD && BF16 && TERMS == 1) {
@@ -143,9 +145,9 @@ __global__ void __launch_bounds__(64 * WAVES) bdlm_gated_pack_kernel(const Gated
                 for (int k = 0; k < kBatch; ++k) {
                     const int64_t r = q + WAVES * k;
                     if (r >= a.rows) continue;
-                    dh[k].load(a.dh, r * a.ld_dh + c, n);
-                    gate[k].load(a.gate, r * a.ld_pre + c, n);
-                    up[k].load(a.up, r * a.ld_pre + c, n);
+                    dh[k].load(a.dh, r * a.ld_dh + c, n, c);
+                    gate[k].load(a.gate, r * a.ld_pre + c, n, c);
+                    up[k].load(a.up, r * a.ld_pre + c, n, c);
                 }
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
@@ -159,6 +161,9 @@ __global__ void __launch_bounds__(64 * WAVES) bdlm_gated_pack_kernel(const Gated
                         continue;
                     }
                     float f[2][8];
+                    dh[k].settle();
+                    gate[k].settle();
+                    up[k].settle();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         float value, slope;

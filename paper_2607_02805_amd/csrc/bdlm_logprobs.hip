@@ -17,6 +17,7 @@
 #include "bdlm.h"
 #include "bdlm_dense.h"
 #include "bdlm_dense_device.h"
+#include "bdlm_store.h"
 
 namespace bdlm {
 namespace {
@@ -87,6 +88,75 @@ struct TopList {
         }
     }
 };
+
+// f over the 16 lanes of a row, in each of them.
+template <class F>
+__device__ __forceinline__ float over_row(float v, F f) {
+    auto step = [&](auto ctrl) {
+        v = f(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    step(Number<0x121>{});   // row_ror:1, 2, 4, 8
+    step(Number<0x122>{});
+    step(Number<0x124>{});
+    step(Number<0x128>{});
+    return v;
+}
+
+// A lane has four columns of a row, 16 lanes a group.
+__global__ void __launch_bounds__(256) bdlm_join_top_kernel(const float *part, int splits, int nrow, int ncol, const TopArgs t) {
+    static_assert(kJoinGroup == 64, "16 lanes of four columns");
+    const int across = (ncol + 1023) / 1024;
+    const int64_t slice = int64_t(nrow) * ncol, all = int64_t(nrow) * across;
+    for (int64_t block = blockIdx.x; block < all; block += gridDim.x) {
+        const int64_t r = block / across;
+        const int c = static_cast<int>(block - r * across) * 1024 + threadIdx.x * 4, group = c / kJoinGroup;
+        const float *p = part + r * ncol + c;
+        f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (c + 4 <= ncol) {
+            v = sum_slices(p, slice, splits);
+        } else {
+            for (int e = 0; e < 4; ++e)
+                if (c + e < ncol) {
+                    v[e] = 0.f;
+                    for (int k = 0; k < splits; ++k) v[e] += p[k * slice + e];
+                }
+        }
+        const int64_t token = t.token ? t.token[r] : -1;
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (c + e == t.exclude) v[e] = -INFINITY;
+            if (c + e == token && c + e < ncol) t.token_logit[r] = v[e];
+            top = fmaxf(top, v[e]);
+        }
+        if (t.list > 0 && group < t.ngroup)
+            *reinterpret_cast<f32x4 *>(t.value + r * t.ngroup * kJoinGroup + c) = v;
+        const float m = over_row(top, [](float x, float y) { return fmaxf(x, y); });
+        // the first of the 64 columns that holds it (a number that is exact as a float) stays out of the sums
+        float at = 64.f;
+#pragma unroll
+        for (int e = 3; e >= 0; --e) at = v[e] == m ? static_cast<float>(4 * (threadIdx.x & 15) + e) : at;
+        at = over_row(at, [](float x, float y) { return fminf(x, y); });
+        const float ref = m == -INFINITY ? 0.f : m;
+        float others = 0.f, slope = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (at == static_cast<float>(4 * (threadIdx.x & 15) + e)) continue;
+            const float s = __builtin_amdgcn_exp2f((v[e] - ref) * kLog2e);
+            others += s;
+            slope += slope_of(s, v[e] - ref);
+        }
+        auto sum = [](float x, float y) { return x + y; };
+        others = over_row(others, sum);
+        slope = over_row(slope, sum);
+        if ((threadIdx.x & 15) == 0 && group < t.ngroup) {
+            const int64_t o = r * t.ngroup + group;
+            t.top[o] = m;
+            t.others[o] = others;
+            t.slope[o] = slope;
+        }
+    }
+}
 
 constexpr int kParts = 64;         // of the groups
 constexpr int kRoom = 256;         // gathered groups, and values
@@ -276,6 +346,14 @@ int launch_logprobs(const LogprobsArgs &a, void *stream) {
     if (a.ngroup <= 256 && a.rows > kWaveRows) hipLaunchKernelGGL(bdlm_logprobs_kernel<64>, dim3(a.rows), dim3(64), 0, s, a);
     else if (a.ngroup > 1024 || a.rows <= 256) hipLaunchKernelGGL(bdlm_logprobs_kernel<1024>, dim3(a.rows), dim3(1024), 0, s, a);
     else hipLaunchKernelGGL(bdlm_logprobs_kernel<256>, dim3(a.rows), dim3(256), 0, s, a);
+    return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
+}
+
+int launch_join_top(const float *part, int32_t splits, int32_t nrow, int32_t ncol, const TopArgs &t, void *stream) {
+    if (nrow <= 0 || ncol <= 0) return BDLM_OK;
+    const int64_t blocks = int64_t(nrow) * ((ncol + 1023) / 1024);
+    hipLaunchKernelGGL(bdlm_join_top_kernel, dim3(static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), part, splits, nrow, ncol, t);
     return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH;
 }
 

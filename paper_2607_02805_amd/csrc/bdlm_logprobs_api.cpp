@@ -8,29 +8,33 @@
 
 namespace {
 
+// Few rows' weights stream past; few tiles' contraction is split and the logits joined from partial sums, in memory; else
+// the logits stay in the tiles.
 struct LogprobsPlan {
-    bool skinny;
+    bool skinny, joined;
     Space ws;
     Operand x, w;
     Shape shape;
     int32_t ngroup, width;     // groups of columns, and values of one that are kept
-    float *top, *others, *slope, *token_logit, *value;
+    float *top, *others, *slope, *token_logit, *value, *part;
     int32_t *column;
     LogprobsPlan(const bdlm_dense_desc_t &d, int64_t n_top, const void *px, const void *pw, void *p)
         : skinny(few(d)), ws(p),
           x(px, skinny ? 0 : d.rows, d.in_features, d.x_stride, d.in_dtype, false, ws),
           w(pw, skinny ? 0 : d.out_features, d.in_features, d.w_stride, d.in_dtype, false, ws),
-          shape(shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), false)) {
-        const int64_t edge = skinny ? skinny_cols(d.out_features) : tile_edge(shape.big);
+          shape(shape_of(d.rows, d.out_features, steps_of(d.in_features, pairs_of(d.in_dtype)), !skinny)) {
+        joined = !skinny && shape.splits > 1;
+        const int64_t edge = skinny ? skinny_cols(d.out_features) : joined ? kJoinGroup : tile_edge(shape.big);
         ngroup = static_cast<int32_t>((d.out_features + edge - 1) / edge);
-        width = static_cast<int32_t>(n_top == 0 ? 0 : skinny ? edge : n_top);
+        width = static_cast<int32_t>(n_top == 0 ? 0 : skinny || joined ? edge : n_top);
         const int64_t records = d.rows * ngroup;
         top = ws.take<float>(records);
         others = ws.take<float>(records);
         slope = ws.take<float>(records);
         token_logit = ws.take<float>(d.rows);
         value = ws.take<float>(records * width);
-        column = ws.take<int32_t>(skinny ? 0 : records * width);
+        column = ws.take<int32_t>(skinny || joined ? 0 : records * width);
+        part = ws.take<float>(joined ? part_size(shape, d.rows, d.out_features) : 0);
     }
     bool fits() const { return skinny || shape.fits; }
 };
@@ -92,9 +96,11 @@ int bdlm_head_logprobs(const bdlm_dense_desc_t *d, const int64_t *tokens, int64_
     } else {
         TRY(lay_all(stream, p.x, p.w));
         TileArgs a = product(p.x.mat, false, p.w.mat, false, d->rows, vocab, d->in_features, pairs_of(d->in_dtype), p.shape);
-        a.out = kTileTop;
+        a.out = p.joined ? kTilePartial : kTileTop;
+        a.part = p.part;
         a.top = top;
         TRY(launch_tile(a, stream));
+        if (p.joined) TRY(launch_join_top(p.part, p.shape.splits, a.nrow, vocab, top, stream));
     }
     LogprobsArgs f{};
     f.top = p.top;
@@ -110,7 +116,7 @@ int bdlm_head_logprobs(const bdlm_dense_desc_t *d, const int64_t *tokens, int64_
     f.list = list;
     f.width = p.width;
     f.value = p.value;
-    f.column = p.skinny ? nullptr : p.column;
+    f.column = p.skinny || p.joined ? nullptr : p.column;
     f.top_token = top_token;
     f.top_logprob = top_logprob;
     return launch_logprobs(f, stream);

@@ -82,17 +82,22 @@ __device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, f32x4 bias, 
 
 // Four consecutive values to a row of bf16 or fp32, n of which there are.  Nontemporal: what a tile stores is not read again by the
 // launch, whose operands keep the L2 (the gated product of 16,384 x 1,024 x 4,096, kept: 321 us with plain stores, 313 so).
+// Four of them are one store at any alignment (one by one, 3,136 x 152 x 314, kept, took GATED314 us).
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void put4(void *dst, int64_t o, int n, bool whole, bool bf16, f32x4 v) {
+typedef u32x2 __attribute__((aligned(2))) u32x2_a2;
+__device__ __forceinline__ void put4(void *dst, int64_t o, int64_t ld, int n, bool bf16, f32x4 v) {
+    const bool past = ld % 32 == 0;
     if (bf16) {
         uint16_t *p = static_cast<uint16_t *>(dst) + o;
-        if (whole)
-            __builtin_nontemporal_store(u32x2{cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])}, reinterpret_cast<u32x2 *>(p));
+        const u32x2 u = {cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3])};
+        if (n == 4 && past) __builtin_nontemporal_store(u, reinterpret_cast<u32x2 *>(p));
+        else if (n == 4) *reinterpret_cast<u32x2_a2 *>(p) = u;
         else
             for (int e = 0; e < n; ++e) p[e] = static_cast<uint16_t>(bf16_bits(v[e]));
     } else {
         float *p = static_cast<float *>(dst) + o;
-        if (whole) __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(p));
+        if (n == 4 && past) __builtin_nontemporal_store(v, reinterpret_cast<f32x4 *>(p));
+        else if (n == 4) *reinterpret_cast<f32x4_a4 *>(p) = v;
         else
             for (int e = 0; e < n; ++e) p[e] = v[e];
     }
@@ -115,13 +120,12 @@ __device__ __forceinline__ void gated4(const GatedArgs &a, f32x4 (&gate)[N], f32
     const int n = a.n - col < 4 ? a.n - col : 4;
     if (n <= 0 || there <= 0) return;
     if (a.pre_gate) {
-        const bool whole = n == 4 && a.ld_pre % 4 == 0;
 #pragma unroll
         for (int k = 0; k < N; ++k)
             if (k < there) {
                 const int64_t o = (row + k) * a.ld_pre + col;
-                put4(a.pre_gate, o, n, whole, a.pre_bf16, gate[k]);
-                put4(a.pre_up, o, n, whole, a.pre_bf16, up[k]);
+                put4(a.pre_gate, o, a.ld_pre, n, a.pre_bf16, gate[k]);
+                put4(a.pre_up, o, a.ld_pre, n, a.pre_bf16, up[k]);
             }
     }
     if (a.act == BDLM_ACT_SILU) {
@@ -140,10 +144,25 @@ __device__ __forceinline__ void gated4(const GatedArgs &a, f32x4 (&gate)[N], f32
 #pragma unroll
             for (int e = 0; e < 4; ++e) gate[k][e] = act_value<true>(gate[k][e], BDLM_ACT_GELU);
     }
-    const bool whole = n == 4 && a.ld_out % 4 == 0;
 #pragma unroll
     for (int k = 0; k < N; ++k)
-        if (k < there) put4(a.out, (row + k) * a.ld_out + col, n, whole, a.out_bf16, gate[k] * up[k]);
+        if (k < there) put4(a.out, (row + k) * a.ld_out + col, a.ld_out, n, a.out_bf16, gate[k] * up[k]);
+}
+
+// The sum of the slices at p, four columns, at any alignment.  Four slices are asked for at a time (one after the other, 128 x 1,024 in 16
+// slices took 4 us more).
+__device__ __forceinline__ f32x4 sum_slices(const float *p, int64_t slice, int splits) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    int k = 0;
+    for (; k + 4 <= splits; k += 4) {
+        f32x4 u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const f32x4_a4 *>(p + (k + j) * slice);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v += u[j];
+    }
+    for (; k < splits; ++k) v += *reinterpret_cast<const f32x4_a4 *>(p + k * slice);
+    return v;
 }
 
 }  // namespace

@@ -75,7 +75,9 @@ struct GatedBackwardPlan {
         ldz = up(d.out_features, 64);
         plane = up(d.rows, 64) * 2 * ldz;
         const int64_t both = ldz + d.out_features;
-        sx = shape_of(d.rows, d.in_features, steps_of(d.out_features, 2 * np), true);
+        // (reading one operand across its rows costs small tiles about what reading both does: 768 x 1,024 x 832 took 37.4 us by
+        // the other figures, 34.8 so)
+        sx = shape_of(d.rows, d.in_features, steps_of(d.out_features, 2 * np), true, true);
         sw = shape_of(both, d.in_features, steps_of(d.rows, np), true, true);
         dz = ws.take<uint16_t>(grad_terms(d) * plane);
         const int64_t sums = int64_t(pack_row_blocks(static_cast<int32_t>(d.rows))) * d.out_features;

@@ -210,7 +210,7 @@ __device__ __forceinline__ void store_two(const StoreArgs &s, void *two_out, int
     const int n = ncol - c < 4 ? ncol - c : 4;
     if (n <= 0 || (r >= two_rows && r < two_at)) return;
     const bool second = r >= two_at;
-    put4(second ? two_out : s.out, (second ? r - two_at : r) * s.ld_out + c, n, n == 4 && s.ld_out % 4 == 0, s.out_bf16, v);
+    put4(second ? two_out : s.out, (second ? r - two_at : r) * s.ld_out + c, s.ld_out, n, s.out_bf16, v);
 }
 
 // Four columns of one row of a tile, in their place.
@@ -221,9 +221,9 @@ __device__ __forceinline__ void tile_quad(const TileArgs &a, f32x4 v, f32x4 bias
         store4(a.store, v, bias, r, c, a.ncol);
     } else if constexpr (OUT == kTilePartial || OUT == kTileGatedPart) {
         float *to = a.part + (int64_t(split) * (a.splits ? a.nrow : nrow) + r) * a.ncol + c;
-        if (c + 4 <= a.ncol && a.ncol % 4 == 0) {
-            if (a.add) v += *reinterpret_cast<const f32x4 *>(to);
-            *reinterpret_cast<f32x4 *>(to) = v;
+        if (c + 4 <= a.ncol) {   // (at any alignment)
+            if (a.add) v += *reinterpret_cast<const f32x4_a4 *>(to);
+            *reinterpret_cast<f32x4_a4 *>(to) = v;
         } else {
             for (int e = 0; e < 4; ++e)
                 if (c + e < a.ncol) to[e] = a.add ? to[e] + v[e] : v[e];
@@ -759,22 +759,6 @@ hipError_t launch_one(const TileArgs &a, dim3 g, hipStream_t s) {
     return hipGetLastError();
 }
 
-// The sum of the slices at p, four columns.  Four slices are asked for at a time (one after the other, 128 x 1,024 in 16
-// slices took 4 us more).
-__device__ __forceinline__ f32x4 sum_slices(const float *p, int64_t slice, int splits) {
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    int k = 0;
-    for (; k + 4 <= splits; k += 4) {
-        f32x4 u[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const f32x4 *>(p + (k + j) * slice);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v += u[j];
-    }
-    for (; k < splits; ++k) v += *reinterpret_cast<const f32x4 *>(p + k * slice);
-    return v;
-}
-
 // out = epilogue(sum of the slices), four columns per thread
 __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int splits, int edge, int nrow, int ncol,
                                                         const int32_t *nrow_dev, const float *scale, const StoreArgs s) {
@@ -787,7 +771,7 @@ __global__ void __launch_bounds__(256) bdlm_join_kernel(const float *part, int s
         const int c = static_cast<int>(x - r * quads) * 4;
         const float *p = part + r * ncol + c;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if (ncol % 4 == 0) {
+        if (c + 4 <= ncol) {
             v = sum_slices(p, slice, splits);
         } else {
             for (int k = 0; k < splits; ++k)
@@ -808,7 +792,7 @@ __global__ void __launch_bounds__(256) bdlm_join_two_kernel(const float *part, i
         const int c = static_cast<int>(x - r * quads) * 4;
         const float *p = part + r * ncol + c;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if (ncol % 4 == 0) {
+        if (c + 4 <= ncol) {
             v = sum_slices(p, slice, splits);
         } else {
             for (int k = 0; k < splits; ++k)

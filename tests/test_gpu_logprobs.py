@@ -102,11 +102,12 @@ def test_logprobs(size, dtype):
         check(got, x, w, tokens if given else None, top, exclude)
 
 
-@pytest.mark.parametrize("rows", [3, 200])
-def test_ties(rows):
+# few rows, tiles, and tiles of a split contraction whose logits are joined
+@pytest.mark.parametrize("rows,k", [(3, 64), (200, 64), (200, 1536)])
+def test_ties(rows, k):
     """Equal logits throughout a group, a tile and over several: the lowest tokens, in order."""
     import paper_2607_02805_amd as bd
-    k, n = 64, 1500
+    n = 1500
     x = torch.ones(rows, k, dtype=BF, device=DEV)
     w = torch.zeros(n, k, dtype=BF, device=DEV)
     got = bd.head_logprobs(x, w, top=16)
@@ -161,11 +162,11 @@ def test_sure_rows(dtype):
         close(got[1], torch.log1p(rest) + slope / (1 + rest), ((8 + far) * 2 + 80) * F * (slope + rest), "sure entropy")
 
 
-@pytest.mark.parametrize("rows", [4, 200])
-def test_not_finite(rows):
+@pytest.mark.parametrize("rows,k", [(4, 64), (200, 64), (200, 1536)])
+def test_not_finite(rows, k):
     """NaN and infinite logits stay in their rows; what is left of a row is listed, and then nothing."""
     import paper_2607_02805_amd as bd
-    k, n, top = 64, 300, 8
+    n, top = 300, 8
     x, w, tokens = inputs(rows, k, n, BF, 3)
     tokens[:] = 7
     clean = bd.head_logprobs(x, w, tokens, top=top)
@@ -194,10 +195,10 @@ def test_not_finite(rows):
         assert torch.equal(g, c)
 
 
-@pytest.mark.parametrize("rows", [6, 90])
-def test_layouts_streams_graphs(rows):
+@pytest.mark.parametrize("rows,k", [(6, 72), (90, 72), (90, 1000)])
+def test_layouts_streams_graphs(rows, k):
     import paper_2607_02805_amd as bd
-    k, n = 72, 900
+    n = 900
     x, w, tokens = inputs(rows, k, n, BF, 4)
     want = bd.head_logprobs(x, w, tokens, top=4, exclude=5)
     wide = torch.zeros(rows, k + 16, dtype=BF, device=DEV)

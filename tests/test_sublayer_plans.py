@@ -36,6 +36,7 @@ int launch_gated_pack(const GatedPackArgs &, void *) { return BDLM_OK; }
 int launch_colsum(const float *, int32_t, int32_t, float *, void *) { return BDLM_OK; }
 int launch_colsum2(const float *, const float *, int32_t, int32_t, float *, float *, void *) { return BDLM_OK; }
 int launch_logprobs(const LogprobsArgs &, void *) { return BDLM_OK; }
+int launch_join_top(const float *, int32_t, int32_t, int32_t, const TopArgs &, void *) { return BDLM_OK; }
 int launch_add_norm(const AddNormArgs &, void *) { return BDLM_OK; }
 int launch_add_norm_grad(const AddNormGradArgs &, void *) { return BDLM_OK; }
 int32_t add_norm_grad_blocks(int64_t rows, int64_t) { return rows > 0; }
@@ -111,14 +112,14 @@ GRAD_SIZES = {
     (1000, 64, 70): {(PARTIAL, 128, 4, True, 3)},
     (20, 64, 260): {(PARTIAL, 128, 4, True, 1)},
     (20000, 64, 4100): {(PARTIAL, 128, 2, True, 3)},
-    (4500, 192, 4100): {(PARTIAL, 256, 2, True, 3)},
-    (20000, 192, 2048): {(PARTIAL, 256, 2, True, 1)},
-    (20000, 192, 70): {(TWO, 128, 2, False, 1)},
-    (4500, 2048, 70): {(TWO, 256, 2, False, 1)},
-    (20, 4096, 12000): {(PARTIAL, 128, 2, True, 1)},
+    (4500, 192, 4100): {(PARTIAL, 256, 2, True, 3), (PARTIAL, 256, 2, True, 1)},
+    (4500, 1600, 70): {(TWO, 128, 2, False, 1)},
+    (20000, 192, 70): {(TWO, 256, 2, False, 1)},
+    (20, 4096, 5300): {(PARTIAL, 128, 2, True, 1)},
 }
 TOP_SIZES = {(20, 64, 70): {(TOP, 0, 0, False, 0)}, (40, 64, 70): {(TOP, 128, 4, False, 0)}, (300, 64, 12000): {(TOP, 128, 2, False, 0)},
-             (2000, 64, 4100): {(TOP, 256, 2, False, 0)}}
+             (2000, 64, 4100): {(TOP, 256, 2, False, 0)},
+             (40, 1600, 1100): {(PARTIAL, 128, 4, True, 0)}, (1000, 4096, 4101): {(PARTIAL, 256, 2, True, 0)}}
 
 
 def kinds(got):
