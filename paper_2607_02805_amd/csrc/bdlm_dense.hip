@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(256) bdlm_pack_some_kernel(const PackSome p) {
 // a time leave too few waves: 179.)
 constexpr int64_t kPackWide = 2048;   // workgroups
 template <int WAVES, bool DH16, bool PRE16, int TERMS>
-__global__ void __launch_bounds__(64 * WAVES) bdlm_gated_pack_kernel(const GatedPackArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, TERMS == 1 ? 4 : 1) bdlm_gated_pack_kernel(const GatedPackArgs a) {
     constexpr int kBatch = 2;
     __shared__ float sums[2][WAVES][64 * 8];
     static_assert(kPackRows % (kBatch * WAVES) == 0, "whole turns");
@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(64 * WAVES) bdlm_gated_pack_kernel(const Gated
                         store_terms<TERMS>(a.dst + r * 2 * a.ldz + c, a.plane, f[0]);
                         store_terms<TERMS>(a.dst + r * 2 * a.ldz + a.ldz + c, a.plane, f[1]);
                     }
+                    __builtin_amdgcn_sched_barrier(0);   // (one row's values in registers at a time)
                 }
             }
         }
