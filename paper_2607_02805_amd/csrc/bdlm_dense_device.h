@@ -18,7 +18,7 @@ typedef f32x4 __attribute__((aligned(4))) f32x4_a4;
 // Eight consecutive elements of a row as they lie, zeros past the n that there are.  The last ones of a row are loaded with
 // those before them in the row (`before` of which there are) and moved down by settle(), which every load is followed by before
 // its values are used: several rows' loads are on their way then.  (Taken one by one, each row's end was waited for: laying out
-// 8,192 rows of 397 took 8.5 us instead of EIGHTUS.)
+// 8,192 rows of 397 took 8.5 us instead of 6.1.)
 template <bool BF16>
 struct Eight {
     u32x4 u[BF16 ? 1 : 2];

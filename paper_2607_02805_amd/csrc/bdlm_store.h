@@ -82,7 +82,8 @@ __device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, f32x4 bias, 
 
 // Four consecutive values to a row of bf16 or fp32, n of which there are.  Nontemporal: what a tile stores is not read again by the
 // launch, whose operands keep the L2 (the gated product of 16,384 x 1,024 x 4,096, kept: 321 us with plain stores, 313 so).
-// Four of them are one store at any alignment (one by one, 3,136 x 152 x 314, kept, took GATED314 us).
+// Four of them are one store at any alignment (one by one, 3,136 x 152 x 314, kept, took 18.2 us instead of 14.9), but not past
+// the caches where rows are not whole cache lines: 3,279 x 448 x 1,934, kept, took 47.5 us so, 28.8 with plain stores.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 __attribute__((aligned(2))) u32x2_a2;
 __device__ __forceinline__ void put4(void *dst, int64_t o, int64_t ld, int n, bool bf16, f32x4 v) {
