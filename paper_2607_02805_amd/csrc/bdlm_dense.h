@@ -114,18 +114,20 @@ struct TileArgs {
     int32_t add;                       // kTilePartial: add onto the slices
     float *part;                       // [splits][nrow][ncol]; splits 0: [split_count][nrow counted][ncol]
     int32_t out;                       // TileOut
-    StoreArgs store;
-    BestArgs best;
-    ProbArgs prob;
+    union {                            // (what `out` says: the arguments of a launch stay few)
+        StoreArgs store;               // kTileStore, kTileTwo
+        BestArgs best;
+        ProbArgs prob;
+        GatedArgs gated;               // kTileGated, kTileGatedPart
+        TopArgs top;
+    };
     // Pairs from `half` on are of the operands' second parts, that many elements further: dz of up beside dz of gate, times
     // w_up after w_gate (half = npair: there are none).  kTileGated: col_duo from w_gate to w_up.
     int32_t half;
     int64_t row_duo, col_duo;
-    GatedArgs gated;
     // kTileTwo: rows below two_rows are store's, those from two_at on go to two_out from its row 0 on (same stride).
     void *two_out;
     int32_t two_rows, two_at;
-    TopArgs top;                       // kTileTop
 };
 int launch_tile(const TileArgs &a, void *stream);
 constexpr int32_t kChip = 256;   // workgroups of large tiles that run at once
@@ -163,11 +165,13 @@ struct SkinnyArgs {
     const int32_t *nrow_dev, *row_of;  // the rows that count: how many, and row r's row of x (null: all)
     int32_t bf16;
     int32_t out;
-    StoreArgs store;
-    BestArgs best;
-    TopArgs top;                       // kTileTop
     const void *w2;                    // kTileGated: w_up, w being w_gate (ncol columns each)
-    GatedArgs gated;
+    union {                            // as TileArgs has them
+        StoreArgs store;
+        BestArgs best;
+        GatedArgs gated;
+        TopArgs top;
+    };
 };
 // Above that many rows the tiles are faster: over 50,257 columns of 1,024 in bf16, 32 rows take 34
 // us here and 29 there, 64 rows 54 and 34, but over 4,384 of them 32 rows take 9 and 11; in fp32,

@@ -98,7 +98,7 @@ int bdlm_head_logprobs(const bdlm_dense_desc_t *d, const int64_t *tokens, int64_
         TileArgs a = product(p.x.mat, false, p.w.mat, false, d->rows, vocab, d->in_features, pairs_of(d->in_dtype), p.shape);
         a.out = p.joined ? kTilePartial : kTileTop;
         a.part = p.part;
-        a.top = top;
+        if (!p.joined) a.top = top;
         TRY(launch_tile(a, stream));
         if (p.joined) TRY(launch_join_top(p.part, p.shape.splits, a.nrow, vocab, top, stream));
     }

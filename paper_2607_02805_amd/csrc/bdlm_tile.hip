@@ -497,8 +497,16 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
         int left, skip;
     };
     int pair = it0 > 0 ? it0 / nkt : 0, kt = it0 - pair * nkt;
-    auto col_at = [&](int i) { return i < a.half ? col_term(a.half, i) * a.col.plane : a.col_duo + col_term(a.half, i - a.half) * a.col.plane; };
-    auto row_at = [&](int i) { return i < a.half ? row_term(a.half, i) * a.row.plane : a.row_duo + row_term(a.half, i - a.half) * a.row.plane; };
+    // (second parts are met in a product over both factors of a gated one alone: the other kernels do without the choice)
+    constexpr bool kParts = COLT && !ROWT && (OUT == kTilePartial || OUT == kTileTwo);
+    auto col_at = [&](int i) {
+        if (kParts && i >= a.half) return a.col_duo + col_term(a.half, i - a.half) * a.col.plane;
+        return col_term(kParts ? a.half : a.npair, i) * a.col.plane;
+    };
+    auto row_at = [&](int i) {
+        if (kParts && i >= a.half) return a.row_duo + row_term(a.half, i - a.half) * a.row.plane;
+        return row_term(kParts ? a.half : a.npair, i) * a.row.plane;
+    };
     From next{sc.at_step(col_at(pair), kt), sr.at_step(row_at(pair), kt), K - kt * kDepth, a.skip - kt * kDepth};
     auto advance = [&]() {   // (past the last stage: to addresses that are not read)
         next = From{next.c + sc.stride(), next.r + sr.stride(), next.left - kDepth, next.skip - kDepth};
