@@ -121,9 +121,10 @@ __global__ void __launch_bounds__(256) bdlm_pack_some_kernel(const PackSome p) {
 // kPackRows rows of 64 x 8 columns, a thread eight columns of two rows at a time, and writes both parts.  With eight waves each
 // waits for memory once: with four, which take two turns, 768 x 832 takes 10 us instead of 7.5; where there are workgroups
 // for more than a round of the chip four are better, 113 us for 16,384 x 4,096 instead of 124 (kPackWide).  (Four rows a thread at
-// a time leave too few waves: 179.)
+// a time leave too few waves: 179.)  WHOLE: widths of whole eights, which need fewer registers (16,384 x 1,024 x 4,096 with its products
+// 614 us, 631 without the distinction).
 constexpr int64_t kPackWide = 2048;   // workgroups
-template <int WAVES, bool DH16, bool PRE16, int TERMS>
+template <int WAVES, bool DH16, bool PRE16, int TERMS, bool WHOLE>
 __global__ void __launch_bounds__(64 * WAVES, TERMS == 1 ? 4 : 1) bdlm_gated_pack_kernel(const GatedPackArgs a) {
     constexpr int kBatch = 2;
     __shared__ float sums[2][WAVES][64 * 8];
@@ -139,8 +140,8 @@ __global__ void __launch_bounds__(64 * WAVES, TERMS == 1 ? 4 : 1) bdlm_gated_pac
         float sum[2][8] = {};
         if (c < a.ldz) {
             for (int64_t q = r0 + wave; q < r0 + kPackRows && q < rows_up; q += WAVES * kBatch) {
-                Eight<DH16> dh[kBatch];
-                Eight<PRE16> gate[kBatch], up[kBatch];
+                Eight<DH16, WHOLE> dh[kBatch];
+                Eight<PRE16, WHOLE> gate[kBatch], up[kBatch];
 #pragma unroll
                 for (int k = 0; k < kBatch; ++k) {
                     const int64_t r = q + WAVES * k;
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(64 * WAVES, TERMS == 1 ? 4 : 1) bdlm_gated_pac
                     for (int e = 0; e < 8; ++e) {
                         float value, slope;
                         act_both<!PRE16>(gate[k].value(e), a.act, value, slope);
-                        const bool here = e < n;   // (a slope of no column is not 0)
+                        const bool here = WHOLE ? n > 0 : e < n;   // (a slope of no column is not 0)
                         f[0][e] = here ? dh[k].value(e) * up[k].value(e) * slope : 0.f;
                         f[1][e] = here ? dh[k].value(e) * value : 0.f;
                         sum[0][e] += f[0][e];
@@ -352,13 +353,18 @@ int launch_pack(const PackArgs &a, void *stream) {
     return done();
 }
 
-template <bool DH16, bool PRE16, int TERMS>
-int gated_pack_of(const GatedPackArgs &a, hipStream_t s) {
+template <bool DH16, bool PRE16, int TERMS, bool WHOLE>
+int gated_pack_as(const GatedPackArgs &a, hipStream_t s) {
     const int64_t blocks = (a.ldz + 511) / 512 * pack_row_blocks(a.rows);
     const dim3 g(static_cast<unsigned>(blocks < (int64_t(1) << 22) ? blocks : int64_t(1) << 22));
-    if (blocks > kPackWide) hipLaunchKernelGGL((bdlm_gated_pack_kernel<4, DH16, PRE16, TERMS>), g, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((bdlm_gated_pack_kernel<8, DH16, PRE16, TERMS>), g, dim3(512), 0, s, a);
+    if (blocks > kPackWide) hipLaunchKernelGGL((bdlm_gated_pack_kernel<4, DH16, PRE16, TERMS, WHOLE>), g, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((bdlm_gated_pack_kernel<8, DH16, PRE16, TERMS, WHOLE>), g, dim3(512), 0, s, a);
     return done();
+}
+
+template <bool DH16, bool PRE16, int TERMS>
+int gated_pack_of(const GatedPackArgs &a, hipStream_t s) {
+    return a.n % 8 == 0 ? gated_pack_as<DH16, PRE16, TERMS, true>(a, s) : gated_pack_as<DH16, PRE16, TERMS, false>(a, s);
 }
 
 int launch_gated_pack(const GatedPackArgs &a, void *stream) {

@@ -19,13 +19,14 @@ typedef f32x4 __attribute__((aligned(4))) f32x4_a4;
 // those before them in the row (`before` of which there are) and moved down by settle(), which every load is followed by before
 // its values are used: several rows' loads are on their way then.  (Taken one by one, each row's end was waited for: laying out
 // 8,192 rows of 397 took 8.5 us instead of 6.1.)
-template <bool BF16>
+// WHOLE: rows of whole eights, which have no such ends.
+template <bool BF16, bool WHOLE = false>
 struct Eight {
     u32x4 u[BF16 ? 1 : 2];
     int cut;
     __device__ __forceinline__ void load(const void *src, int64_t at, int n, int before) {
         cut = 0;
-        if (n > 0 && n < 8) {
+        if (!WHOLE && n > 0 && n < 8) {
             if (n + before < 8) {   // a row of fewer than eight
                 uint32_t h[8];
 #pragma unroll
@@ -56,7 +57,7 @@ struct Eight {
     }
     // Moves the elements down by `cut`, zeros after them.
     __device__ __forceinline__ void settle() {
-        if (cut == 0) return;
+        if (WHOLE || cut == 0) return;
         if constexpr (BF16) {
             uint64_t lo = u[0][0] | uint64_t(u[0][1]) << 32, hi = u[0][2] | uint64_t(u[0][3]) << 32;
             if (cut & 4) lo = hi, hi = 0;

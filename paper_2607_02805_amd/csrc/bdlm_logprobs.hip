@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(256) bdlm_join_top_kernel(const float *part, i
 }
 
 constexpr int kParts = 64;         // of the groups
+static_assert(BDLM_MAX_TOP <= kParts, "as many parts as values");
 constexpr int kRoom = 256;         // gathered groups, and values
 
 // A gathered value.
