@@ -1158,11 +1158,27 @@ def _two_weights(x, w_gate, w_up):
     return d, lead
 
 
+def _apart(shape, x):
+    """Two new tensors like x that are written together with a third.  Large ones start 1 and 2 KiB past where tensors start, so
+    that the same element of the three does not lie in the same bank of memory (a gated product of 16,384 x 1,024 x 4,096 takes 303
+    us with them and 340 with tensors that start alike)."""
+    torch = _torch()
+    n = 1
+    for v in shape:
+        n *= v
+    size, skip = x.element_size(), 1024 // x.element_size()
+    if n * size < 1 << 20:
+        return tuple(torch.empty(shape, dtype=x.dtype, device=x.device) for _ in range(2))
+    up = (n + skip - 1) // skip * skip
+    both = torch.empty(2 * up + 2 * skip, dtype=x.dtype, device=x.device)
+    return both[skip:skip + n].view(shape), both[2 * skip + up:2 * skip + up + n].view(shape)
+
+
 def _pair(t, d, lead, x, what: str):
     """Two tensors [..., out_features] in x's type at one row stride, new ones for True; and the stride."""
     shape = (*lead, d.out_features)
     if t is True:
-        t = tuple(_torch().empty(shape, dtype=x.dtype, device=x.device) for _ in range(2))
+        t = _apart(shape, x)
     if not isinstance(t, (tuple, list)) or len(t) != 2:
         raise ValueError(f"{what} must be two tensors")
     for v in t:

@@ -19,6 +19,7 @@
 #include <Python.h>
 
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/ops/as_strided.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
@@ -675,8 +676,21 @@ struct Two {
     Two(PyObject *o, const Dense &t, int64_t cols) {
         const auto full = t.shape(cols);
         if (o == Py_True) {
-            a = t.output(Py_True, full, t.type);
-            b = t.output(Py_True, full, t.type);
+            // large ones past where tensors start, as the Python code has them (_apart)
+            int64_t n = 1;
+            for (const int64_t v : full) n *= v;
+            const int64_t size = t.x.element_size(), skip = 1024 / size, up = (n + skip - 1) / skip * skip;
+            if (n * size < (int64_t(1) << 20)) {
+                a = t.output(Py_True, full, t.type);
+                b = t.output(Py_True, full, t.type);
+            } else {
+                c10::SmallVector<int64_t, 5> strides(full.size(), 1);
+                for (size_t i = full.size() - 1; i > 0; --i) strides[i - 1] = strides[i] * full[i];
+                const at::Tensor both = t.output(Py_True, {2 * up + 2 * skip}, t.type);
+                const Unlocked u;
+                a = at::as_strided(both, full, strides, skip);
+                b = at::as_strided(both, full, strides, 2 * skip + up);
+            }
         } else {
             need(PyTuple_CheckExact(o) && PyTuple_GET_SIZE(o) == 2);
             a = t.output(PyTuple_GET_ITEM(o, 0), full, t.type);

@@ -697,6 +697,25 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             const int most = static_cast<int>(rows_out - row0) - r1;
             // (rows eight apart in a pass: their quads lie in both halves of the banks)
             constexpr int kBatch = 4;
+            // Of large tiles, what is kept goes first, one matrix after the other: at sizes of a power of two the three lie at the same places of
+            // memory's banks, and stores to them in turn wait for each other (16,384 x 1,024 x 4,096 took 374 us so, 340 one by one, and
+            // 303 where they lie 1 KiB further from each other, as the binding allocates them, and 306 one by one; small tiles read
+            // LDS once: 1,000 x 832 x 2,048 took 13.2 us, 13.9 one by one).
+            constexpr bool kFirst = KS == 1;
+            if (kFirst && a.gated.pre_gate) {
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {
+#pragma unroll
+                    for (int k = 0; k < 8 / KS; ++k) {
+                        const int x = half * (8 / KS) + k + 8 * gate_sub;
+                        const f32x4 v = mine[x * kQuads + ((gate_quad + 8 * which) ^ (x & 15))] + (which ? bias_up : bias);
+                        const int n = a.gated.n - gate_col < 4 ? a.gated.n - gate_col : 4;
+                        if (x < most && n > 0)
+                            put4(which ? a.gated.pre_up : a.gated.pre_gate, (row0 + r1 + x) * a.gated.ld_pre + gate_col, a.gated.ld_pre, n,
+                                 a.gated.pre_bf16, v);
+                    }
+                }
+            }
 #pragma unroll
             for (int k0 = 0; k0 < 8 / KS; k0 += kBatch) {
                 f32x4 gate[kBatch], up[kBatch];
@@ -707,7 +726,7 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
                     gate[k] = from[gate_quad ^ ((x0 + k) & 15)] + bias;
                     up[k] = from[(gate_quad + 8) ^ ((x0 + k) & 15)] + bias_up;
                 }
-                gated4(a.gated, gate, up, row0 + r1 + x0, most - x0, gate_col);
+                gated4<!kFirst>(a.gated, gate, up, row0 + r1 + x0, most - x0, gate_col);
             }
         } else if constexpr (OUT == kTileTwo) {
             // (four rows' reads, then their stores)
@@ -820,7 +839,7 @@ __global__ void __launch_bounds__(256) bdlm_join_gated_kernel(const float *part,
         const float *p = part + r * ncol + (c >> 5) * 64 + (c & 31);
         const f32x4 gate = sum_slices(p, slice, splits), up = sum_slices(p + 32, slice, splits);
         f32x4 both[2][1] = {{gate + gated_bias(g.bias_gate, c, g.n)}, {up + gated_bias(g.bias_up, c, g.n)}};
-        gated4(g, both[0], both[1], r, 1, c);
+        gated4<true>(g, both[0], both[1], r, 1, c);
     }
 }
 

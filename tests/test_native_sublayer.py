@@ -94,6 +94,28 @@ def test_native_and_python_marshalling_agree(monkeypatch, name, dtype):
             assert torch.equal(a.view(torch.uint8) if a.dtype == E4 else a, b.view(torch.uint8) if b.dtype == E4 else b)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(40, 64, 4099), (2048, 64, 520)])
+def test_large_products_that_are_kept_start_apart(monkeypatch, size):
+    """From 1 MiB on: contiguous, apart from each other, at the same places from either side, and what small calls give."""
+    m, k, n = size
+    g = torch.Generator().manual_seed(2)
+    x, wg, wu = (torch.randn(*s, generator=g).cuda() for s in ((m, k), (n, k), (n, k)))
+    got = []
+    for native in (bd._native(), _Absent()):
+        monkeypatch.setattr(bd, "_marshal", native)
+        out, (gate, up) = bd.gated_projection(x, wg, wu, pre=True)
+        assert gate.is_contiguous() and up.is_contiguous() and gate.shape == up.shape == (m, n)
+        large = gate.numel() * 4 >= 1 << 20
+        assert (gate.storage_offset(), gate.untyped_storage().data_ptr() == up.untyped_storage().data_ptr()) == (256 * large, large)
+        assert not large or up.data_ptr() - gate.data_ptr() >= gate.numel() * 4 + 1024
+        got.append((out, gate, up, up.storage_offset()))
+    assert all(torch.equal(a, b) for a, b in zip(*[v[:3] for v in got])) and got[0][3] == got[1][3]
+    out, pre = torch.empty(m, n).cuda(), (torch.empty(m, n).cuda(), torch.empty(m, n).cuda())
+    bd.gated_projection(x, wg, wu, out=out, pre=pre)
+    assert all(torch.equal(a, b) for a, b in zip((out, *pre), got[0][:3]))
+
+
 @pytest.mark.parametrize("name", NAMES)
 def test_tensors_off_the_gpu_are_refused_as_before(monkeypatch, name):
     native = _Counting(bd._native())
