@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(BF16 ? 1024 : 512) bdlm_skinny_kernel(const Sk
                 gate[0] += *reinterpret_cast<const f32x4 *>(p);
                 up[0] += *reinterpret_cast<const f32x4 *>(p + 16);
             }
-            gated4<true>(a.gated, gate, up, r, nrow - r, col0 + c);
+            gated4(a.gated, gate, up, r, nrow - r, col0 + c);
         }
         return;
     }

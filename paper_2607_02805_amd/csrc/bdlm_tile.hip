@@ -699,10 +699,13 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             constexpr int kBatch = 4;
             // Of large tiles, what is kept goes first, one matrix after the other: at sizes of a power of two the three lie at the same places of
             // memory's banks, and stores to them in turn wait for each other (16,384 x 1,024 x 4,096 took 374 us so, 340 one by one, and
-            // 303 where they lie 1 KiB further from each other, as the binding allocates them, and 306 one by one; small tiles read
-            // LDS once: 1,000 x 832 x 2,048 took 13.2 us, 13.9 one by one).
-            constexpr bool kFirst = KS == 1;
-            if (kFirst && a.gated.pre_gate) {
+            // 303 where they lie 1 KiB further from each other, as the binding allocates them, and 306 one by one).
+            // Rows of other lengths do not meet so and read LDS once: 3,279 x 448 x 1,934 takes 27.4 us, 29.8 one by one, and small
+            // tiles 1,000 x 832 x 2,048 13.2 and 13.9.
+            const bool first = KS == 1 && a.gated.pre_gate && a.gated.ld_pre % 512 == 0;
+            GatedArgs g = a.gated;
+            if (first) g.pre_gate = nullptr;
+            if (first) {
 #pragma unroll
                 for (int which = 0; which < 2; ++which) {
 #pragma unroll
@@ -726,7 +729,7 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
                     gate[k] = from[gate_quad ^ ((x0 + k) & 15)] + bias;
                     up[k] = from[(gate_quad + 8) ^ ((x0 + k) & 15)] + bias_up;
                 }
-                gated4<!kFirst>(a.gated, gate, up, row0 + r1 + x0, most - x0, gate_col);
+                gated4(g, gate, up, row0 + r1 + x0, most - x0, gate_col);
             }
         } else if constexpr (OUT == kTileTwo) {
             // (four rows' reads, then their stores)
@@ -839,7 +842,7 @@ __global__ void __launch_bounds__(256) bdlm_join_gated_kernel(const float *part,
         const float *p = part + r * ncol + (c >> 5) * 64 + (c & 31);
         const f32x4 gate = sum_slices(p, slice, splits), up = sum_slices(p + 32, slice, splits);
         f32x4 both[2][1] = {{gate + gated_bias(g.bias_gate, c, g.n)}, {up + gated_bias(g.bias_up, c, g.n)}};
-        gated4<true>(g, both[0], both[1], r, 1, c);
+        gated4(g, both[0], both[1], r, 1, c);
     }
 }
 

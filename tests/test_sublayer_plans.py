@@ -102,6 +102,7 @@ GATED_SIZES = {
     (40, 64, 30000): {(GATED, 128, 2, False, 0)},
     (40, 64, 70): {(GATED, 128, 4, False, 0)},
     (300, 64, 12000): {(GATED, 256, 2, False, 0)},
+    (4096, 128, 2048): {(GATED, 256, 2, False, 0)},        # rows of a multiple of 512, which are stored one matrix after the other
     (40, 1600, 70): {(GATED_PART, 128, 4, True, 0)},
     (20000, 4096, 70): {(GATED_PART, 256, 2, True, 0)},
 }
