@@ -438,7 +438,8 @@ int bdlm_gated_rmsnorm(int64_t batch, int64_t len, int64_t nheads, int64_t ngrou
  * its root mean square, per row of `width` columns:
  *     s = x + residual,   out = norm_w * s / sqrt(mean s^2 + eps).
  * s is formed in fp32 and normalised unrounded (squares may leave fp32's range, s itself may not: an infinity or NaN
- * makes its row's norm 0 or NaN, as the formula says).
+ * makes its row's norm 0 or NaN, as the formula says).  1 / sqrt(mean s^2 + eps) has to be an fp32 number too: with eps 0
+ * it overflows for a root mean square below 2^-128, and such a row's norm is infinite or NaN.
  * x            device [rows][width], x_dtype; residual residual_dtype, or NULL (s = x); row strides in elements, which
  *              may be 0 or overlap.
  * sum          s in residual_dtype (what the gradient takes), or NULL; may be residual (same stride).
