@@ -10,6 +10,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "bdlm.h"
 #include "bdlm_dense.h"
 #include "bdlm_dense_device.h"
@@ -484,6 +486,16 @@ Way way_of(int64_t width) {
     return {4, width <= 8192 ? 4 : 0};
 }
 constexpr int64_t kMostGroups = 2048;   // workgroups of the forward call: eight on a CU
+constexpr int64_t kMostGradGroups = 512;   // of the gradient, each with a row of sums of dw
+// Of the gradient without dw, which every turn of rows can have a workgroup for (16 rows of 1,024: 3.9 us, 8.5 in one workgroup) and
+// which has no sums: 16,384 x 2,048 in bf16 takes 35 us so and 50 with 512, 4,000 x 2,048 12.7 and 16.5, 2,000 x 8,192 38 and 34, 45 with 2,048.
+constexpr int64_t kMostStreamGroups = 1024;
+
+// Turns of rows of a gradient's workgroup.
+int64_t grad_groups(int64_t rows, int64_t width) {
+    const int64_t per = kWaves / way_of(width).waves;
+    return (rows + per - 1) / per;
+}
 
 int done() { return hipGetLastError() == hipSuccess ? BDLM_OK : BDLM_E_LAUNCH; }
 
@@ -503,7 +515,8 @@ int norm_of(const AddNormArgs &a, hipStream_t s) {
 template <bool Y16, bool S16>
 int grad_of(const AddNormGradArgs &a, hipStream_t s) {
     const Way y = way_of(a.width);
-    const dim3 g(static_cast<unsigned>(add_norm_grad_blocks(a.rows, a.width))), b(64 * kWaves);
+    const int64_t groups = a.part ? add_norm_grad_blocks(a.rows, a.width) : std::min(grad_groups(a.rows, a.width), kMostStreamGroups);
+    const dim3 g(static_cast<unsigned>(groups)), b(64 * kWaves);
     if (y.waves == 1 && y.pieces == 1) hipLaunchKernelGGL((bdlm_add_rmsnorm_grad_kernel<1, 1, Y16, S16>), g, b, 0, s, a);
     else if (y.waves == 1) hipLaunchKernelGGL((bdlm_add_rmsnorm_grad_kernel<1, 2, Y16, S16>), g, b, 0, s, a);
     else if (y.pieces == 1) hipLaunchKernelGGL((bdlm_add_rmsnorm_grad_kernel<4, 1, Y16, S16>), g, b, 0, s, a);
@@ -516,10 +529,11 @@ int grad_of(const AddNormGradArgs &a, hipStream_t s) {
 }  // namespace
 
 int32_t add_norm_grad_blocks(int64_t rows, int64_t width) {
-    // One workgroup takes four turns of rows, whose dw needs no second launch (13 rows of 97 columns: 9.3 us in two launches,
-    // 6 in one).
-    const int64_t per = kWaves / way_of(width).waves, groups = (rows + per - 1) / per;
-    return static_cast<int32_t>(groups <= 4 ? (groups > 0 ? 1 : 0) : groups < 512 ? groups : 512);
+    // Two turns of rows of up to 4,096 columns are one workgroup's, whose dw needs no second launch: 8 rows of 448 columns take 4.1 us
+    // so and 5.1 in two launches, 8 of 1,024 5.8 and 6.2, 2 of 4,096 6.0 and 6.4.  Past that the turns one after the other cost more
+    // than the launch: 2 rows of 8,192 take 9.5 and 8.7, three turns 12 of 1,024 7.4 and 6.2, 4 rows of 32,768 93 and 26.
+    const int64_t groups = grad_groups(rows, width);
+    return static_cast<int32_t>(groups <= (width <= 4096 ? 2 : 1) ? (groups > 0 ? 1 : 0) : std::min(groups, kMostGradGroups));
 }
 
 int launch_add_norm(const AddNormArgs &a, void *stream) {

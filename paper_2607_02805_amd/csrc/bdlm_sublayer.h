@@ -38,7 +38,7 @@ struct AddNormGradArgs {
     float eps;
 };
 int launch_add_norm_grad(const AddNormGradArgs &a, void *stream);
-// Workgroups of the gradient, each with a row of partial sums of dw.
+// Workgroups of the gradient with dw, each with a row of partial sums of it.
 int32_t add_norm_grad_blocks(int64_t rows, int64_t width);
 
 }  // namespace bdlm
