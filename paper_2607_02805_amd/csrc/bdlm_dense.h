@@ -157,7 +157,7 @@ int launch_join_two(const float *part, int32_t splits, int32_t nrow, int32_t nco
 int launch_join_gated(const float *part, int32_t splits, int32_t nrow, const GatedArgs &g, void *stream);
 
 // Few rows (skinny_rows): the weights stream through once.  x [nrow][k], w [ncol][k], both bf16
-// or both fp32, any stride; out kTileStore or kTileBest (one record per skinny_cols columns).
+// or both fp32, any stride; out kTileStore, kTileBest or kTileTop (one record per skinny_cols columns), or kTileGated.
 struct SkinnyArgs {
     const void *x, *w;
     int64_t ldx, ldw;

@@ -215,20 +215,6 @@ __device__ __forceinline__ Best merge(const Best &a, const Best &b) {
 struct Spread {
     float top, others, slope;
 };
-__device__ __forceinline__ Spread merge(const Spread &a, const Spread &b) {
-    const bool second = b.top > a.top;
-    const Spread &hi = second ? b : a;
-    const Spread &lo = second ? a : b;
-    const float f = share(lo.top, hi.top);   // 0 for a lower record that holds nothing
-    Spread r = hi;
-    if (f != 0.f) {
-        r.others = fmaf(1.f + lo.others, f, hi.others);
-        r.slope = fmaf(fmaf(lo.top - hi.top, 1.f + lo.others, lo.slope), f, hi.slope);
-    } else if (lo.others != lo.others) {     // a NaN stays one
-        r.others = r.slope = lo.others;
-    }
-    return r;
-}
 // exp(d) d of a value's own exp(d) = s: 0 where d is -infinity
 __device__ __forceinline__ float slope_of(float s, float d) { return s * fmaxf(d, -1e30f); }
 

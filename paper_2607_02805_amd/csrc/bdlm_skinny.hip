@@ -249,12 +249,16 @@ hipError_t launch_cols_of(const SkinnyArgs &a, hipStream_t s) {
     constexpr int kMost = BF16 ? 16 : 8, kRoom = 32 / (MT * G);   // registers; LDS
     constexpr int most = kMost < kRoom ? kMost : kRoom;
     waves = waves < 1 ? 1 : waves > most ? most : waves;
-    const int across = a.out == kTileGated ? 16 : 16 * G;
+    const int across = G == 2 && a.out == kTileGated ? 16 : 16 * G;
     const dim3 g((a.ncol + across - 1) / across), blk(64 * waves);
     const size_t lds = size_t(waves) * 16 * MT * (16 * G + 4) * 4;   // at most 40 KB
+    if constexpr (G == 2)   // (a group of either matrix)
+        if (a.out == kTileGated) {
+            hipLaunchKernelGGL((bdlm_skinny_kernel<MT, 2, BF16, kTileGated>), g, blk, lds, s, a);
+            return hipGetLastError();
+        }
     if (a.out == kTileStore) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileStore>), g, blk, lds, s, a);
     else if (a.out == kTileTop) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileTop>), g, blk, lds, s, a);
-    else if (a.out == kTileGated) hipLaunchKernelGGL((bdlm_skinny_kernel<MT, 2, BF16, kTileGated>), g, blk, lds, s, a);
     else hipLaunchKernelGGL((bdlm_skinny_kernel<MT, G, BF16, kTileBest>), g, blk, lds, s, a);
     return hipGetLastError();
 }
