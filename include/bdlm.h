@@ -563,6 +563,8 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t
  * bias_gate, bias_up  device fp32 [out_features], each or NULL.
  * out          device [rows][out_features], out_dtype; formed from the unrounded gate and up.
  * pre_gate, pre_up    gate and up, device [rows][out_features], in_dtype, at one stride, both or neither: kept for the gradient.
+ *              Where out, pre_gate and pre_up start at the same place modulo the memory's banks and rows are a multiple of 512 elements,
+ *              storing them takes longer: 16,384 x 1,024 x 4,096 in bf16 340 us, and 307 where each starts 1 KiB further than the one before.
  * Up to 32 rows (fp32: 64) need no workspace.
  * Errors: as bdlm_projection.  rows == 0 enqueues nothing.
  */

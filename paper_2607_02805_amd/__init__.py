@@ -1199,6 +1199,10 @@ def gated_projection(x, w_gate, w_up, bias_gate=None, bias_up=None, act="silu", 
     float32) is [..., out_features].  ``pre`` keeps both products with their biases in x's dtype for the gradient: None
     (no), True (allocate) or two tensors at one row stride.  Returns out, or (out, (gate, up)) if ``pre`` was asked for.
 
+    From 1 MiB each on, the two that ``pre=True`` allocates are contiguous views of one storage, 1 KiB and 2 KiB past where tensors
+    start: their memory is freed when both are gone, a saved one takes the other along, and they share a version counter.
+    Two tensors of the caller's own have none of this (for the time that their places cost see ``include/bdlm.h``).
+
     No autograd graph is recorded: :func:`gated_projection_backward` has the gradients."""
     if stream is not None:
         with _on(stream, x):

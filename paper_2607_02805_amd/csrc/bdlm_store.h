@@ -80,8 +80,15 @@ __device__ __forceinline__ void store4(const StoreArgs &s, f32x4 v, f32x4 bias, 
     }
 }
 
-// Four consecutive values to a row of bf16 or fp32, n of which there are.  Nontemporal: what a tile stores is not read again by the
-// launch, whose operands keep the L2 (the gated product of 16,384 x 1,024 x 4,096, kept: 321 us with plain stores, 313 so).
+// Four consecutive values to a row of bf16 or fp32, n of which there are.  Nontemporal: the launch does not read again what a tile
+// stores, and its operands keep the L2.  1,024 x 4,096 in bf16, with plain stores and so, and together with the projection to 1,024
+// that reads the output next:
+//   16,384 rows   gated 281 and 261 us, kept 330 and 308   with the projection 424 and 412, kept 506 and 461
+//    2,048 rows          35.3 and 33.8       42.0 and 40.3                       66.0 and 66.5       73.8 and 73.1
+//      512 rows          14.7 and 14.5       16.5 and 15.2                       30.6 and 31.6       32.7 and 32.6
+//       32 rows           6.9 and  7.2        7.3 and  7.5                       20.8 and 21.3       21.2 and 21.8
+// Gradients gain 1 to 5 % (64 rows 35.6 and 34.0, 512 49 and 47, 16,384 623 and 618).  One rule for every size costs calls of few rows up to
+// 4 % of themselves and 3 % of the pair, where the output would have stayed in the caches for its reader.
 // Four of them are one store at any alignment (one by one, 3,136 x 152 x 314, kept, took 18.2 us instead of 14.9), but not past
 // the caches where rows are not whole cache lines: 3,279 x 448 x 1,934, kept, took 47.5 us so, 28.8 with plain stores.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
