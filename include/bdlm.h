@@ -448,6 +448,7 @@ int bdlm_gated_rmsnorm(int64_t batch, int64_t len, int64_t nheads, int64_t ngrou
  * scale        BDLM_DTYPE_E4M3 only, else not used: device fp32, contiguous, what an 8-bit value is to be multiplied with: the largest
  *              |out| of those that share it divided by 448 (1 where they are all 0; NaN in a row that holds a NaN or infinity).
  *              scale_block 0: one a row, [rows]; 128: one for each 128 columns, [rows][(width + 127) / 128].
+ *              (Values in 8 bits are for a scaled product of the caller's: no entry point here takes them as an input.)
  * Matrices and norm_w 16-byte aligned; rows 0 .. 2^22, width 1 .. 2^22; otherwise no argument overlaps an output.
  * Errors: BDLM_E_NULL, BDLM_E_SHAPE, BDLM_E_DTYPE, BDLM_E_ALIGN, BDLM_E_LAUNCH.  rows == 0 enqueues nothing.
  */
@@ -564,7 +565,8 @@ int bdlm_projection_backward(const bdlm_dense_desc_t *desc, int32_t act, int32_t
  * out          device [rows][out_features], out_dtype; formed from the unrounded gate and up.
  * pre_gate, pre_up    gate and up, device [rows][out_features], in_dtype, at one stride, both or neither: kept for the gradient.
  *              Where out, pre_gate and pre_up start at the same place modulo the memory's banks and rows are a multiple of 512 elements,
- *              storing them takes longer: 16,384 x 1,024 x 4,096 in bf16 340 us, and 307 where each starts 1 KiB further than the one before.
+ *              storing them takes longer: 16,384 x 1,024 x 4,096 in bf16 320 to 340 us by card, and 303 to 307 where each starts 1 KiB further
+ *              than the one before.
  * Up to 32 rows (fp32: 64) need no workspace.
  * Errors: as bdlm_projection.  rows == 0 enqueues nothing.
  */

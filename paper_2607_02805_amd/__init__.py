@@ -955,7 +955,8 @@ def add_rmsnorm(x, w, residual=None, eps=1e-5, out_dtype=None, out=None, sum=Non
     is s in its type, allocated if None, False if not wanted, or a tensor, ``residual`` itself among them; without a
     residual it is None.  ``out`` has ``out_dtype`` (x's if None): bfloat16, float32, or float8_e4m3fn, whose
     values are to be multiplied with ``scale``, float32 [..., 1] (``scale_block`` 0) or one for every
-    128 columns (``scale_block`` 128): the largest magnitude among them over 448.
+    128 columns (``scale_block`` 128): the largest magnitude among them over 448.  (8-bit values are for a scaled product of
+    the caller's own: no call here takes them as an input.)
 
     No autograd graph is recorded: :func:`add_rmsnorm_backward` has the gradients."""
     torch = _torch()
@@ -1161,7 +1162,7 @@ def _two_weights(x, w_gate, w_up):
 def _apart(shape, x):
     """Two new tensors like x that are written together with a third.  Large ones start 1 and 2 KiB past where tensors start, so
     that the same element of the three does not lie in the same bank of memory (a gated product of 16,384 x 1,024 x 4,096 takes 303
-    us with them and 340 with tensors that start alike)."""
+    to 307 us with them by card, and 320 to 340 with tensors that start alike)."""
     torch = _torch()
     n = 1
     for v in shape:

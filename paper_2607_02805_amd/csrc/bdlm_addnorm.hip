@@ -488,7 +488,8 @@ Way way_of(int64_t width) {
 constexpr int64_t kMostGroups = 2048;   // workgroups of the forward call: eight on a CU
 constexpr int64_t kMostGradGroups = 512;   // of the gradient, each with a row of sums of dw
 // Of the gradient without dw, which every turn of rows can have a workgroup for (16 rows of 1,024: 3.9 us, 8.5 in one workgroup) and
-// which has no sums: 16,384 x 2,048 in bf16 takes 35 us so and 50 with 512, 4,000 x 2,048 12.7 and 16.5, 2,000 x 8,192 38 and 34, 45 with 2,048.
+// which has no sums.  In bf16, inputs not in the caches, 16,384 x 2,048 takes 40 us so and 59 with 512, 60,000 x 448 31 and 47, but
+// 16,384 x 1,024 25.4 and 25.1, 8,000 x 8,192 126 and 121 (138 with 2,048).
 constexpr int64_t kMostStreamGroups = 1024;
 
 // Turns of rows of a gradient's workgroup.
@@ -529,6 +530,7 @@ int grad_of(const AddNormGradArgs &a, hipStream_t s) {
 }  // namespace
 
 int32_t add_norm_grad_blocks(int64_t rows, int64_t width) {
+    // (Times of rows that the caches hold.)
     // Two turns of rows of up to 4,096 columns are one workgroup's, whose dw needs no second launch: 8 rows of 448 columns take 4.1 us
     // so and 5.1 in two launches, 8 of 1,024 5.8 and 6.2, 2 of 4,096 6.0 and 6.4.  Past that the turns one after the other cost more
     // than the launch: 2 rows of 8,192 take 9.5 and 8.7, three turns 12 of 1,024 7.4 and 6.2, 4 rows of 32,768 93 and 26.

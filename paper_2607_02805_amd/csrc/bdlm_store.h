@@ -122,7 +122,7 @@ __device__ __forceinline__ f32x4 gated_bias(const float *bias, int col, int n) {
 // Four consecutive columns of N consecutive rows (`there` of which there are) of a gated product, biases added already:
 // act(gate) * up, of the unrounded ones.  All rows take a step before any takes the next: one after the other, whose chains of
 // reads, exponentials and reciprocals wait for each, the end of a small tile took 2.4 us instead
-// of 1.1 (512 x 1,024 x 4,096 13.7 instead of 12.3, 16,384 rows of it 273 instead of 250).
+// of 1.1 (512 x 1,024 x 4,096 13.7 instead of 12.3, 16,384 rows of it 273 instead of 250, timed in turn on one card; on others the first takes 13.3 to 14).
 template <int N>
 __device__ __forceinline__ void gated4(const GatedArgs &a, f32x4 (&gate)[N], f32x4 (&up)[N], int64_t row, int there, int col) {
     const int n = a.n - col < 4 ? a.n - col : 4;

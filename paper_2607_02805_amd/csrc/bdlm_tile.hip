@@ -698,8 +698,8 @@ __global__ void __launch_bounds__(64 * WR * WC * KS, KS * (BUFS == 2 ? 2 : 1)) b
             // (rows eight apart in a pass: their quads lie in both halves of the banks)
             constexpr int kBatch = 4;
             // Of large tiles, what is kept goes first, one matrix after the other: at sizes of a power of two the three lie at the same places of
-            // memory's banks, and stores to them in turn wait for each other (16,384 x 1,024 x 4,096 took 374 us so, 340 one by one, and
-            // 303 where they lie 1 KiB further from each other, as the binding allocates them, and 306 one by one).
+            // memory's banks, and stores to them in turn wait for each other (16,384 x 1,024 x 4,096 took 374 us so, 340 one by one, 320 on
+            // another card, and 303 where they lie 1 KiB further from each other, as the binding allocates them, and 306 one by one).
             // Rows of other lengths do not meet so and read LDS once: 3,279 x 448 x 1,934 takes 27.4 us, 29.8 one by one, and small
             // tiles 1,000 x 832 x 2,048 13.2 and 13.9.
             const bool first = KS == 1 && a.gated.pre_gate && a.gated.ld_pre % 512 == 0;
