@@ -200,7 +200,9 @@ inline TileArgs product(const Mat &row, bool row_t, const Mat &col, bool col_t, 
 // Terms of a gradient's first operand (dz, or the logits' gradients).  With bf16 inputs they are
 // rounded to bf16, as the activations of the forward products are: the outputs of 16,384 x 1,024 x 4,096 are then
 // off by 0.0023 of their size, where their own rounding makes 0.0017 of it, and a second term would double both
-// products (277 of 352 us).  Of few rows, where an output's errors do not average out and the weights' bytes
+// products (277 of 352 us).  A gated product's gradients are off by 0.00235 so, whatever the sizes (the factors' gradients are rounded as the outputs are,
+// 0.00166 each), and with a second term by 0.00166, but take 1,140 us instead of 606 there, 175 instead of 110 of 2,048 rows, 63 instead of 45 of 512, 38 instead
+// of 31 of 65.  Of few rows, where an output's errors do not average out and the weights' bytes
 // bound the products, two terms are kept; fp32 inputs keep three, and are the choice of a caller who needs more.
 inline int grad_terms(const bdlm_dense_desc_t &d) {
     return d.in_dtype != BDLM_DTYPE_BF16 ? 3 : d.rows <= kFewRows ? 2 : 1;
